@@ -81,7 +81,8 @@ def draw(rng):
         new = rng.choice([1, 1, 1, 2, 4, 7])
         batch = _log(rng, 1, 64)
         # no more cached values, and no more products, than the largest listed case has
-        most = min(64 * 16384 * 8 * 128 // (batch * heads[1] * heads[2]), 64 * 16384 * 64 * 128 // (batch * heads[0] * heads[2] * new), 131072)
+        held = sum(_lengths(listed()[5])[0]) * 128
+        most = min(held * 8 // (batch * heads[1] * heads[2]), held * 64 // (batch * heads[0] * heads[2] * new), 131072)
         c = _attend("", batch, new, _log(rng, max(new, 9), max(most, 17)), heads, fmt, dtype, block, mix)
     elif op == "append":
         batch = _log(rng, 1, 64)
