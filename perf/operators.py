@@ -359,7 +359,7 @@ def _tables_plain(s):
     fits = want <= width
     need = torch.where(fits, need, 0)
     given_back, asked = gone.cumsum(0), need.cumsum(0)
-    granted = fits & (asked <= nf + given_back[-1])
+    granted = fits & ((need == 0) | (asked <= nf + given_back[-1]))
     need = torch.where(granted, need, 0)
     first = asked - torch.where(granted, need, 0)
     # what is given back lies on the free list, in order of the requests and of their blocks; what is asked for comes off its end
