@@ -442,6 +442,189 @@ fluxbin_status_t fluxbin_pack_device(const fluxbin_layer_desc_t *d_desc, const i
                                      size_t d_bytes, void *d_workspace, size_t ws_bytes, void *cuda_stream,
                                      fluxbin_weight_t **out);
 
+/* ---- the attention side of a decode step: positions, an 8-bit block-paged cache, attention over it, its block tables ----
+ *
+ * The paper's decode step is made of the linear layers above; these entry points are what stands between the q/k/v
+ * projections and the output projection of a decoder layer.  (The paper has no counterpart.)
+ *
+ * Conventions, on top of those at the head of this file:
+ *   - Heads come as [token][head][dim]: a pointer, a stride between tokens and a stride between heads, both in
+ *     elements; the elements of a head are contiguous.  A projection's output y [B][ldy] is such a tensor with a token
+ *     stride of ldy and a head stride of head_dim.
+ *   - dtype: FLUXBIN_TYPE_FP16, _FP32 or _BF16.  Arithmetic is fp32; results are rounded once, to nearest even.
+ *   - Every call is asynchronous on cuda_stream, allocates nothing, does not synchronise and can be captured into a
+ *     graph.  Kernels are launched with programmatic stream serialization and wait on the device before they read.
+ *   - Values that live on the device (lengths, slots, block ids, positions) cannot be checked by the host.  The kernels
+ *     check each one against the sizes given here before it becomes an address; what they do with a bad one is stated.
+ */
+#define FLUXBIN_TYPE_FP16 0
+#define FLUXBIN_TYPE_FP32 1
+#define FLUXBIN_TYPE_BF16 2
+
+/*
+ * Rotary positions: in every head the first rotary_dim elements form pairs -- elements i and i + rotary_dim / 2
+ * (interleaved == 0) or 2i and 2i + 1 (interleaved != 0) -- and pair i of a token at position p is turned by the angle
+ * p * f_i and multiplied by `magnitude`; the elements past rotary_dim are copied.
+ *
+ * d_turns[i] is f_i as a 64-bit binary fraction of a turn, round(2^64 * f_i / (2 pi)): the product with a position wraps
+ * around exactly as the angle does, so the angle carries no rounding error that grows with the position.
+ */
+typedef struct {
+    int32_t head_dim, rotary_dim;   /* 2 <= rotary_dim <= head_dim <= 512, rotary_dim even */
+    int32_t interleaved;
+    float magnitude;
+    const uint64_t *d_turns;        /* DEVICE [rotary_dim / 2] */
+} fluxbin_rotary_t;
+
+/*
+ * The frequencies of the pairs, f_i = base^(-2 i / rotary_dim), and how they are stretched for contexts longer than the
+ * weights were trained on (host only):
+ *   FLUXBIN_ROPE_NONE     f_i
+ *   FLUXBIN_ROPE_LINEAR   f_i / factor
+ *   FLUXBIN_ROPE_BASE     base * factor^(d / (d - 2)) in the place of base, d = rotary_dim (needs d > 2)
+ *   FLUXBIN_ROPE_RAMP     f_i for pairs that turn at least `a` times in `original` positions, f_i / factor for pairs
+ *                         that turn at most `b` times, linear in the pair's index between (whole indices at both
+ *                         ends); magnitude 0.1 ln(factor) + 1
+ *   FLUXBIN_ROPE_BANDS    f_i / factor for pairs that turn at most `a` times in `original` positions, f_i for pairs
+ *                         that turn at least `b` times, between them linear in the number of turns
+ * h_turns HOST [rotary_dim / 2], h_magnitude HOST.  Errors: NULL, RANGE (also for parameters a kind cannot use:
+ * factor < 1, original < 1, for RAMP a <= b or b <= 0, for BANDS b <= a or a <= 0), UNSUPPORTED (unknown kind).
+ */
+#define FLUXBIN_ROPE_NONE 0
+#define FLUXBIN_ROPE_LINEAR 1
+#define FLUXBIN_ROPE_BASE 2
+#define FLUXBIN_ROPE_RAMP 3
+#define FLUXBIN_ROPE_BANDS 4
+fluxbin_status_t fluxbin_rotary_frequencies(int32_t rotary_dim, double base, int32_t kind, double factor, double original,
+                                            double a, double b, uint64_t *h_turns, float *h_magnitude);
+
+/*
+ * Turn the heads of q and k (k may be NULL) of `tokens` tokens at d_positions [tokens] (int32, any value; negative
+ * positions turn backwards).  inverse != 0 turns by the negative angle: with magnitude 1 it undoes the call, and it is
+ * the gradient of the call with respect to its input.  Outputs may be the inputs themselves (same pointer and strides).
+ * tokens may be 0.  Errors: NULL, RANGE, UNSUPPORTED (dtype), ALIGNMENT (a pointer that is no multiple of the element
+ * size), CUDA.
+ */
+fluxbin_status_t fluxbin_rotary(const fluxbin_rotary_t *rotary, int32_t dtype, int32_t inverse, int32_t tokens,
+                                const int32_t *d_positions,
+                                const void *d_q, int32_t q_heads, int64_t q_token, int64_t q_head,
+                                void *d_q_out, int64_t qo_token, int64_t qo_head,
+                                const void *d_k, int32_t k_heads, int64_t k_token, int64_t k_head,
+                                void *d_k_out, int64_t ko_token, int64_t ko_head, void *cuda_stream);
+
+/*
+ * A cache of keys and values in 8 bits, in blocks of block_tokens tokens, with one fp32 scale for each block and key
+ * head: an entry stands for (its 8-bit value) * (its block's and head's scale).
+ *
+ *   FLUXBIN_CACHE_INT8   two's complement, -127 .. 127;  scale = largest magnitude / 127
+ *   FLUXBIN_CACHE_E4M3   8-bit floats with 4 exponent and 3 mantissa bits (largest value 448, no infinities);
+ *                        scale = largest magnitude / 448
+ *
+ * Entry (block, head, token of the block, element) is at block * block_stride + head * head_stride +
+ * token * token_stride + element, in bytes, the same for k and v: both orders of the middle axes, and blocks of k and v
+ * that alternate in one buffer, are strides.
+ */
+typedef struct {
+    int32_t num_blocks, block_tokens, kv_heads, head_dim, format;
+    void *d_k, *d_v;                                        /* DEVICE, 16-byte aligned */
+    int64_t block_stride, head_stride, token_stride;        /* multiples of 16 */
+    float *d_k_scale, *d_v_scale;                           /* DEVICE [num_blocks][kv_heads] */
+} fluxbin_kv_cache_t;
+#define FLUXBIN_CACHE_INT8 0
+#define FLUXBIN_CACHE_E4M3 1
+
+/* Dimension rules of a cache (host only): block_tokens a multiple of 16 up to 1024, head_dim 64, 128 or 256
+ * (UNSUPPORTED otherwise), kv_heads >= 1, num_blocks >= 1, num_blocks * block_tokens < 2^31, entries that do not overlap
+ * (RANGE), pointers (NULL, ALIGNMENT). */
+fluxbin_status_t fluxbin_kv_validate(const fluxbin_kv_cache_t *cache);
+
+/*
+ * Quantise the keys and values of new tokens and store token t at slot d_slots[t] = block * block_tokens + offset
+ * (int32; negative or too large: the token is skipped).  The tokens of one block must be consecutive in the call, at
+ * consecutive offsets.  Per block, head and side:
+ *   - entered at offset 0, a block starts anew: scale = (largest magnitude of its new entries) / top;
+ *   - entered later, its scale is kept unless a new entry exceeds it; then the scale grows to that entry's and the
+ *     entries before the first new one are requantised from what they stood for.
+ * Entries past the last new token are not touched.  A scale below 2^-100 counts as 0 (all its entries stand for 0); an
+ * infinity or NaN among the new entries makes the scale NaN, so that whoever reads the block sees it.
+ *
+ * rotary (may be NULL): the keys are turned to d_positions in fp32 before they are quantised, and the q heads of the
+ * same tokens (d_q may be NULL) are turned into d_q_out (may be d_q with the same strides).  Without rotary the d_q and
+ * d_positions arguments are not looked at.  dtype is that of k, v and q.
+ * Errors: as fluxbin_kv_validate; NULL, RANGE, UNSUPPORTED (dtype; a rotary for another head_dim), ALIGNMENT, CUDA.
+ */
+fluxbin_status_t fluxbin_kv_append(const fluxbin_kv_cache_t *cache, int32_t dtype, int32_t tokens, const int32_t *d_slots,
+                                   const void *d_k, int64_t k_token, int64_t k_head, const void *d_v, int64_t v_token, int64_t v_head,
+                                   const fluxbin_rotary_t *rotary, const int32_t *d_positions,
+                                   const void *d_q, int32_t q_heads, int64_t q_token, int64_t q_head,
+                                   void *d_q_out, int64_t qo_token, int64_t qo_head, void *cuda_stream);
+
+/* The keys and values that the entries at `tokens` slots stand for, contiguous [tokens][kv_heads][head_dim] of dtype
+ * (d_k_out or d_v_out may be NULL); zeros for a slot outside the cache.  Errors as fluxbin_kv_append. */
+fluxbin_status_t fluxbin_kv_read(const fluxbin_kv_cache_t *cache, int32_t dtype, int32_t tokens, const int32_t *d_slots,
+                                 void *d_k_out, void *d_v_out, void *cuda_stream);
+
+/*
+ * Attention of new tokens over the cache:  out[t][h] = sum_j softmax_j(scale * q[t][h] . K[j]) V[j]  with the keys and
+ * values of key head h / (q_heads / kv_heads), over the cached tokens j of the token's request up to the token itself.
+ *
+ *   d_query_start   DEVICE int32 [batch + 1], ascending: request r asks with tokens query_start[r] ..
+ *                   query_start[r + 1] - 1 of q, which are its last ones (already appended).  NULL: one token a request
+ *                   (tokens == batch).  Entries are clamped to [0, tokens].
+ *   d_lengths       DEVICE int32 [batch]: cached tokens of each request, the new ones included.  0 (or less) leaves the
+ *                   request's rows empty; a length past block_table_width * block_tokens is cut to that.
+ *   d_block_table   DEVICE int32 [batch][block_table_stride]: block of tokens 0.., block_tokens.., ...; entries past the
+ *                   length are not read; tokens of a block id outside the cache are masked out.
+ *   d_q, d_out      fp16 or bf16 heads; 16-byte aligned, strides multiples of 8 elements
+ *   d_lse           DEVICE fp32 [tokens][q_heads] or NULL: log of the sum of exp(scale * q . k) (natural)
+ * A row that sees nothing gets out = 0 and lse = -inf.  What lies in the cache past a request's length (NaN patterns
+ * included) has no influence.  Scores, maxima, sums and accumulators are fp32; the probabilities of a step and the
+ * 8-bit entries enter the matrix instructions as fp16 (8-bit entries exactly).  Results do not depend on timing: sums
+ * are joined in a fixed order.
+ * d_workspace: fluxbin_kv_attend_workspace_size bytes, zeroed once with fluxbin_workspace_init; calls leave its counters
+ * zeroed, and calls that share one must be ordered on a stream.
+ * Errors: as fluxbin_kv_validate; NULL, RANGE (q_heads no multiple of kv_heads, tokens != batch without query_start),
+ * UNSUPPORTED (dtype), ALIGNMENT, BUFFER_TOO_SMALL, CUDA.
+ */
+size_t fluxbin_kv_attend_workspace_size(int32_t batch, int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim);
+fluxbin_status_t fluxbin_kv_attend(const fluxbin_kv_cache_t *cache, int32_t dtype, int32_t batch, int32_t tokens,
+                                   const void *d_q, int32_t q_heads, int64_t q_token, int64_t q_head,
+                                   const int32_t *d_query_start, const int32_t *d_lengths,
+                                   const int32_t *d_block_table, int64_t block_table_stride, int32_t block_table_width,
+                                   float scale, void *d_out, int64_t out_token, int64_t out_head, float *d_lse,
+                                   void *d_workspace, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * Move a batch of requests on by one step, on the device: from the length of each request and its count of new tokens
+ * to its new length, its blocks and the slots of its tokens.
+ *
+ *   d_lengths     int32 [batch]: cached tokens of each request before the step (negative reads as 0)
+ *   d_new         int32 [batch]: > 0 tokens to add, 0 nothing, < 0 tokens to drop off the end (more than there are: all)
+ *   d_table       int32 [batch][table_stride], in and out: the requests' blocks; entries of blocks taken are written,
+ *                 entries of blocks given back are left as they are
+ *   d_free        int32 [free_capacity], in and out: the ids of the free blocks are its first d_num_free[0] entries.
+ *                 The blocks that requests give back go behind them, in order of the requests and of their blocks; the
+ *                 blocks asked for are taken off the end of that list, in the same order.
+ * A request that grows is granted its blocks if those of all growing requests up to and including it fit into the free
+ * list (one that needs no further block always is), and its table has room for them; a request whose table has no room
+ * is left out of that count.  A request that is not granted keeps its length, and its tokens get slot -1 (and are
+ * skipped by fluxbin_kv_append).  A length that does not fit the table's width gives nothing back.
+ *
+ *   d_num_free_out, d_lengths_out, d_granted   int32 [1], [batch], [batch] (0 or 1)
+ *   d_query_start                              int32 [batch + 1]: first token of each request among the new ones
+ *   d_positions, d_slots, d_requests           int32 [tokens]: position, slot and request of every new token; tokens past
+ *                                              the last request's get position 0, slot -1 and request -1
+ * Outputs must not overlap inputs (d_table and d_free excepted).  batch <= 8192.  `tokens` is the length of the token
+ * arrays (0 allowed); new tokens past it are not written.
+ * Errors: NULL, RANGE, CUDA.
+ */
+fluxbin_status_t fluxbin_kv_advance(int32_t batch, int32_t tokens, int32_t block_tokens, const int32_t *d_lengths,
+                                    const int32_t *d_new, int32_t *d_table, int64_t table_stride, int32_t table_width,
+                                    int32_t *d_free, int32_t free_capacity, const int32_t *d_num_free,
+                                    int32_t *d_num_free_out, int32_t *d_lengths_out, int32_t *d_granted,
+                                    int32_t *d_query_start, int32_t *d_positions, int32_t *d_slots, int32_t *d_requests,
+                                    void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,255 @@
+"""The attention side of a decode step on torch tensors: rotary positions, the 8-bit block-paged key/value cache, attention
+over it and the block tables both go by.  torch owns the memory and the stream, the C-ABI library does the work
+(include/fluxbin.h states every rule); the checks here are those of types and shapes that the C side cannot see.
+
+    rope = Rotary(128)
+    cache = KVCache(num_blocks, 16, kv_heads=8, head_dim=128, fmt="int8")
+    tables = BlockTables.empty(batch, max_blocks, num_blocks, 16)
+    step = tables.advance(lengths, new_tokens, num_free, tokens)          # blocks, positions and slots of the new tokens
+    q = cache.append(k, v, step.slots, rotary=rope, positions=step.positions, q=q)
+    out = cache.attend(q, tables.table, step.lengths, ws, query_start=step.query_start)
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+from types import SimpleNamespace
+
+import torch
+
+from . import fluxbin
+from .layer import Workspace, _stream_ptr
+
+_TYPES = {torch.float16: fluxbin.TYPE_FP16, torch.float32: fluxbin.TYPE_FP32, torch.bfloat16: fluxbin.TYPE_BF16}
+_STORED = {torch.int8: fluxbin.CACHE_INT8, torch.float8_e4m3fn: fluxbin.CACHE_E4M3}
+_FORMATS = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}
+_KINDS = {"none": fluxbin.ROPE_NONE, "linear": fluxbin.ROPE_LINEAR, "base": fluxbin.ROPE_BASE, "ramp": fluxbin.ROPE_RAMP,
+          "bands": fluxbin.ROPE_BANDS}
+
+
+def _check(status: int, where: str):
+    if status:
+        raise fluxbin.FluxBinError(status, where)
+
+
+def _heads(x: torch.Tensor, tokens: int, dim: int, dtype: torch.dtype, what: str):
+    """(pointer, heads, token stride, head stride) of a [tokens][heads][dim] tensor with contiguous heads."""
+    if x.dtype is not dtype or x.dim() != 3 or not x.is_cuda:
+        raise TypeError(f"{what}: a CUDA tensor [tokens][heads][dim] of {dtype} is wanted")
+    t, h, d = x.shape
+    if t != tokens or d != dim:
+        raise ValueError(f"{what}: shape {tuple(x.shape)}, wanted [{tokens}][heads][{dim}]")
+    st, sh, se = x.stride()
+    if se != 1:
+        raise ValueError(f"{what}: the elements of a head have to be contiguous")
+    return x.data_ptr(), h, st, sh
+
+
+def _int32(x: torch.Tensor, n: int, what: str) -> int:
+    if x.dtype is not torch.int32 or not x.is_cuda or x.dim() != 1 or x.shape[0] != n or (n > 1 and x.stride(0) != 1):
+        raise ValueError(f"{what}: a contiguous CUDA int32 tensor of {n} elements is wanted")
+    return x.data_ptr()
+
+
+class Rotary:
+    """Rotary positions (fluxbin_rotary): the frequencies live on the device, angles are formed in the kernels.
+
+    `scaling`: "none", "linear" (factor), "base" (factor), "ramp" (factor, original, fast, slow) or "bands" (factor, original,
+    low, high), see fluxbin_rotary_frequencies."""
+
+    def __init__(self, head_dim: int, rotary_dim: int | None = None, base: float = 10000.0, interleaved: bool = False,
+                 scaling: str = "none", factor: float = 1.0, original: float = 1.0, fast: float = 32.0, slow: float = 1.0,
+                 low: float = 1.0, high: float = 4.0, device="cuda"):
+        if scaling not in _KINDS:
+            raise ValueError(f"scaling: one of {sorted(_KINDS)} is wanted")
+        self.head_dim, self.rotary_dim, self.interleaved = head_dim, rotary_dim or head_dim, bool(interleaved)
+        if self.rotary_dim > head_dim:
+            raise fluxbin.FluxBinError(3, "Rotary: rotary_dim past head_dim")
+        a, b = (fast, slow) if scaling == "ramp" else (low, high)
+        turns, self.magnitude = fluxbin.rotary_frequencies(self.rotary_dim, base, _KINDS[scaling], factor, original, a, b)
+        self.turns = torch.from_numpy(turns.view("int64")).to(device)
+        self.desc = fluxbin.RotaryDesc(head_dim, self.rotary_dim, int(self.interleaved), self.magnitude, self.turns.data_ptr())
+        self._ref = ctypes.addressof(self.desc)
+
+    def apply(self, q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor, inverse: bool = False,
+              q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, stream=None):
+        """q, k [tokens][heads][head_dim] turned to positions [tokens] (int32); outputs may be the inputs.  `inverse` turns
+        back: the gradient of the turned heads with respect to q and k.  Returns (q_out, k_out), k_out None without k."""
+        n = q.shape[0]
+        dt = q.dtype
+        if dt not in _TYPES:
+            raise TypeError("q: fp16, bf16 or fp32 is wanted")
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=dt, device=q.device)
+        qp, qh, qt, qs = _heads(q, n, self.head_dim, dt, "q")
+        op, oh, ot, os_ = _heads(q_out, n, self.head_dim, dt, "q_out")
+        if oh != qh:
+            raise ValueError("q_out: as many heads as q are wanted")
+        kp = kop = None
+        kh = kt = ks = kot = kos = 0
+        if k is not None:
+            if k_out is None:
+                k_out = torch.empty(k.shape, dtype=dt, device=k.device)
+            kp, kh, kt, ks = _heads(k, n, self.head_dim, dt, "k")
+            kop, koh, kot, kos = _heads(k_out, n, self.head_dim, dt, "k_out")
+            if koh != kh:
+                raise ValueError("k_out: as many heads as k are wanted")
+        else:
+            k_out = None
+        _check(fluxbin.rotary_status(self._ref, _TYPES[dt], int(inverse), n, _int32(positions, n, "positions"), qp, qh, qt, qs, op, ot, os_,
+                                     kp, kh, kt, ks, kop, kot, kos, _stream_ptr(stream)), "fluxbin_rotary")
+        return q_out, k_out
+
+
+class KVCache:
+    """Keys and values in 8 bits, in blocks of tokens, one scale for each block and key head (fluxbin_kv_cache_t).
+
+    `k`, `v`: [num_blocks][kv_heads][block_tokens][head_dim] int8 or float8_e4m3fn tensors (any strides with contiguous
+    elements, the same for both); `k_scale`, `v_scale`: fp32 [num_blocks][kv_heads].  `token_major` lays a block out as
+    [block_tokens][kv_heads][head_dim] in memory."""
+
+    def __init__(self, num_blocks: int, block_tokens: int, kv_heads: int, head_dim: int, fmt: str = "int8", token_major: bool = False,
+                 device="cuda"):
+        if fmt not in _FORMATS:
+            raise ValueError(f"fmt: one of {sorted(_FORMATS)} is wanted")
+        shape = (num_blocks, block_tokens, kv_heads, head_dim) if token_major else (num_blocks, kv_heads, block_tokens, head_dim)
+        k, v = (torch.zeros(shape, dtype=torch.int8, device=device).view(_FORMATS[fmt]) for _ in range(2))
+        if token_major:
+            k, v = k.transpose(1, 2), v.transpose(1, 2)
+        scales = (torch.zeros((num_blocks, kv_heads), dtype=torch.float32, device=device) for _ in range(2))
+        self._set(k, v, *scales)
+
+    @classmethod
+    def wrap(cls, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor) -> "KVCache":
+        """A cache over tensors that are there already."""
+        c = object.__new__(cls)
+        c._set(k, v, k_scale, v_scale)
+        return c
+
+    def _set(self, k, v, k_scale, v_scale):
+        if k.dtype not in _STORED or v.dtype is not k.dtype:
+            raise TypeError("k, v: int8 or float8_e4m3fn is wanted")
+        if k.dim() != 4 or v.shape != k.shape or v.stride() != k.stride() or k.stride(3) != 1:
+            raise ValueError("k, v: [num_blocks][kv_heads][block_tokens][head_dim] with the same strides and contiguous elements are wanted")
+        nb, H, bs, D = k.shape
+        for s in (k_scale, v_scale):
+            if s.dtype is not torch.float32 or s.shape != (nb, H) or not s.is_contiguous():
+                raise ValueError("scales: contiguous fp32 [num_blocks][kv_heads] is wanted")
+        if len({t.device for t in (k, v, k_scale, v_scale)}) != 1:
+            raise ValueError("k, v and the scales have to be on one device")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.num_blocks, self.kv_heads, self.block_tokens, self.head_dim, self.device = nb, H, bs, D, k.device
+        self.desc = fluxbin.CacheDesc(nb, bs, H, D, _STORED[k.dtype], k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
+                                      k_scale.data_ptr(), v_scale.data_ptr())
+        self._ref = ctypes.addressof(self.desc)
+        _check(fluxbin.kv_validate_status(self.desc), "fluxbin_kv_validate")
+
+    def append(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, rotary: Rotary | None = None,
+               positions: torch.Tensor | None = None, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None, stream=None):
+        """fluxbin_kv_append: quantise and store k, v [tokens][kv_heads][head_dim] at `slots` [tokens] (int32).  With `rotary` the
+        keys, and the q heads if given, are turned to `positions` on the way; returns the turned q (else None)."""
+        n, dt = k.shape[0], k.dtype
+        if dt not in _TYPES:
+            raise TypeError("k: fp16, bf16 or fp32 is wanted")
+        kp, kh, kt, ks = _heads(k, n, self.head_dim, dt, "k")
+        vp, vh, vt, vs = _heads(v, n, self.head_dim, dt, "v")
+        if kh != self.kv_heads or vh != self.kv_heads:
+            raise ValueError(f"k, v: {self.kv_heads} heads are wanted")
+        rp = pp = qp = op = None
+        qh = qt = qs = ot = os_ = 0
+        if rotary is not None:
+            if positions is None:
+                raise ValueError("positions are wanted with rotary")
+            rp, pp = rotary._ref, _int32(positions, n, "positions")
+            if q is not None:
+                if q_out is None:
+                    q_out = torch.empty(q.shape, dtype=dt, device=q.device)
+                qp, qh, qt, qs = _heads(q, n, self.head_dim, dt, "q")
+                op, oh, ot, os_ = _heads(q_out, n, self.head_dim, dt, "q_out")
+                if oh != qh:
+                    raise ValueError("q_out: as many heads as q are wanted")
+        elif q is not None:
+            raise ValueError("q is only turned with rotary")
+        _check(fluxbin.kv_append_status(self._ref, _TYPES[dt], n, _int32(slots, n, "slots"), kp, kt, ks, vp, vt, vs, rp, pp, qp, qh, qt, qs,
+                                        op, ot, os_, _stream_ptr(stream)), "fluxbin_kv_append")
+        return q_out if q is not None else None
+
+    def read(self, slots: torch.Tensor, dtype: torch.dtype = torch.float16, stream=None):
+        """fluxbin_kv_read: the keys and values that the entries at `slots` stand for, two [tokens][kv_heads][head_dim] tensors."""
+        if dtype not in _TYPES:
+            raise TypeError("dtype: fp16, bf16 or fp32 is wanted")
+        n = slots.shape[0]
+        k = torch.empty((n, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
+        v = torch.empty_like(k)
+        _check(fluxbin.kv_read_status(self._ref, _TYPES[dtype], n, _int32(slots, n, "slots"), k.data_ptr(), v.data_ptr(), _stream_ptr(stream)),
+               "fluxbin_kv_read")
+        return k, v
+
+    def workspace(self, batch: int, tokens: int, q_heads: int) -> Workspace:
+        """The workspace of attend() for up to `batch` requests with `tokens` new tokens in all."""
+        n = fluxbin.kv_attend_workspace_size(batch, tokens, q_heads, self.kv_heads, self.head_dim)
+        if n == 0:
+            raise ValueError("workspace: batch >= 1, tokens >= 0 and a multiple of kv_heads for q_heads are wanted")
+        return Workspace(n, self.device)
+
+    def attend(self, q: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, ws: Workspace, query_start: torch.Tensor | None = None,
+               scale: float | None = None, out: torch.Tensor | None = None, with_lse: bool = False, stream=None):
+        """fluxbin_kv_attend: q [tokens][q_heads][head_dim] (fp16 or bf16) over the cached tokens of its requests.
+
+        `table` int32 [batch][max_blocks], `lengths` int32 [batch] (the new tokens included), `query_start` int32
+        [batch + 1] or None for one token a request, `scale` head_dim ** -0.5 if not given.  Returns out [tokens][q_heads]
+        [head_dim], with `with_lse` also the natural log of each row's sum, fp32 [tokens][q_heads]."""
+        n, dt = q.shape[0], q.dtype
+        if dt is not torch.float16 and dt is not torch.bfloat16:
+            raise TypeError("q: fp16 or bf16 is wanted")
+        qp, qh, qt, qs = _heads(q, n, self.head_dim, dt, "q")
+        if table.dtype is not torch.int32 or table.dim() != 2 or not table.is_cuda or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("table: a CUDA int32 tensor [batch][max_blocks] with contiguous rows is wanted")
+        B, width = table.shape
+        if out is None:
+            out = torch.empty(q.shape, dtype=dt, device=q.device)
+        op, oh, ot, os_ = _heads(out, n, self.head_dim, dt, "out")
+        if oh != qh:
+            raise ValueError("out: as many heads as q are wanted")
+        lse = torch.empty((n, qh), dtype=torch.float32, device=q.device) if with_lse else None
+        _check(fluxbin.kv_attend_status(self._ref, _TYPES[dt], B, n, qp, qh, qt, qs,
+                                        None if query_start is None else _int32(query_start, B + 1, "query_start"),
+                                        _int32(lengths, B, "lengths"), table.data_ptr(), max(table.stride(0), width), width,
+                                        1.0 / math.sqrt(self.head_dim) if scale is None else scale, op, ot, os_,
+                                        None if lse is None else lse.data_ptr(), ws.tensor.data_ptr(), ws.nbytes, _stream_ptr(stream)),
+               "fluxbin_kv_attend")
+        return (out, lse) if with_lse else out
+
+
+class BlockTables:
+    """The blocks of a batch of requests and the free list they come from (fluxbin_kv_advance).
+
+    `table` int32 [batch][max_blocks] and `free` int32 [capacity] are changed in place by advance(); the lengths and the
+    number of free blocks go in and come out, so a step's outputs are the next step's inputs."""
+
+    def __init__(self, table: torch.Tensor, free: torch.Tensor, block_tokens: int):
+        if table.dtype is not torch.int32 or table.dim() != 2 or not table.is_cuda or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("table: a CUDA int32 tensor [batch][max_blocks] with contiguous rows is wanted")
+        self.table, self.free, self.block_tokens = table, free, block_tokens
+        self._free = _int32(free, free.shape[0], "free")
+        self.batch, self.max_blocks = table.shape
+        self._args = (table.data_ptr(), max(table.stride(0), table.shape[1]), table.shape[1], self._free, free.shape[0])
+
+    @classmethod
+    def empty(cls, batch: int, max_blocks: int, num_blocks: int, block_tokens: int, device="cuda") -> "BlockTables":
+        """No request holds a block yet: all num_blocks are free (the number of free blocks starts as num_blocks)."""
+        return cls(torch.full((batch, max_blocks), -1, dtype=torch.int32, device=device),
+                   torch.arange(num_blocks - 1, -1, -1, dtype=torch.int32, device=device), block_tokens)
+
+    def advance(self, lengths: torch.Tensor, new_tokens: torch.Tensor, num_free: torch.Tensor, tokens: int, stream=None) -> SimpleNamespace:
+        """One step: `new_tokens` int32 [batch] tokens to add (> 0) or drop (< 0), `tokens` the sum of those to add.  Returns
+        lengths, num_free, granted, query_start, positions, slots, requests (int32 tensors, all new)."""
+        B = self.batch
+        buf = torch.empty(3 * B + 2 + 3 * tokens, dtype=torch.int32, device=self.table.device)
+        nfo, lo, gr, qs, po, sl, rq = buf.split((1, B, B, B + 1, tokens, tokens, tokens))
+        p = buf.data_ptr()
+        o = p + 4 * (3 * B + 2)
+        _check(fluxbin.kv_advance_status(B, tokens, self.block_tokens, _int32(lengths, B, "lengths"), _int32(new_tokens, B, "new_tokens"),
+                                         *self._args, _int32(num_free, 1, "num_free"), p, p + 4, p + 4 + 4 * B, p + 4 + 8 * B,
+                                         o, o + 4 * tokens, o + 8 * tokens, _stream_ptr(stream)), "fluxbin_kv_advance")
+        return SimpleNamespace(num_free=nfo, lengths=lo, granted=gr, query_start=qs, positions=po, slots=sl, requests=rq)

@@ -42,7 +42,27 @@ EXPORTS = ["fluxbin_packed_size", "fluxbin_validate", "fluxbin_pack_host", "flux
            "fluxbin_plan_free",
            "fluxbin_linear_noalloc", "fluxbin_noalloc_capacity", "fluxbin_set_table_format", "fluxbin_get_table_format",
            "fluxbin_rc_decomp", "fluxbin_rc_decomp_workspace_size", "fluxbin_rc_decomp_passes",
-           "fluxbin_rc_salient_collect", "fluxbin_pack_device", "fluxbin_pack_device_workspace_size", "fluxbin_rc_salient_residual"]
+           "fluxbin_rc_salient_collect", "fluxbin_pack_device", "fluxbin_pack_device_workspace_size", "fluxbin_rc_salient_residual",
+           "fluxbin_rotary_frequencies", "fluxbin_rotary", "fluxbin_kv_validate", "fluxbin_kv_append", "fluxbin_kv_read",
+           "fluxbin_kv_attend_workspace_size", "fluxbin_kv_attend", "fluxbin_kv_advance"]
+
+TYPE_FP16, TYPE_FP32, TYPE_BF16 = 0, 1, 2
+CACHE_INT8, CACHE_E4M3 = 0, 1
+ROPE_NONE, ROPE_LINEAR, ROPE_BASE, ROPE_RAMP, ROPE_BANDS = 0, 1, 2, 3, 4
+
+
+class RotaryDesc(ctypes.Structure):
+    """fluxbin_rotary_t"""
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("magnitude", ctypes.c_float), ("d_turns", ctypes.c_void_p)]
+
+
+class CacheDesc(ctypes.Structure):
+    """fluxbin_kv_cache_t"""
+    _fields_ = [("num_blocks", ctypes.c_int32), ("block_tokens", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("format", ctypes.c_int32), ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p),
+                ("block_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("d_k_scale", ctypes.c_void_p), ("d_v_scale", ctypes.c_void_p)]
 
 _LIB = None
 
@@ -111,6 +131,22 @@ def _lib():
         lib.fluxbin_pack_device_workspace_size.restype, lib.fluxbin_pack_device_workspace_size.argtypes = sz, [i32, i32, i32]
         lib.fluxbin_pack_device.restype = ctypes.c_int
         lib.fluxbin_pack_device.argtypes = [dp, vp, vp, sz, vp, sz, vp, ctypes.POINTER(vp)]
+        f64, f32 = ctypes.c_double, ctypes.c_float
+        lib.fluxbin_rotary_frequencies.restype = ctypes.c_int
+        lib.fluxbin_rotary_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, vp, ctypes.POINTER(f32)]
+        heads = [vp, i32, i64, i64]
+        lib.fluxbin_rotary.restype = ctypes.c_int
+        lib.fluxbin_rotary.argtypes = [vp, i32, i32, i32, vp] + heads + [vp, i64, i64] + heads + [vp, i64, i64, vp]
+        lib.fluxbin_kv_validate.restype, lib.fluxbin_kv_validate.argtypes = ctypes.c_int, [vp]
+        lib.fluxbin_kv_append.restype = ctypes.c_int
+        lib.fluxbin_kv_append.argtypes = [vp, i32, i32, vp, vp, i64, i64, vp, i64, i64, vp, vp] + heads + [vp, i64, i64, vp]
+        lib.fluxbin_kv_read.restype, lib.fluxbin_kv_read.argtypes = ctypes.c_int, [vp, i32, i32, vp, vp, vp, vp]
+        lib.fluxbin_kv_attend_workspace_size.restype = sz
+        lib.fluxbin_kv_attend_workspace_size.argtypes = [i32] * 5
+        lib.fluxbin_kv_attend.restype = ctypes.c_int
+        lib.fluxbin_kv_attend.argtypes = [vp, i32, i32, i32] + heads + [vp, vp, vp, i64, i32, f32, vp, i64, i64, vp, vp, sz, vp]
+        lib.fluxbin_kv_advance.restype = ctypes.c_int
+        lib.fluxbin_kv_advance.argtypes = [i32, i32, i32, vp, vp, vp, i64, i32, vp, i32] + [vp] * 8 + [vp]
         _LIB = lib
     return _LIB
 
@@ -431,3 +467,44 @@ def plan_create(weights, d_x, ldx, d_y, ldy, B, y_is_fp32, d_table, table_bytes,
         st, h = plan_create_status(weights, d_x, ldx, d_y, ldy, B, y_is_fp32, d_table, table_bytes, d_ws, ws_bytes, stream)
         _check(st, "fluxbin_plan_create")
     return Plan(h, (list(weights), keep))
+
+
+# ---- the attention side of a decode step --------------------------------------------------------------------------
+
+def rotary_frequencies(rotary_dim: int, base: float = 10000.0, kind: int = ROPE_NONE, factor: float = 1.0, original: float = 1.0,
+                       a: float = 0.0, b: float = 0.0):
+    """fluxbin_rotary_frequencies: (turns per position as uint64 binary fractions [rotary_dim / 2], magnitude)."""
+    turns = np.zeros(max(1, rotary_dim // 2), np.uint64)
+    magnitude = ctypes.c_float()
+    _check(_lib().fluxbin_rotary_frequencies(rotary_dim, base, kind, factor, original, a, b, turns.ctypes.data, ctypes.byref(magnitude)),
+           "fluxbin_rotary_frequencies")
+    return turns, magnitude.value
+
+
+def rotary_status(*args) -> int:
+    """fluxbin_rotary with the arguments of the C call (the descriptor by ctypes.byref)."""
+    return _lib().fluxbin_rotary(*args)
+
+
+def kv_validate_status(desc: CacheDesc) -> int:
+    return _lib().fluxbin_kv_validate(ctypes.byref(desc))
+
+
+def kv_append_status(*args) -> int:
+    return _lib().fluxbin_kv_append(*args)
+
+
+def kv_read_status(*args) -> int:
+    return _lib().fluxbin_kv_read(*args)
+
+
+def kv_attend_status(*args) -> int:
+    return _lib().fluxbin_kv_attend(*args)
+
+
+def kv_attend_workspace_size(batch: int, tokens: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(_lib().fluxbin_kv_attend_workspace_size(batch, tokens, q_heads, kv_heads, head_dim))
+
+
+def kv_advance_status(*args) -> int:
+    return _lib().fluxbin_kv_advance(*args)
