@@ -625,6 +625,19 @@ fluxbin_status_t fluxbin_kv_advance(int32_t batch, int32_t tokens, int32_t block
                                     int32_t *d_query_start, int32_t *d_positions, int32_t *d_slots, int32_t *d_requests,
                                     void *cuda_stream);
 
+/*
+ * The calls above with their arguments, in order, as an array of 64-bit words (integers and pointers as they are, `scale`
+ * as a double): for bindings that pay for every argument they convert -- a decode step makes these calls in every layer,
+ * and converting 20 arguments takes ctypes longer than the whole call takes without.  Checks, results and errors are
+ * those of the call; UNSUPPORTED for an unknown one.
+ */
+#define FLUXBIN_CALL_ROTARY 0
+#define FLUXBIN_CALL_KV_APPEND 1
+#define FLUXBIN_CALL_KV_READ 2
+#define FLUXBIN_CALL_KV_ATTEND 3
+#define FLUXBIN_CALL_KV_ADVANCE 4
+fluxbin_status_t fluxbin_call_words(int32_t which, const int64_t *h_words);
+
 #ifdef __cplusplus
 }
 #endif

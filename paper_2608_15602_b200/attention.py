@@ -27,9 +27,9 @@ _KINDS = {"none": fluxbin.ROPE_NONE, "linear": fluxbin.ROPE_LINEAR, "base": flux
           "bands": fluxbin.ROPE_BANDS}
 
 
-def _check(status: int, where: str):
-    if status:
-        raise fluxbin.FluxBinError(status, where)
+def _stream(x: torch.Tensor, stream) -> int:
+    """The raw stream of a call: `stream`, or the current one of the tensor's device."""
+    return torch._C._cuda_getCurrentRawStream(x.device.index) if stream is None else _stream_ptr(stream)
 
 
 def _heads(x: torch.Tensor, tokens: int, dim: int, dtype: torch.dtype, what: str):
@@ -46,9 +46,18 @@ def _heads(x: torch.Tensor, tokens: int, dim: int, dtype: torch.dtype, what: str
 
 
 def _int32(x: torch.Tensor, n: int, what: str) -> int:
-    if x.dtype is not torch.int32 or not x.is_cuda or x.dim() != 1 or x.shape[0] != n or (n > 1 and x.stride(0) != 1):
+    if x.dtype is not torch.int32 or not x.is_cuda or x.shape != (n,) or (n > 1 and x.stride(0) != 1):
         raise ValueError(f"{what}: a contiguous CUDA int32 tensor of {n} elements is wanted")
     return x.data_ptr()
+
+
+def _output(given: torch.Tensor | None, like: torch.Tensor, heads: int, what: str):
+    """An output like a [tokens][heads][dim] input: (tensor, pointer, token stride, head stride)."""
+    y = torch.empty_like(like) if given is None else given
+    p, h, st, sh = _heads(y, like.shape[0], like.shape[2], like.dtype, what)
+    if h != heads:
+        raise ValueError(f"{what}: {heads} heads are wanted")
+    return y, p, st, sh
 
 
 class Rotary:
@@ -75,29 +84,19 @@ class Rotary:
               q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, stream=None):
         """q, k [tokens][heads][head_dim] turned to positions [tokens] (int32); outputs may be the inputs.  `inverse` turns
         back: the gradient of the turned heads with respect to q and k.  Returns (q_out, k_out), k_out None without k."""
-        n = q.shape[0]
-        dt = q.dtype
+        n, dt = q.shape[0], q.dtype
         if dt not in _TYPES:
             raise TypeError("q: fp16, bf16 or fp32 is wanted")
-        if q_out is None:
-            q_out = torch.empty(q.shape, dtype=dt, device=q.device)
         qp, qh, qt, qs = _heads(q, n, self.head_dim, dt, "q")
-        op, oh, ot, os_ = _heads(q_out, n, self.head_dim, dt, "q_out")
-        if oh != qh:
-            raise ValueError("q_out: as many heads as q are wanted")
-        kp = kop = None
-        kh = kt = ks = kot = kos = 0
-        if k is not None:
-            if k_out is None:
-                k_out = torch.empty(k.shape, dtype=dt, device=k.device)
-            kp, kh, kt, ks = _heads(k, n, self.head_dim, dt, "k")
-            kop, koh, kot, kos = _heads(k_out, n, self.head_dim, dt, "k_out")
-            if koh != kh:
-                raise ValueError("k_out: as many heads as k are wanted")
-        else:
+        q_out, op, ot, os_ = _output(q_out, q, qh, "q_out")
+        kp = kh = kt = ks = kop = kot = kos = 0
+        if k is None:
             k_out = None
-        _check(fluxbin.rotary_status(self._ref, _TYPES[dt], int(inverse), n, _int32(positions, n, "positions"), qp, qh, qt, qs, op, ot, os_,
-                                     kp, kh, kt, ks, kop, kot, kos, _stream_ptr(stream)), "fluxbin_rotary")
+        else:
+            kp, kh, kt, ks = _heads(k, n, self.head_dim, dt, "k")
+            k_out, kop, kot, kos = _output(k_out, k, kh, "k_out")
+        fluxbin.rotary_call(self._ref, _TYPES[dt], inverse, n, _int32(positions, n, "positions"), qp, qh, qt, qs, op, ot, os_,
+                            kp, kh, kt, ks, kop, kot, kos, _stream(q, stream))
         return q_out, k_out
 
 
@@ -141,8 +140,10 @@ class KVCache:
         self.num_blocks, self.kv_heads, self.block_tokens, self.head_dim, self.device = nb, H, bs, D, k.device
         self.desc = fluxbin.CacheDesc(nb, bs, H, D, _STORED[k.dtype], k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
                                       k_scale.data_ptr(), v_scale.data_ptr())
-        self._ref = ctypes.addressof(self.desc)
-        _check(fluxbin.kv_validate_status(self.desc), "fluxbin_kv_validate")
+        self._ref, self._scale = ctypes.addressof(self.desc), 1.0 / math.sqrt(D)
+        status = fluxbin.kv_validate_status(self.desc)
+        if status:
+            raise fluxbin.FluxBinError(status, "fluxbin_kv_validate")
 
     def append(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, rotary: Rotary | None = None,
                positions: torch.Tensor | None = None, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None, stream=None):
@@ -155,34 +156,28 @@ class KVCache:
         vp, vh, vt, vs = _heads(v, n, self.head_dim, dt, "v")
         if kh != self.kv_heads or vh != self.kv_heads:
             raise ValueError(f"k, v: {self.kv_heads} heads are wanted")
-        rp = pp = qp = op = None
-        qh = qt = qs = ot = os_ = 0
+        rp = pp = qp = qh = qt = qs = op = ot = os_ = 0
         if rotary is not None:
             if positions is None:
                 raise ValueError("positions are wanted with rotary")
             rp, pp = rotary._ref, _int32(positions, n, "positions")
             if q is not None:
-                if q_out is None:
-                    q_out = torch.empty(q.shape, dtype=dt, device=q.device)
                 qp, qh, qt, qs = _heads(q, n, self.head_dim, dt, "q")
-                op, oh, ot, os_ = _heads(q_out, n, self.head_dim, dt, "q_out")
-                if oh != qh:
-                    raise ValueError("q_out: as many heads as q are wanted")
+                q_out, op, ot, os_ = _output(q_out, q, qh, "q_out")
         elif q is not None:
             raise ValueError("q is only turned with rotary")
-        _check(fluxbin.kv_append_status(self._ref, _TYPES[dt], n, _int32(slots, n, "slots"), kp, kt, ks, vp, vt, vs, rp, pp, qp, qh, qt, qs,
-                                        op, ot, os_, _stream_ptr(stream)), "fluxbin_kv_append")
-        return q_out if q is not None else None
+        fluxbin.kv_append_call(self._ref, _TYPES[dt], n, _int32(slots, n, "slots"), kp, kt, ks, vp, vt, vs, rp, pp, qp, qh, qt, qs,
+                               op, ot, os_, _stream(k, stream))
+        return None if q is None else q_out
 
     def read(self, slots: torch.Tensor, dtype: torch.dtype = torch.float16, stream=None):
         """fluxbin_kv_read: the keys and values that the entries at `slots` stand for, two [tokens][kv_heads][head_dim] tensors."""
         if dtype not in _TYPES:
             raise TypeError("dtype: fp16, bf16 or fp32 is wanted")
         n = slots.shape[0]
-        k = torch.empty((n, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
-        v = torch.empty_like(k)
-        _check(fluxbin.kv_read_status(self._ref, _TYPES[dtype], n, _int32(slots, n, "slots"), k.data_ptr(), v.data_ptr(), _stream_ptr(stream)),
-               "fluxbin_kv_read")
+        both = torch.empty((2, n, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
+        k, v = both.unbind()
+        fluxbin.kv_read_call(self._ref, _TYPES[dtype], n, _int32(slots, n, "slots"), k.data_ptr(), v.data_ptr(), _stream(slots, stream))
         return k, v
 
     def workspace(self, batch: int, tokens: int, q_heads: int) -> Workspace:
@@ -206,18 +201,12 @@ class KVCache:
         if table.dtype is not torch.int32 or table.dim() != 2 or not table.is_cuda or (table.shape[1] > 1 and table.stride(1) != 1):
             raise ValueError("table: a CUDA int32 tensor [batch][max_blocks] with contiguous rows is wanted")
         B, width = table.shape
-        if out is None:
-            out = torch.empty(q.shape, dtype=dt, device=q.device)
-        op, oh, ot, os_ = _heads(out, n, self.head_dim, dt, "out")
-        if oh != qh:
-            raise ValueError("out: as many heads as q are wanted")
-        lse = torch.empty((n, qh), dtype=torch.float32, device=q.device) if with_lse else None
-        _check(fluxbin.kv_attend_status(self._ref, _TYPES[dt], B, n, qp, qh, qt, qs,
-                                        None if query_start is None else _int32(query_start, B + 1, "query_start"),
-                                        _int32(lengths, B, "lengths"), table.data_ptr(), max(table.stride(0), width), width,
-                                        1.0 / math.sqrt(self.head_dim) if scale is None else scale, op, ot, os_,
-                                        None if lse is None else lse.data_ptr(), ws.tensor.data_ptr(), ws.nbytes, _stream_ptr(stream)),
-               "fluxbin_kv_attend")
+        out, op, ot, os_ = _output(out, q, qh, "out")
+        lse = torch.empty((n, qh), dtype=torch.float32, device=self.device) if with_lse else None
+        fluxbin.kv_attend_call(self._ref, _TYPES[dt], B, n, qp, qh, qt, qs, 0 if query_start is None else _int32(query_start, B + 1, "query_start"),
+                               _int32(lengths, B, "lengths"), table.data_ptr(), max(table.stride(0), width), width,
+                               self._scale if scale is None else scale, op, ot, os_, 0 if lse is None else lse.data_ptr(), ws.tensor.data_ptr(),
+                               ws.nbytes, _stream(q, stream))
         return (out, lse) if with_lse else out
 
 
@@ -225,12 +214,13 @@ class BlockTables:
     """The blocks of a batch of requests and the free list they come from (fluxbin_kv_advance).
 
     `table` int32 [batch][max_blocks] and `free` int32 [capacity] are changed in place by advance(); the lengths and the
-    number of free blocks go in and come out, so a step's outputs are the next step's inputs."""
+    number of free blocks go in and come out."""
 
     def __init__(self, table: torch.Tensor, free: torch.Tensor, block_tokens: int):
         if table.dtype is not torch.int32 or table.dim() != 2 or not table.is_cuda or (table.shape[1] > 1 and table.stride(1) != 1):
             raise ValueError("table: a CUDA int32 tensor [batch][max_blocks] with contiguous rows is wanted")
         self.table, self.free, self.block_tokens = table, free, block_tokens
+        self._tokens = self._sets = None
         self._free = _int32(free, free.shape[0], "free")
         self.batch, self.max_blocks = table.shape
         self._args = (table.data_ptr(), max(table.stride(0), table.shape[1]), table.shape[1], self._free, free.shape[0])
@@ -243,13 +233,25 @@ class BlockTables:
 
     def advance(self, lengths: torch.Tensor, new_tokens: torch.Tensor, num_free: torch.Tensor, tokens: int, stream=None) -> SimpleNamespace:
         """One step: `new_tokens` int32 [batch] tokens to add (> 0) or drop (< 0), `tokens` the sum of those to add.  Returns
-        lengths, num_free, granted, query_start, positions, slots, requests (int32 tensors, all new)."""
+        lengths, num_free, granted, query_start, positions, slots, requests: int32 tensors that belong to this object, two
+        sets in turn, so that a step's outputs can be the next step's inputs; keep a copy of what has to live longer."""
         B = self.batch
-        buf = torch.empty(3 * B + 2 + 3 * tokens, dtype=torch.int32, device=self.table.device)
-        nfo, lo, gr, qs, po, sl, rq = buf.split((1, B, B, B + 1, tokens, tokens, tokens))
-        p = buf.data_ptr()
-        o = p + 4 * (3 * B + 2)
-        _check(fluxbin.kv_advance_status(B, tokens, self.block_tokens, _int32(lengths, B, "lengths"), _int32(new_tokens, B, "new_tokens"),
-                                         *self._args, _int32(num_free, 1, "num_free"), p, p + 4, p + 4 + 4 * B, p + 4 + 8 * B,
-                                         o, o + 4 * tokens, o + 8 * tokens, _stream_ptr(stream)), "fluxbin_kv_advance")
-        return SimpleNamespace(num_free=nfo, lengths=lo, granted=gr, query_start=qs, positions=po, slots=sl, requests=rq)
+        lp, np_, fp = _int32(lengths, B, "lengths"), _int32(new_tokens, B, "new_tokens"), _int32(num_free, 1, "num_free")
+        if tokens != self._tokens:                       # (a decode loop keeps one size)
+            self._tokens, self._sets = tokens, [self._outputs(tokens), self._outputs(tokens)]
+        step, other = self._sets
+        self._sets = [other, step]
+        if step.first <= lp < step.last or step.first <= np_ < step.last or step.first <= fp < step.last:
+            step = self._sets[1] = self._outputs(tokens)  # an input of this step is an output of the last but one: keep that
+        fluxbin.kv_advance_call(B, tokens, self.block_tokens, lp, np_, *self._args, fp, *step.pointers, _stream(self.table, stream))
+        return step
+
+    def _outputs(self, tokens: int) -> SimpleNamespace:
+        B = self.batch
+        sizes = (1, B, B, B + 1, tokens, tokens, tokens)
+        parts = torch.empty(sum(sizes), dtype=torch.int32, device=self.table.device).split(sizes)
+        step = SimpleNamespace(**dict(zip(("num_free", "lengths", "granted", "query_start", "positions", "slots", "requests"), parts)))
+        first = parts[0].data_ptr()
+        step.pointers = tuple(first + 4 * sum(sizes[:i]) for i in range(7))
+        step.first, step.last = first, first + 4 * sum(sizes)
+        return step

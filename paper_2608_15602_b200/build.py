@@ -9,7 +9,8 @@ CSRC = os.path.join(_PKG, "csrc")
 LIB_DIR = os.path.join(_PKG, "lib")
 LIB_PATH = os.environ.get("FLUXBIN_LIB") or os.path.join(LIB_DIR, "libfluxbin.so")
 SOURCES = ["fluxbin_api.cu", "fluxbin_pack.cpp", "fluxbin_pack_device.cu", "fluxbin_noalloc.cu", "fluxbin_rc_decomp.cu",
-           "fluxbin_rotary.cu", "fluxbin_kv_cache.cu", "fluxbin_kv_attend.cu", "fluxbin_kv_advance.cu"]
+           "fluxbin_rotary.cu", "fluxbin_kv_cache.cu", "fluxbin_kv_attend.cu", "fluxbin_kv_advance.cu",
+           "fluxbin_words.cpp"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC,-fopenmp", "-shared", "--threads", "0"]
 

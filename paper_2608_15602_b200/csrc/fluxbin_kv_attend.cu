@@ -6,9 +6,10 @@
 // with the tokens (then the elements of a head) as the 16-row side of the matrix instruction and the query rows as its
 // 8-column side: a decode step has as few rows as query heads share a key head, and 8 columns waste the least.
 //
-// What bounds it is the cache's bytes.  Every byte goes from memory straight into the register of the lane that holds it
-// as a matrix operand -- no shared memory, no shuffles: which element a lane's operand slot stands for is free as long as
-// both operands agree, so a lane takes 16 consecutive bytes wherever the instruction would want scattered pairs.
+// What bounds it is the cache's bytes.  Each lane copies (cp.async) the 16-byte pieces that it will hold as matrix operands
+// into its own places of a ring in shared memory, a few tiles ahead, and takes them from there itself: no barrier, no bank
+// conflict, no shuffle.  Which element a lane's operand slot stands for is free as long as both operands agree, so a lane
+// takes 16 consecutive bytes wherever the instruction would want scattered pairs.
 //   keys:    lane (r, q) = (lane / 4, lane % 4) reads elements 16 q .. + 15 of each 64-byte piece of tokens r and r + 8
 //   values:  the same lane reads elements 16 r .. + 15 (of 128) of tokens 2q, 2q + 1, 2q + 8, 2q + 9 and interleaves the
 //            bytes of two tokens, which the conversion to fp16 does on the way
@@ -19,8 +20,8 @@
 // letting the reference m lag: it is raised to (row maximum - 7) only when a P would pass 2^15, so that most steps need no
 // reduction over lanes and what is flushed to zero is below 2^-31 of the largest probability.
 //
-// Work is cut evenly whatever the lengths are: all (request, rows, head) jobs in units of 128 tokens form a line, CTA i of
-// n takes the i-th n-th of it (the lengths are read on the device: a captured graph serves every step).  A job cut between
+// Work is cut evenly whatever the lengths are: all (request, head, rows) jobs in units of cached tokens form a line, which is
+// cut into a range for each CTA (the lengths are read on the device: a captured graph serves every step).  A job cut between
 // CTAs leaves normalised partial results and their lse in the workspace; the CTA that arrives last joins them in order.
 #include "fluxbin_cache.cuh"
 
@@ -30,9 +31,26 @@ using namespace fbd;
 
 namespace {
 
-constexpr int kWarps = 8, kThreads = kWarps * 32;
-constexpr int kUnit = kWarps * 16;              // cached tokens of a unit: 16 for each warp
-constexpr int kMaxGrid = 320;                   // two CTAs on each SM
+// Warps of a CTA, CTAs on an SM, tiles of 16 tokens that a warp has under way.  Measured at head_dim 128 with 8 rows on 64
+// requests of up to 16384 tokens: 4 x 3 with 4 tiles 242 us, 8 x 2 with 3 249, 6 x 2 with 4 257, 4 x 4 with 3 (128
+// registers, spills) 277, 12 x 1 with 4 288: small CTAs, so that the others go on while one ends a job, and tiles on their
+// way rather than warps.
+template <int D, int NT> struct Shape;
+template <> struct Shape<64, 1> { static constexpr int warps = 8, ctas = 2, stages = 6; };
+template <> struct Shape<64, 2> { static constexpr int warps = 8, ctas = 2, stages = 6; };
+template <> struct Shape<128, 1> { static constexpr int warps = 4, ctas = 3, stages = 4; };
+template <> struct Shape<128, 2> { static constexpr int warps = 8, ctas = 1, stages = 6; };
+template <> struct Shape<256, 1> { static constexpr int warps = 8, ctas = 1, stages = 3; };
+
+// Units that it costs to begin a job (the chain from the block table to the first tile, the ring that runs dry, the warps'
+// results put together): CTAs that cross from job to job get fewer tokens.  Units are 64 tokens with 4 warps.  Measured 0 / 2 /
+// 4 / 6 / 9: 36.7 / 35.2 / 33.9 / 33.0 / 33.4 us on 16 requests, 64.8 / 58.0 / 56.8 / 56.8 / 59.1 on 8 with 40 key heads.
+constexpr int kJobCost = 6;
+
+// The part of a range that is drawn, and the units that it has to have: below that the further partial results cost more
+// than the evener end gives.  10 % of 156 units: 240 -> 226 us; of 37 units (one request of 131071 tokens): 74 -> 86 us.
+constexpr int kTailPercent = 10, kTailMin = 8;
+constexpr int kMaxGrid = 480, kMaxShares = kMaxGrid * 2;
 constexpr int kMaxRows = 16;
 
 struct Args {
@@ -46,9 +64,10 @@ struct Args {
     void *out;
     long long out_token, out_head;
     float *lse;
-    unsigned *arrived;                          // [kMaxGrid], by the CTA in which a cut job begins
-    float *partial;                             // [kMaxGrid][2][rows][D], then [kMaxGrid][2][rows] lse (base 2)
-    int min_share;                              // units a CTA has at least
+    unsigned *drawn;                            // shares drawn so far
+    unsigned *arrived;                          // [kMaxShares], by the share in which a cut job begins
+    float *partial_lse;                         // [kMaxShares][2][kMaxRows], base 2
+    float *partial;                             // [kMaxShares][2][rows][D]
 };
 
 // ---- conversions of four 8-bit entries to two pairs of fp16 ---------------------------------------------
@@ -91,15 +110,23 @@ __device__ __forceinline__ float exp2_fast(float x)         // relative error 2^
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// the cache is read once: past L1
+// Copies from the cache into a lane's own places of the ring, past L1 (the cache is read once).  A lane reads back only
+// what it copied itself, so its own wait is all the order that is needed.
+template <int N> __device__ __forceinline__ void copy_ahead(uint32_t to, const unsigned char *from)
+{
+    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
 template <int N> struct Words { uint32_t w[N]; };
-template <int N> __device__ __forceinline__ Words<N> load_stream(const unsigned char *p)
+template <int N> __device__ __forceinline__ Words<N> take(uint32_t from)
 {
     Words<N> v;
     if constexpr (N == 4)
-        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]) : "l"(p));
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]) : "r"(from) : "memory");
     else
-        asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.w[0]), "=r"(v.w[1]) : "l"(p));
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.w[0]), "=r"(v.w[1]) : "r"(from) : "memory");
     return v;
 }
 
@@ -110,7 +137,7 @@ struct Request {
     int length;                  // its cached tokens
     int row_tiles, pieces;       // tiles of query rows a head has, units of cached tokens
 };
-template <int ROWS> __device__ __forceinline__ Request request_of(const Args &a, int r)
+template <int ROWS, int kUnit> __device__ __forceinline__ Request request_of(const Args &a, int r)
 {
     Request q;
     if (a.query_start) {
@@ -125,26 +152,36 @@ template <int ROWS> __device__ __forceinline__ Request request_of(const Args &a,
     q.pieces = max((q.length + kUnit - 1) / kUnit, 1);          // an empty request still has rows to write
     return q;
 }
-__device__ __forceinline__ long long units_of(const Args &a, const Request &q) { return (long long)q.row_tiles * a.c.kv_heads * q.pieces; }
+__device__ __forceinline__ long long units_of(const Args &a, const Request &q) { return (long long)q.row_tiles * a.c.kv_heads * (q.pieces + kJobCost); }
 
-template <int D, int ROWS> struct Shared {
-    float o[kWarps][ROWS][D + 4];
-    float m[kWarps][ROWS], l[kWarps][ROWS], v[kWarps];
-    long long scan[kWarps], before;
-    int request, last;
+template <int D, int ROWS, int WARPS, int STAGES> struct Shared {
+    static constexpr int kTile = 32 * D;            // 16 tokens of keys and of values
+    union {
+        unsigned char ring[WARPS][STAGES][kTile];
+        struct {                                    // after a job: the warps' results
+            float o[WARPS][ROWS][D + 4];
+            float m[WARPS][ROWS], l[WARPS][ROWS], v[WARPS];
+        };
+        struct { float join_max[ROWS], join_inv[ROWS], join_lse[ROWS]; };       // after the last part of a cut job
+    };
+    long long scan[WARPS], before;
+    int request, last, share;
 };
 
 // one CTA: its part of the line, job after job
 template <int D, int FMT, int NT, typename T>
-__global__ void __launch_bounds__(kThreads, D == 256 || NT == 2 ? 1 : 2) attend_kernel(const __grid_constant__ Args a)
+__global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) attend_kernel(const __grid_constant__ Args a)
 {
     constexpr int ROWS = 8 * NT;
+    constexpr int kWarps = Shape<D, NT>::warps, kThreads = kWarps * 32;
+    constexpr int STAGES = Shape<D, NT>::stages;
+    constexpr int kUnit = kWarps * 16;           // cached tokens of a unit: 16 for each warp
     constexpr int KC = D / 64;                   // 64-byte pieces of a key
     constexpr int VW = D >= 128 ? 4 : 2;         // words of a load of values
     constexpr int VC = D / (VW * 32);            // pieces of a value row (eight lanes of VW words each)
     constexpr int MT = D / 16;                   // 16-element tiles of the output
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    Shared<D, ROWS> &sm = *reinterpret_cast<Shared<D, ROWS> *>(smem_raw);
+    Shared<D, ROWS, kWarps, STAGES> &sm = *reinterpret_cast<Shared<D, ROWS, kWarps, STAGES> *>(smem_raw);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, lr = lane >> 2, lq = lane & 3;
     const int H = a.c.kv_heads, G = a.q_heads / H, bs = a.c.block_tokens;
 
@@ -154,7 +191,7 @@ __global__ void __launch_bounds__(kThreads, D == 256 || NT == 2 ? 1 : 2) attend_
     // ---- where this CTA's part begins: a sum over the requests, each thread over a run of them
     const int per = (a.batch + kThreads - 1) / kThreads, r_lo = min(tid * per, a.batch), r_hi = min(r_lo + per, a.batch);
     long long mine = 0;
-    for (int r = r_lo; r < r_hi; ++r) mine += units_of(a, request_of<ROWS>(a, r));
+    for (int r = r_lo; r < r_hi; ++r) mine += units_of(a, request_of<ROWS, kUnit>(a, r));
     long long upto = mine;
     for (int o = 1; o < 32; o <<= 1) {
         const long long x = __shfl_up_sync(0xffffffffu, upto, o);
@@ -167,15 +204,30 @@ __global__ void __launch_bounds__(kThreads, D == 256 || NT == 2 ? 1 : 2) attend_
         if (w < warp) upto += sm.scan[w];
         total += sm.scan[w];
     }
-    const long long shares = min((long long)gridDim.x, (total + a.min_share - 1) / a.min_share);
-    if (blockIdx.x >= shares) return;
-    auto cut = [&](long long i) { return i * total / shares; };
-    long long u = cut(blockIdx.x);
-    const long long u_end = cut(blockIdx.x + 1);
+    const long long active = min((long long)gridDim.x, total);
+    if (blockIdx.x >= active) return;
+    // A range of the line for each CTA.  Of long ranges the last part is a share of its own, drawn by whoever is through
+    // with the first part of its own range, since SMs do not all get the same part of the memory's rate.  The cuts depend
+    // on the line alone, so results do not depend on who drew what.  Shares are numbered along the line.
+    const long long tail = total / active * kTailPercent / 100, extra = tail >= kTailMin ? active : 0;
+    const long long size = total / active, over = total - size * active;
+    auto cut = [&](long long i) {
+        if (extra == 0) return i * size + min(i, over);
+        const long long at = (i + 1) / 2 * size + min((i + 1) / 2, over);
+        return i & 1 ? at - tail : at;
+    };
+    auto owner = [&](long long x) {
+        const int i = (int)(x < over * (size + 1) ? x / (size + 1) : over + (x - over * (size + 1)) / size);
+        return extra == 0 ? i : 2 * i + (x >= cut(2 * i + 1));
+    };
+
+    for (long long share = extra ? 2 * blockIdx.x : blockIdx.x;;) {
+    long long u = cut(share);
+    const long long u_end = cut(share + 1);
     if (u >= upto - mine && u < upto) {
         long long before = upto - mine;
         for (int r = r_lo; r < r_hi; ++r) {
-            const long long n = units_of(a, request_of<ROWS>(a, r));
+            const long long n = units_of(a, request_of<ROWS, kUnit>(a, r));
             if (u < before + n) { sm.request = r; sm.before = before; break; }
             before += n;
         }
@@ -183,41 +235,74 @@ __global__ void __launch_bounds__(kThreads, D == 256 || NT == 2 ? 1 : 2) attend_
     __syncthreads();
     int r = sm.request;
     long long r_before = sm.before;
-    Request rq = request_of<ROWS>(a, r);
+    Request rq = request_of<ROWS, kUnit>(a, r);
 
     while (u < u_end) {
         while (u >= r_before + units_of(a, rq)) {
             r_before += units_of(a, rq);
-            rq = request_of<ROWS>(a, ++r);
+            rq = request_of<ROWS, kUnit>(a, ++r);
         }
-        const long long in_request = u - r_before;
-        const int job = (int)(in_request / rq.pieces), p0 = (int)(in_request % rq.pieces);
-        const int p1 = (int)min((long long)rq.pieces, p0 + (u_end - u));
+        // a job is kJobCost places for what it costs to begin it, then its pieces
+        const int span = rq.pieces + kJobCost, job = (int)((u - r_before) / span);
+        const long long job_begin = r_before + (long long)job * span;
+        const int p0 = max((int)(u - job_begin) - kJobCost, 0);
+        const int p1 = (int)min(u_end - job_begin, (long long)span) - kJobCost;
+        u = min(u_end, job_begin + span);
+        if (p1 <= p0) continue;
         const int h = job / rq.row_tiles, row0 = job % rq.row_tiles * ROWS;
         const int rows = (int)min((long long)ROWS, (long long)rq.count * G - row0);
         // tokens that the last and the first row of the tile see
         const int seen = rq.length - (rq.count - 1 - (row0 + rows - 1) / G);
         const int seen_first = rq.length - (rq.count - 1 - row0 / G);
-        int limit[NT][2];
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) limit[t][e] = rq.length - (rq.count - 1 - min(row0 + t * 8 + 2 * lq + e, row0 + rows - 1) / G);
+        auto limit = [&](int t, int e) { return rq.length - (rq.count - 1 - min(row0 + t * 8 + 2 * lq + e, row0 + rows - 1) / G); };
 
-        // ---- the block ids and scales of this warp's tiles: lane i holds those of tile i of a batch of 32
+        // ---- the places and scales of this warp's tiles: lane i holds those of tile i of a batch of 32
         const int tok0 = p0 * kUnit + warp * 16;
         const int tiles = max((min(seen, p1 * kUnit) - tok0 + kUnit - 1) / kUnit, 0);
         const int *row_table = a.table + r * a.table_stride;
-        auto id_of = [&](int tile) {
+        // (a tile of 16 tokens lies in one block): where they begin in the cache, -1 for a block that is none
+        struct Place { long long at; float ks, vs; };
+        auto block_of = [&](int tile) {
             if (tile >= tiles) return -1;
             const int id = row_table[(tok0 + tile * kUnit) / bs];
             return id >= 0 && id < a.c.num_blocks ? id : -1;
         };
-        int id_now = id_of(lane), id_next = -1;
-        float ks_now = 0.f, vs_now = 0.f, ks_next = 0.f, vs_next = 0.f;
-        if (id_now >= 0) {
-            ks_now = a.c.d_k_scale[(long long)id_now * H + h];
-            vs_now = a.c.d_v_scale[(long long)id_now * H + h];
+        auto place_of = [&](int id, int tile) {
+            Place x = {-1, 0.f, 0.f};
+            if (id >= 0) {
+                x.at = id * a.c.block_stride + (tok0 + tile * kUnit) % bs * a.c.token_stride;
+                x.ks = a.c.d_k_scale[(long long)id * H + h];
+                x.vs = a.c.d_v_scale[(long long)id * H + h];
+            }
+            return x;
+        };
+        Place now = place_of(block_of(lane), lane), next = {-1, 0.f, 0.f};
+        int id_next = tiles > 32 ? block_of(32 + lane) : -1;
+
+        // ---- the ring: where a lane's pieces of a tile lie, and their way there
+        const long long ts = a.c.token_stride;
+        const unsigned char *k_lane = (const unsigned char *)a.c.d_k + h * a.c.head_stride + lr * ts + lq * 16;
+        const unsigned char *v_lane = (const unsigned char *)a.c.d_v + h * a.c.head_stride + 2 * lq * ts + lr * (VW * 4);
+        const uint32_t k_ring = (uint32_t)__cvta_generic_to_shared(&sm.ring[warp][0][lane * 16]);
+        const uint32_t v_ring = (uint32_t)__cvta_generic_to_shared(&sm.ring[warp][0][16 * D + lane * (VW * 4)]);
+        // a block that is none reads the cache's first one instead (and is masked out)
+        auto fetch = [&](long long at, int stage) {
+            const unsigned char *kp = k_lane + max(at, 0ll), *vp = v_lane + max(at, 0ll);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int c = 0; c < KC; ++c) copy_ahead<16>(k_ring + stage * (32 * D) + (i * KC + c) * 512, kp + i * 8 * ts + c * 64);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int c = 0; c < VC; ++c)
+                    copy_ahead<VW * 4>(v_ring + stage * (32 * D) + (i * VC + c) * (VW * 128), vp + ((i & 1) + (i >> 1) * 8) * ts + c * (VW * 32));
+        };
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; ++i) {
+            const long long at = __shfl_sync(0xffffffffu, now.at, i);
+            if (i < tiles) fetch(at, i);
+            copies_commit();
         }
 
         // ---- the query rows as the 8-column operand: lane (r, q) holds row r, 16 elements of each 64-element piece
@@ -267,52 +352,43 @@ __global__ void __launch_bounds__(kThreads, D == 256 || NT == 2 ? 1 : 2) attend_
             for (int e = 0; e < 2; ++e) factor[t][e] = __shfl_sync(0xffffffffu, f, (2 * lq + e) * 4);
         }
 
-        float o[NT][MT][4], ref[NT][2], sum[NT][2], vref = 0.f, vref_inverse = 0.f;
+        float o[NT][MT][4], ref[NT][2], top[NT][2], sum[NT][2], vref = 0.f, vref_inverse = 0.f;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
             for (int i = 0; i < MT; ++i) o[t][i][0] = o[t][i][1] = o[t][i][2] = o[t][i][3] = 0.f;
-            ref[t][0] = ref[t][1] = -INFINITY;
+            ref[t][0] = ref[t][1] = 0.f;                 // the reference, and what a score may not pass against it
+            top[t][0] = top[t][1] = -INFINITY;
             sum[t][0] = sum[t][1] = 0.f;
         }
 
-        Words<4> kw[2][KC];
-        Words<VW> vw[4][VC];
-        auto load_k = [&](int id, int tok) {
-            const unsigned char *p = (const unsigned char *)a.c.d_k + id * a.c.block_stride + h * a.c.head_stride + (tok % bs + lr) * a.c.token_stride + lq * 16;
+        int stage = 0, stage_ahead = STAGES - 1;
+        for (int tile = 0; tile < tiles; ++tile) {
+            const int tok = tok0 + tile * kUnit, slot = tile & 31;
+            // ---- the place of this tile and of the one to fetch; a new batch of 32 is looked up well ahead
+            if (slot == 0 && tile > 0) {
+                now = next;
+                if (tile + 32 < tiles) id_next = block_of(tile + 32 + lane);
+            }
+            if (slot == 8 && tile + 24 < tiles) next = place_of(id_next, tile + 24 + lane);
+            const bool none = __shfl_sync(0xffffffffu, (int)(now.at >> 32), slot) < 0;
+            const float ks = __shfl_sync(0xffffffffu, now.ks, slot), vs = __shfl_sync(0xffffffffu, now.vs, slot);
+            const long long ahead = __shfl_sync(0xffffffffu, slot + STAGES - 1 < 32 ? now.at : next.at, (slot + STAGES - 1) & 31);
+            copies_wait<STAGES - 2>();
+            if (tile + STAGES - 1 < tiles) fetch(ahead, stage_ahead);
+            copies_commit();
+            Words<4> kw[2][KC];
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int c = 0; c < KC; ++c) {
-                    if (id >= 0) kw[i][c] = load_stream<4>(p + i * 8 * a.c.token_stride + c * 64);
-                    else kw[i][c] = Words<4>{{0, 0, 0, 0}};
-                }
-        };
-        auto load_v = [&](int id, int tok) {
-            const unsigned char *p = (const unsigned char *)a.c.d_v + id * a.c.block_stride + h * a.c.head_stride + (tok % bs + 2 * lq) * a.c.token_stride + lr * (VW * 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int c = 0; c < VC; ++c) {
-                    if (id >= 0) vw[i][c] = load_stream<VW>(p + ((i & 1) + (i >> 1) * 8) * a.c.token_stride + c * (VW * 32));
-                    else vw[i][c] = Words<VW>{};
-                }
-        };
-
-        int id = __shfl_sync(0xffffffffu, id_now, 0);
-        float ks = __shfl_sync(0xffffffffu, ks_now, 0), vs = __shfl_sync(0xffffffffu, vs_now, 0);
-        if (tiles > 0) {
-            load_k(id, tok0);
-            load_v(id, tok0);
-        }
-        if (tiles > 32) id_next = id_of(32 + lane);
-
-        for (int tile = 0; tile < tiles; ++tile) {
-            const int tok = tok0 + tile * kUnit;
+                for (int c = 0; c < KC; ++c) kw[i][c] = take<4>(k_ring + stage * (32 * D) + (i * KC + c) * 512);
             // ---- scores
-            float s[NT][4];
+            // (two chains of products, so that one is issued while the other's last is under way)
+            float s[NT][4], s2[NT][4];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[t][e] = s2[t][e] = 0.f;
 #pragma unroll
             for (int c = 0; c < KC; ++c)
 #pragma unroll
@@ -321,30 +397,26 @@ __global__ void __launch_bounds__(kThreads, D == 256 || NT == 2 ? 1 : 2) attend_
                     to_half4<FMT>(kw[0][c].w[w], a0, a2);
                     to_half4<FMT>(kw[1][c].w[w], a1, a3);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) mma(s[t], a0, a1, a2, a3, qf[t][c * 4 + w][0], qf[t][c * 4 + w][1]);
+                    for (int t = 0; t < NT; ++t) mma(w & 1 ? s2[t] : s[t], a0, a1, a2, a3, qf[t][c * 4 + w][0], qf[t][c * 4 + w][1]);
                 }
-            // ---- the next tile's block and scales, its keys on their way
-            const int nt = tile + 1, slot = nt & 31;
-            if (slot == 0) { id_now = id_next; ks_now = ks_next; vs_now = vs_next; if (nt + 32 < tiles) id_next = id_of(nt + 32 + lane); }
-            if (slot == 16 && id_next >= 0) {
-                ks_next = a.c.d_k_scale[(long long)id_next * H + h];
-                vs_next = a.c.d_v_scale[(long long)id_next * H + h];
-            }
-            const int id_then = __shfl_sync(0xffffffffu, id_now, slot);
-            const float ks_then = __shfl_sync(0xffffffffu, ks_now, slot), vs_then = __shfl_sync(0xffffffffu, vs_now, slot);
-            if (nt < tiles) load_k(id_then, tok + kUnit);
-
             // ---- softmax against a lagging reference
             bool above = false;
-            const bool edge = tok + 16 > seen_first || id < 0;
+            const bool edge = tok + 16 > seen_first || none;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[t][e] *= factor[t][e & 1] * ks;
-                    if (edge && (id < 0 || tok + lr + (e >> 1) * 8 >= limit[t][e & 1])) s[t][e] = -INFINITY;
-                    above |= s[t][e] > ref[t][e & 1] + 15.f;
-                }
+                for (int e = 0; e < 4; ++e) s[t][e] = (s[t][e] + s2[t][e]) * (factor[t][e & 1] * ks);
+            if (edge) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (none || tok + lr + (e >> 1) * 8 >= limit(t, e & 1)) s[t][e] = -INFINITY;
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) above |= s[t][e] > top[t][e & 1];
             if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
@@ -354,9 +426,10 @@ __global__ void __launch_bounds__(kThreads, D == 256 || NT == 2 ? 1 : 2) attend_
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16)) - 7.f;
-                        if (m > ref[t][e]) {
-                            const float f = exp2_fast(ref[t][e] - m);
+                        if (m > top[t][e] - 15.f) {
+                            const float f = top[t][e] == -INFINITY ? 0.f : exp2_fast(ref[t][e] - m);
                             ref[t][e] = m;
+                            top[t][e] = m + 15.f;
                             sum[t][e] *= f;
 #pragma unroll
                             for (int i = 0; i < MT; ++i) { o[t][i][e] *= f; o[t][i][e + 2] *= f; }
@@ -381,17 +454,22 @@ __global__ void __launch_bounds__(kThreads, D == 256 || NT == 2 ? 1 : 2) attend_
                 float p[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    p[e] = exp2_fast(s[t][e] - (ref[t][e & 1] == -INFINITY ? 0.f : ref[t][e & 1]));
+                    p[e] = exp2_fast(s[t][e] - ref[t][e & 1]);
                     sum[t][e & 1] += p[e];
                 }
                 pf[t][0] = transposed(pack_half2(p[0] * vf, p[1] * vf));
                 pf[t][1] = transposed(pack_half2(p[2] * vf, p[3] * vf));
             }
-            // ---- values: what lies past the request's length may be a NaN pattern
-            if (FMT == FLUXBIN_CACHE_E4M3 && tok + 16 > rq.length) {
+            Words<VW> vw[4][VC];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int c = 0; c < VC; ++c) vw[i][c] = take<VW>(v_ring + stage * (32 * D) + (i * VC + c) * (VW * 128));
+            // ---- values: what lies past the request's length, or in no block of its own, may be a NaN pattern
+            if (FMT == FLUXBIN_CACHE_E4M3 && (none || tok + 16 > rq.length)) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (tok + 2 * lq + (i & 1) + (i >> 1) * 8 >= rq.length)
+                    if (none || tok + 2 * lq + (i & 1) + (i >> 1) * 8 >= rq.length)
 #pragma unroll
                         for (int c = 0; c < VC; ++c) vw[i][c] = Words<VW>{};
             }
@@ -412,11 +490,11 @@ __global__ void __launch_bounds__(kThreads, D == 256 || NT == 2 ? 1 : 2) attend_
                         mma(o[t][(c * VW + w) * 2 + 1], f[0][2], f[0][3], f[1][2], f[1][3], pf[t][0], pf[t][1]);
                     }
                 }
-            if (nt < tiles) load_v(id_then, tok + kUnit);
-            id = id_then;
-            ks = ks_then;
-            vs = vs_then;
+            stage = stage + 1 == STAGES ? 0 : stage + 1;
+            stage_ahead = stage_ahead + 1 == STAGES ? 0 : stage_ahead + 1;
         }
+        copies_wait<0>();
+        __syncthreads();                          // the ring is done with: its place holds the results now
 
         // ---- the warps' results, then one for the CTA
 #pragma unroll
@@ -428,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, D == 256 || NT == 2 ? 1 : 2) attend_
                 l += __shfl_xor_sync(0xffffffffu, l, 8);
                 l += __shfl_xor_sync(0xffffffffu, l, 16);
                 const int row = t * 8 + 2 * lq + e;
-                if (lr == 0) { sm.m[warp][row] = ref[t][e]; sm.l[warp][row] = l; }
+                if (lr == 0) { sm.m[warp][row] = top[t][e] == -INFINITY ? -INFINITY : ref[t][e]; sm.l[warp][row] = l; }
 #pragma unroll
                 for (int c = 0; c < VC; ++c)
 #pragma unroll
@@ -440,8 +518,7 @@ __global__ void __launch_bounds__(kThreads, D == 256 || NT == 2 ? 1 : 2) attend_
         __syncthreads();
         const bool whole = p0 == 0 && p1 == rq.pieces;
         const int first_cta_slot = p0 == 0;                  // this job begins here, or goes on from the CTA before
-        float *part = a.partial + ((long long)blockIdx.x * 2 + first_cta_slot) * ROWS * D;
-        float *part_lse = a.partial + (long long)kMaxGrid * 2 * kMaxRows * D + ((long long)blockIdx.x * 2 + first_cta_slot) * kMaxRows;
+        float *part = a.partial + (share * 2 + first_cta_slot) * ROWS * D, *part_lse = a.partial_lse + (share * 2 + first_cta_slot) * kMaxRows;
         auto write_out = [&](int row, int d, float4 v, float lse2) {
             const int g = row0 + row;
             const long long tok = rq.first + g / G;
@@ -476,43 +553,64 @@ __global__ void __launch_bounds__(kThreads, D == 256 || NT == 2 ? 1 : 2) attend_
         }
         if (!whole) {
             // the CTAs that hold parts of this job, by the cut of the line
-            const long long job_begin = u - p0, job_end = job_begin + rq.pieces;
-            auto owner = [&](long long x) {
-                long long i = x * shares / total;
-                while (cut(i + 1) <= x) ++i;
-                while (cut(i) > x) --i;
-                return (int)i;
-            };
-            const int c0 = owner(job_begin), c1 = owner(job_end - 1);
+            const int c0 = owner(job_begin + kJobCost), c1 = owner(job_begin + span - 1);
             __threadfence();
             __syncthreads();
             if (tid == 0) sm.last = atomicAdd(&a.arrived[c0], 1u) == (unsigned)(c1 - c0);
             __syncthreads();
             if (sm.last) {
                 __threadfence();
-                const float *lses = a.partial + (long long)kMaxGrid * 2 * kMaxRows * D;
-                auto slot_of = [&](int c) { return (long long)c * 2 + (c == c0); };
-                for (int i = tid; i < ROWS * (D / 4); i += kThreads) {
-                    const int row = i / (D / 4), d = i % (D / 4) * 4;
-                    if (row >= rows) continue;
+                const int parts = c1 - c0 + 1;
+                auto slot_of = [&](int c) { return (long long)(c0 + c) * 2 + (c == 0); };
+                for (int row = warp; row < rows; row += kWarps) {
                     float m = -INFINITY, l = 0.f;
-                    for (int c = c0; c <= c1; ++c) m = fmaxf(m, __ldcg(lses + slot_of(c) * kMaxRows + row));
-                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-                    for (int c = c0; c <= c1; ++c) {
-                        const float x = __ldcg(lses + slot_of(c) * kMaxRows + row), f = x == -INFINITY ? 0.f : exp2_fast(x - m);
-                        const float4 y = __ldcg(reinterpret_cast<const float4 *>(a.partial + slot_of(c) * ROWS * D + row * D + d));
-                        l += f;
-                        v.x += f * y.x; v.y += f * y.y; v.z += f * y.z; v.w += f * y.w;
+                    for (int c = lane; c < parts; c += 32) {
+                        const float x = __ldcg(a.partial_lse + slot_of(c) * kMaxRows + row), m_now = fmaxf(m, x);
+                        l = l * (m == -INFINITY ? 0.f : exp2_fast(m - m_now)) + (x == -INFINITY ? 0.f : exp2_fast(x - m_now));
+                        m = m_now;
                     }
-                    const float inv = l == 0.f ? 0.f : 1.f / l;
-                    write_out(row, d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv), l == 0.f ? -INFINITY : m + log2f(l));
+                    float top = m;
+                    for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+                    l *= m == -INFINITY ? (l == l ? 0.f : 1.f) : exp2_fast(m - top);
+                    for (int x = 16; x; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+                    if (lane == 0) {
+                        sm.join_max[row] = top == -INFINITY ? 0.f : top;
+                        sm.join_inv[row] = l == 0.f ? 0.f : 1.f / l;
+                        sm.join_lse[row] = l == 0.f ? -INFINITY : top + log2f(l);
+                    }
+                }
+                __syncthreads();
+                constexpr int kItems = ROWS * (D / 4), kEach = (kItems + kThreads - 1) / kThreads;
+                float4 v[kEach];
+#pragma unroll
+                for (int k = 0; k < kEach; ++k) v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll(16 / kEach > 1 ? 16 / kEach : 1)
+                for (int c = 0; c < parts; ++c)
+#pragma unroll
+                    for (int k = 0; k < kEach; ++k) {
+                        const int i = min(tid + k * kThreads, kItems - 1), row = i / (D / 4);
+                        const float f = exp2_fast(__ldcg(a.partial_lse + slot_of(c) * kMaxRows + row) - sm.join_max[row]);
+                        const float4 y = __ldcg(reinterpret_cast<const float4 *>(a.partial + slot_of(c) * (ROWS * D)) + i);
+                        v[k].x += f * y.x; v[k].y += f * y.y; v[k].z += f * y.z; v[k].w += f * y.w;
+                    }
+#pragma unroll
+                for (int k = 0; k < kEach; ++k) {
+                    const int i = tid + k * kThreads, row = i / (D / 4);
+                    if (i >= kItems || row >= rows) continue;
+                    const float inv = sm.join_inv[row];
+                    write_out(row, i % (D / 4) * 4, make_float4(v[k].x * inv, v[k].y * inv, v[k].z * inv, v[k].w * inv), sm.join_lse[row]);
                 }
                 if (tid == 0) a.arrived[c0] = 0;
             }
         }
         __syncthreads();                          // the shared arrays are free again
-        u += p1 - p0;
+    }
+    if (extra == 0) return;
+    // every CTA draws until one draw is past the end: after as many draws as there are, the counter is 0 again
+    if (tid == 0) sm.share = (int)atomicInc(a.drawn, (unsigned)(extra + active - 1));
+    __syncthreads();
+    if (sm.share >= extra) return;
+    share = 2 * sm.share + 1;
     }
 }
 
@@ -532,7 +630,7 @@ int num_sms()
 template <int D, int FMT, int NT, typename T>
 cudaError_t run(const Args &a, cudaStream_t s)
 {
-    const size_t smem = sizeof(Shared<D, 8 * NT>);
+    const size_t smem = sizeof(Shared<D, 8 * NT, Shape<D, NT>::warps, Shape<D, NT>::stages>);
     static std::atomic<bool> opted[fb::kMaxDevices];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -545,8 +643,8 @@ cudaError_t run(const Args &a, cudaStream_t s)
     }
     const int sms = num_sms();
     if (sms == 0) return cudaErrorInvalidDevice;
-    const int grid = sms * (D == 256 || NT == 2 ? 1 : 2);
-    return launch(attend_kernel<D, FMT, NT, T>, dim3((unsigned)(grid < kMaxGrid ? grid : kMaxGrid)), kThreads, smem, s, a);
+    const int grid = sms * Shape<D, NT>::ctas;
+    return launch(attend_kernel<D, FMT, NT, T>, dim3((unsigned)(grid < kMaxGrid ? grid : kMaxGrid)), Shape<D, NT>::warps * 32, smem, s, a);
 }
 template <int D, int FMT, typename T> cudaError_t run_rows(const Args &a, cudaStream_t s)
 {
@@ -566,14 +664,14 @@ template <typename T> cudaError_t run_dim(const Args &a, cudaStream_t s)
     return a.c.head_dim == 64 ? run_format<64, T>(a, s) : a.c.head_dim == 128 ? run_format<128, T>(a, s) : run_format<256, T>(a, s);
 }
 
-constexpr size_t kCounterBytes = (kMaxGrid * sizeof(unsigned) + 255) / 256 * 256;
+constexpr size_t kCounterBytes = ((1 + kMaxShares) * sizeof(unsigned) + 255) / 256 * 256, kLseBytes = (size_t)kMaxShares * 2 * kMaxRows * sizeof(float);
 
 } // namespace
 
 extern "C" size_t fluxbin_kv_attend_workspace_size(int32_t batch, int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim)
 {
     if (batch < 1 || tokens < 0 || q_heads < 1 || kv_heads < 1 || q_heads % kv_heads != 0 || head_dim < 1) return 0;
-    return kCounterBytes + (size_t)kMaxGrid * 2 * kMaxRows * (head_dim + 1) * sizeof(float);
+    return kCounterBytes + kLseBytes * (1 + (size_t)head_dim);
 }
 
 extern "C" fluxbin_status_t fluxbin_kv_attend(const fluxbin_kv_cache_t *cache, int32_t dtype, int32_t batch, int32_t tokens,
@@ -596,7 +694,8 @@ extern "C" fluxbin_status_t fluxbin_kv_attend(const fluxbin_kv_cache_t *cache, i
     if (ws_bytes < fluxbin_kv_attend_workspace_size(batch, tokens, q_heads, cache->kv_heads, cache->head_dim)) return FLUXBIN_ERR_BUFFER_TOO_SMALL;
     const Args a = {*cache, batch, tokens, q_heads, block_table_width, d_q, q_token, q_head, d_query_start, d_lengths, d_block_table,
                     block_table_stride, scale, d_out, out_token, out_head, d_lse,
-                    (unsigned *)d_workspace, (float *)((char *)d_workspace + kCounterBytes), 1};
+                    (unsigned *)d_workspace, (unsigned *)d_workspace + 1, (float *)((char *)d_workspace + kCounterBytes),
+                    (float *)((char *)d_workspace + kCounterBytes + kLseBytes)};
     cudaStream_t s = (cudaStream_t)cuda_stream;
     FBD_CUDA(dtype == FLUXBIN_TYPE_FP16 ? run_dim<__half>(a, s) : run_dim<__nv_bfloat16>(a, s));
     return FLUXBIN_OK;

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -44,7 +45,7 @@ EXPORTS = ["fluxbin_packed_size", "fluxbin_validate", "fluxbin_pack_host", "flux
            "fluxbin_rc_decomp", "fluxbin_rc_decomp_workspace_size", "fluxbin_rc_decomp_passes",
            "fluxbin_rc_salient_collect", "fluxbin_pack_device", "fluxbin_pack_device_workspace_size", "fluxbin_rc_salient_residual",
            "fluxbin_rotary_frequencies", "fluxbin_rotary", "fluxbin_kv_validate", "fluxbin_kv_append", "fluxbin_kv_read",
-           "fluxbin_kv_attend_workspace_size", "fluxbin_kv_attend", "fluxbin_kv_advance"]
+           "fluxbin_kv_attend_workspace_size", "fluxbin_kv_attend", "fluxbin_kv_advance", "fluxbin_call_words"]
 
 TYPE_FP16, TYPE_FP32, TYPE_BF16 = 0, 1, 2
 CACHE_INT8, CACHE_E4M3 = 0, 1
@@ -63,6 +64,7 @@ class CacheDesc(ctypes.Structure):
                 ("head_dim", ctypes.c_int32), ("format", ctypes.c_int32), ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p),
                 ("block_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
                 ("d_k_scale", ctypes.c_void_p), ("d_v_scale", ctypes.c_void_p)]
+
 
 _LIB = None
 
@@ -147,6 +149,7 @@ def _lib():
         lib.fluxbin_kv_attend.argtypes = [vp, i32, i32, i32] + heads + [vp, vp, vp, i64, i32, f32, vp, i64, i64, vp, vp, sz, vp]
         lib.fluxbin_kv_advance.restype = ctypes.c_int
         lib.fluxbin_kv_advance.argtypes = [i32, i32, i32, vp, vp, vp, i64, i32, vp, i32] + [vp] * 8 + [vp]
+        lib.fluxbin_call_words.restype, lib.fluxbin_call_words.argtypes = ctypes.c_int, [i32, ctypes.c_char_p]
         _LIB = lib
     return _LIB
 
@@ -508,3 +511,23 @@ def kv_attend_workspace_size(batch: int, tokens: int, q_heads: int, kv_heads: in
 
 def kv_advance_status(*args) -> int:
     return _lib().fluxbin_kv_advance(*args)
+
+
+class Words:
+    """One of the calls above through fluxbin_call_words: called with the C call's arguments (None is not an integer: 0)."""
+
+    def __init__(self, which: int, layout: str, where: str):
+        self.which, self.pack, self.where = which, struct.Struct(layout).pack, where
+
+    def __call__(self, *args):
+        status = _lib().fluxbin_call_words(self.which, self.pack(*args))
+        if status:
+            raise FluxBinError(status, self.where)
+
+
+# (pointers as unsigned words, everything else signed; the scale of an attention as a double)
+rotary_call = Words(0, "=Q3qQQ3qQ2qQ3qQ2qQ", "fluxbin_rotary")
+kv_append_call = Words(1, "=Q2qQQ2qQ2qQQQ3qQ2qQ", "fluxbin_kv_append")
+kv_read_call = Words(2, "=Q2qQQQQ", "fluxbin_kv_read")
+kv_attend_call = Words(3, "=Q3qQ3qQQQ2qdQ2qQQQQ", "fluxbin_kv_attend")
+kv_advance_call = Words(4, "=3qQQQ2qQq9Q", "fluxbin_kv_advance")
