@@ -551,7 +551,8 @@ fluxbin_status_t fluxbin_kv_validate(const fluxbin_kv_cache_t *cache);
  * rotary (may be NULL): the keys are turned to d_positions in fp32 before they are quantised, and the q heads of the
  * same tokens (d_q may be NULL) are turned into d_q_out (may be d_q with the same strides).  Without rotary the d_q and
  * d_positions arguments are not looked at.  dtype is that of k, v and q.
- * Errors: as fluxbin_kv_validate; NULL, RANGE, UNSUPPORTED (dtype; a rotary for another head_dim), ALIGNMENT, CUDA.
+ * Errors: as fluxbin_kv_validate; NULL, RANGE (tokens up to 2^24), UNSUPPORTED (dtype; a rotary for another head_dim),
+ * ALIGNMENT, CUDA.
  */
 fluxbin_status_t fluxbin_kv_append(const fluxbin_kv_cache_t *cache, int32_t dtype, int32_t tokens, const int32_t *d_slots,
                                    const void *d_k, int64_t k_token, int64_t k_head, const void *d_v, int64_t v_token, int64_t v_head,

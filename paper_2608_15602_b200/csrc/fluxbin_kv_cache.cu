@@ -12,6 +12,7 @@ struct Heads { const void *p; long long token, head; int heads; };
 struct HeadsOut { void *p; long long token, head; };
 
 constexpr int kThreads = 128;
+constexpr int kMaxTokens = 1 << 24;              // of a call: the grids stay within 31 bits
 
 __device__ __forceinline__ float block_max(float v, float *scratch)
 {
@@ -36,9 +37,10 @@ __device__ __forceinline__ float turned(const T *x, int e, const fluxbin_rotary_
     return second ? v : u;
 }
 
-// One CTA per (token, head).  The first token of a run -- new tokens at consecutive slots of one block -- does the run.
+// Any strides, alignment and rotary dimension: one CTA per (token, head), element by element.  The first token of a run --
+// new tokens at consecutive slots of one block -- does the run.
 template <typename T, int FMT, bool ROT>
-__global__ void append_kernel(fluxbin_kv_cache_t c, int tokens, const int *slots, Heads k, Heads v, fluxbin_rotary_t rot,
+__global__ void append_any_kernel(fluxbin_kv_cache_t c, int tokens, const int *slots, Heads k, Heads v, fluxbin_rotary_t rot,
                               const int *positions, Heads q, HeadsOut qo)
 {
     __shared__ float scratch[4];
@@ -101,39 +103,420 @@ __global__ void append_kernel(fluxbin_kv_cache_t c, int tokens, const int *slots
     }
 }
 
-template <typename T, int FMT>
-__global__ void read_kernel(fluxbin_kv_cache_t c, const int *slots, T *k_out, T *v_out)
+// ---- 16-byte accesses ------------------------------------------------------------------------------------
+//
+// A run of new tokens in a block and a head share one scale, so their largest magnitude has to be known before the first
+// is stored; both halves of the work read the values once, into registers.
+//   short runs (a decode step: one token a run): a warp per head, half its lanes the keys, half the values;
+//   long runs (a prompt: whole blocks): the CTA on one head at a time, four pieces of eight elements a thread and pass.
+// Keys are turned in fp32 on the way; the angles of a run's tokens are formed once for all heads of the CTA.  The q heads of
+// the same tokens are turned by CTAs of the same launch.
+
+constexpr int kWide = 256, kWarpsWide = kWide / 32;
+constexpr int kShortRun = 4;
+
+template <typename T> struct Eight {
+    uint4 w[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T *p)
+    {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = reinterpret_cast<const uint4 *>(p)[i];
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const
+    {
+        T e[8];
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(e)[i] = w[i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = to_float(e[i]);
+    }
+};
+
+// elements e0 .. e0 + 7 of a head after its turn; `angles` are those of its token
+template <typename T>
+__device__ __forceinline__ void turned8(const T *x, int e0, const fluxbin_rotary_t &rot, const float2 *angles, float (&v)[8])
 {
+    Eight<T> own;
+    own.load(x + e0);
+    own.get(v);
+    if (e0 >= rot.rotary_dim) return;
+    if (rot.interleaved) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 a = angles[e0 / 2 + i];
+            float f, g;
+            turn_pair(v[2 * i], v[2 * i + 1], a.x, a.y, f, g);
+            v[2 * i] = f;
+            v[2 * i + 1] = g;
+        }
+        return;
+    }
+    const int half = rot.rotary_dim / 2;
+    const bool second = e0 >= half;
+    float w[8];
+    Eight<T> other;
+    other.load(x + (second ? e0 - half : e0 + half));
+    other.get(w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float2 a = angles[(second ? e0 - half : e0) + i];
+        float f, g;
+        turn_pair(second ? w[i] : v[i], second ? v[i] : w[i], a.x, a.y, f, g);
+        v[i] = second ? g : f;
+    }
+}
+
+// |v| of eight elements; a NaN or infinity among them counts as infinity
+__device__ __forceinline__ float largest8(const float (&v)[8])
+{
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fabsf(v[i]) < INFINITY ? fmaxf(m, fabsf(v[i])) : INFINITY;
+    return m;
+}
+template <int FMT> __device__ __forceinline__ uint2 entries8(const float (&v)[8], float inverse)
+{
+    unsigned char e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = Entry<FMT>::store(__fmul_rn(v[i], inverse));
+    uint2 w;
+    w.x = e[0] | e[1] << 8 | e[2] << 16 | (unsigned)e[3] << 24;
+    w.y = e[4] | e[5] << 8 | e[6] << 16 | (unsigned)e[7] << 24;
+    return w;
+}
+template <int FMT> __device__ __forceinline__ void requantise8(unsigned char *p, float ratio)
+{
+    const uint2 w = *reinterpret_cast<const uint2 *>(p);
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = Entry<FMT>::load((unsigned char)((i < 4 ? w.x : w.y) >> (i % 4 * 8)));
+    *reinterpret_cast<uint2 *>(p) = entries8<FMT>(v, ratio);
+}
+
+struct Run { int first, count, block, offset; };
+
+struct AppendArgs {
+    fluxbin_kv_cache_t c;
+    int tokens;
+    const int *slots;
+    Heads k, v;
+    fluxbin_rotary_t rot;
+    const int *positions;
+    Side q;
+    int tokens_each, heads_each, groups;         // tokens a CTA looks for runs in, heads it does, groups of heads
+    int append_ctas, q_heads_each, q_groups;
+};
+
+template <typename T, int FMT, int D, bool ROT>
+__global__ void __launch_bounds__(kWide) append_kernel(const __grid_constant__ AppendArgs a)
+{
+    constexpr int PIECES = D / 8;                // of eight elements
+    constexpr int AT_ONCE = kWide / PIECES;      // tokens a pass has side by side
+    constexpr int DEEP = 4, PASS = AT_ONCE * DEEP;
+    extern __shared__ float2 angles[];           // [PASS][pairs], or [kMaxPairs] for the q heads
+    __shared__ float part[2][kWarpsWide];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    let_successor_start();
     wait_for_predecessor();
-    const int t = blockIdx.x, s = slots[t], n = c.kv_heads * c.head_dim;
+
+    if (ROT && (int)blockIdx.x >= a.append_ctas) {
+        const int i = blockIdx.x - a.append_ctas, t = i / a.q_groups, h0 = i % a.q_groups * a.q_heads_each;
+        token_angles(a.rot, a.positions[t], 1.f, angles, tid, kWide);
+        __syncthreads();
+        const Side none = {};
+        const int h1 = min(h0 + a.q_heads_each, a.q.heads);
+        if (a.rot.interleaved) turn_heads<T, 16 / sizeof(T), true>(a.rot, angles, a.q, none, t, h0, h1, tid, kWide);
+        else turn_heads<T, 16 / sizeof(T), false>(a.rot, angles, a.q, none, t, h0, h1, tid, kWide);
+        return;
+    }
+
+    const int bs = a.c.block_tokens, limit = a.c.num_blocks * bs, H = a.c.kv_heads;
+    const int h0 = blockIdx.x % a.groups * a.heads_each, h1 = min(h0 + a.heads_each, H);
+    const int t_begin = blockIdx.x / a.groups * a.tokens_each, t_end = min(t_begin + a.tokens_each, a.tokens);
+    const int pairs = ROT ? a.rot.rotary_dim / 2 : 0;
+    const float top_inverse = 1.f / Entry<FMT>::kTop;
+
+    // ---- the runs that begin in this CTA's tokens: lane i looks at token i
+    unsigned short_runs, long_runs;
+    int my_count = 0, my_slot = -1;
+    {
+        const int t = t_begin + lane;
+        if (t < t_end) {
+            const int s = a.slots[t];
+            const bool first = s >= 0 && s < limit && !(s % bs > 0 && t > 0 && a.slots[t - 1] == s - 1);
+            if (first) {
+                const int most = min(bs - s % bs, a.tokens - t);
+                my_slot = s;
+                my_count = 1;
+                while (my_count < most && my_count <= kShortRun && a.slots[t + my_count] == s + my_count) ++my_count;
+            }
+        }
+        short_runs = __ballot_sync(0xffffffffu, my_count > 0 && my_count <= kShortRun);
+        long_runs = __ballot_sync(0xffffffffu, my_count > kShortRun);
+    }
+    if ((short_runs | long_runs) == 0) return;
+
+    if (short_runs) {
+        // ---- a warp per run and head: lanes of the lower half the keys, of the upper half the values
+        if constexpr (ROT) {
+            // (the angles of every token up to the last one of the last short run)
+            const int n = min(t_end - t_begin + kShortRun - 1, a.tokens - t_begin);
+            for (int i = tid; i < n * pairs; i += kWide) {
+                float2 x;
+                pair_angle(a.positions[t_begin + i / pairs], a.rot.d_turns[i % pairs], a.rot.magnitude, 1.f, x.x, x.y);
+                angles[i] = x;
+            }
+            __syncthreads();
+        }
+        constexpr int LANES = PIECES < 16 ? PIECES : 16;                             // lanes of a side
+        constexpr int EACH = PIECES / LANES;                                         // pieces of a lane
+        const int side = lane >> 4, sl = lane & 15, tasks = __popc(short_runs) * (h1 - h0);
+        for (int task = warp; task < tasks; task += kWarpsWide) {
+            const int h = h0 + task % (h1 - h0), at_lane = __fns(short_runs, 0, task / (h1 - h0) + 1);
+            const int t0 = t_begin + at_lane, count = __shfl_sync(0xffffffffu, my_count, at_lane), s0 = __shfl_sync(0xffffffffu, my_slot, at_lane);
+            const int block = s0 / bs, offset = s0 % bs;
+            const Heads &src = side ? a.v : a.k;
+            float *scale = (side ? a.c.d_v_scale : a.c.d_k_scale) + (long long)block * H + h;
+            const float before = offset ? *scale : 0.f;
+            float v[kShortRun][EACH][8], most = 0.f;
+#pragma unroll
+            for (int i = 0; i < kShortRun; ++i)
+#pragma unroll
+                for (int j = 0; j < EACH; ++j) {
+                    if (i >= count || sl >= LANES) continue;
+                    const T *x = (const T *)src.p + (long long)(t0 + i) * src.token + h * src.head;
+                    const int e0 = (j * LANES + sl) * 8;
+                    if (ROT && side == 0) turned8<T>(x, e0, a.rot, angles + (at_lane + i) * pairs, v[i][j]);
+                    else {
+                        Eight<T> w;
+                        w.load(x + e0);
+                        w.get(v[i][j]);
+                    }
+                    most = fmaxf(most, largest8(v[i][j]));
+                }
+#pragma unroll
+            for (int o = 8; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));      // of this half
+            const Scale s = scale_of(before, most, top_inverse);
+            unsigned char *cells = (unsigned char *)(side ? a.c.d_v : a.c.d_k) + block * a.c.block_stride + h * a.c.head_stride;
+            if (offset && !(s.now == before) && sl < LANES) {
+                const float ratio = __fmul_rn(before, s.inverse);
+                for (int i = 0; i < offset; ++i)
+#pragma unroll
+                    for (int j = 0; j < EACH; ++j) requantise8<FMT>(cells + i * a.c.token_stride + (j * LANES + sl) * 8, ratio);
+            }
+#pragma unroll
+            for (int i = 0; i < kShortRun; ++i)
+#pragma unroll
+                for (int j = 0; j < EACH; ++j)
+                    if (i < count && sl < LANES)
+                        *reinterpret_cast<uint2 *>(cells + (offset + i) * a.c.token_stride + (j * LANES + sl) * 8) = entries8<FMT>(v[i][j], s.inverse);
+            __syncwarp();
+            if (sl == 0) *scale = s.now;
+        }
+        if (ROT) __syncthreads();                                                    // the angles are free again
+    }
+
+    for (; long_runs; long_runs &= long_runs - 1) {
+        const int at_lane = __ffs(long_runs) - 1, t0 = t_begin + at_lane, s0 = __shfl_sync(0xffffffffu, my_slot, at_lane);
+        Run r = {t0, kShortRun + 1, s0 / bs, s0 % bs};
+        // its length: all lanes look at once, 32 tokens at a time
+        for (int most = min(bs - r.offset, a.tokens - t0); r.count < most;) {
+            const int i = r.count + lane;
+            const unsigned on = __ballot_sync(0xffffffffu, i < most && a.slots[min(t0 + i, a.tokens - 1)] == s0 + i);
+            const int n = on == 0xffffffffu ? 32 : __ffs(~on) - 1;
+            r.count += n;
+            if (n < 32) break;
+        }
+
+        // ---- the CTA on one head at a time
+        const int e0 = tid % PIECES * 8, sub = tid / PIECES;
+        const bool one_pass = r.count <= PASS;
+        auto pass_angles = [&](int base) {
+            if constexpr (ROT) {
+                const int n = min(PASS, r.count - base) * pairs;
+                __syncthreads();
+                for (int i = tid; i < n; i += kWide) {
+                    float2 x;
+                    pair_angle(a.positions[t0 + base + i / pairs], a.rot.d_turns[i % pairs], a.rot.magnitude, 1.f, x.x, x.y);
+                    angles[i] = x;
+                }
+                __syncthreads();
+            }
+        };
+        if (one_pass) pass_angles(0);
+        for (int h = h0; h < h1; ++h) {
+            float kv[DEEP][8], most[2] = {0.f, 0.f};
+            Eight<T> vv[DEEP];
+            auto load = [&](int base) {
+#pragma unroll
+                for (int j = 0; j < DEEP; ++j) {
+                    const int i = base + sub + j * AT_ONCE;
+                    if (i < r.count) vv[j].load((const T *)a.v.p + (long long)(t0 + i) * a.v.token + h * a.v.head + e0);
+                }
+#pragma unroll
+                for (int j = 0; j < DEEP; ++j) {
+                    const int i = base + sub + j * AT_ONCE;
+                    if (i >= r.count) continue;
+                    const T *x = (const T *)a.k.p + (long long)(t0 + i) * a.k.token + h * a.k.head;
+                    if (ROT) turned8<T>(x, e0, a.rot, angles + (i - base) * pairs, kv[j]);
+                    else {
+                        Eight<T> w;
+                        w.load(x + e0);
+                        w.get(kv[j]);
+                    }
+                }
+            };
+            for (int base = 0; base < r.count; base += PASS) {
+                if (!one_pass) pass_angles(base);
+                load(base);
+#pragma unroll
+                for (int j = 0; j < DEEP; ++j) {
+                    if (base + sub + j * AT_ONCE >= r.count) continue;
+                    float w[8];
+                    vv[j].get(w);
+                    most[0] = fmaxf(most[0], largest8(kv[j]));
+                    most[1] = fmaxf(most[1], largest8(w));
+                }
+            }
+#pragma unroll
+            for (int o = 16; o; o >>= 1)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) most[x] = fmaxf(most[x], __shfl_xor_sync(0xffffffffu, most[x], o));
+            __syncthreads();                                                         // `part` of the head before has been read
+            if (lane == 0) { part[0][warp] = most[0]; part[1][warp] = most[1]; }
+            __syncthreads();
+            Scale sc[2];
+            unsigned char *cells[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                float m = 0.f;
+#pragma unroll
+                for (int w = 0; w < kWarpsWide; ++w) m = fmaxf(m, part[x][w]);
+                float *scale = (x ? a.c.d_v_scale : a.c.d_k_scale) + (long long)r.block * H + h;
+                const float before = r.offset ? *scale : 0.f;
+                sc[x] = scale_of(before, m, top_inverse);
+                cells[x] = (unsigned char *)(x ? a.c.d_v : a.c.d_k) + r.block * a.c.block_stride + h * a.c.head_stride;
+                if (r.offset && !(sc[x].now == before)) {
+                    const float ratio = __fmul_rn(before, sc[x].inverse);
+                    for (int i = sub; i < r.offset; i += AT_ONCE) requantise8<FMT>(cells[x] + i * a.c.token_stride + e0, ratio);
+                }
+            }
+            for (int base = 0; base < r.count; base += PASS) {
+                if (!one_pass) {
+                    pass_angles(base);
+                    load(base);
+                }
+#pragma unroll
+                for (int j = 0; j < DEEP; ++j) {
+                    const int i = base + sub + j * AT_ONCE;
+                    if (i >= r.count) continue;
+                    const long long at = (r.offset + i) * a.c.token_stride + e0;
+                    float w[8];
+                    vv[j].get(w);
+                    *reinterpret_cast<uint2 *>(cells[0] + at) = entries8<FMT>(kv[j], sc[0].inverse);
+                    *reinterpret_cast<uint2 *>(cells[1] + at) = entries8<FMT>(w, sc[1].inverse);
+                }
+            }
+            __syncthreads();                                                         // every thread has read the old scales
+            if (tid < 2) (tid ? a.c.d_v_scale : a.c.d_k_scale)[(long long)r.block * H + h] = tid ? sc[1].now : sc[0].now;
+        }
+    }
+}
+
+// Eight entries a thread and side; the entries of a token and head are PIECES neighbouring threads.
+template <typename T, int FMT>
+__global__ void __launch_bounds__(kWide) read_kernel(fluxbin_kv_cache_t c, int tokens, const int *slots, T *k_out, T *v_out)
+{
+    let_successor_start();
+    wait_for_predecessor();
+    const int pieces = c.head_dim / 8, each = c.kv_heads * pieces;
+    const long long n = (long long)tokens * each, i = (long long)blockIdx.x * kWide + threadIdx.x;
+    if (i >= n) return;
+    const int t = (int)(i / each), h = (int)(i % each) / pieces, e0 = (int)(i % pieces) * 8;
+    const int s = slots[t];
     const bool live = s >= 0 && s < c.num_blocks * c.block_tokens;
     const int b = live ? s / c.block_tokens : 0, off = live ? s % c.block_tokens : 0;
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        const int h = i / c.head_dim, e = i % c.head_dim;
-        const long long at = b * c.block_stride + h * c.head_stride + off * c.token_stride + e;
-        const long long sc = (long long)b * c.kv_heads + h;
-        if (k_out) k_out[(long long)t * n + i] = from_float<T>(live ? Entry<FMT>::load(((const unsigned char *)c.d_k)[at]) * c.d_k_scale[sc] : 0.f);
-        if (v_out) v_out[(long long)t * n + i] = from_float<T>(live ? Entry<FMT>::load(((const unsigned char *)c.d_v)[at]) * c.d_v_scale[sc] : 0.f);
+    const long long at = b * c.block_stride + h * c.head_stride + off * c.token_stride + e0, sc = (long long)b * c.kv_heads + h;
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        T *out = side ? v_out : k_out;
+        if (!out) continue;
+        const uint2 w = *reinterpret_cast<const uint2 *>((const unsigned char *)(side ? c.d_v : c.d_k) + at);
+        const float scale = (side ? c.d_v_scale : c.d_k_scale)[sc];
+        T e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = from_float<T>(live ? Entry<FMT>::load((unsigned char)((j < 4 ? w.x : w.y) >> (j % 4 * 8))) * scale : 0.f);
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4 *>(out + i * 8)[j] = reinterpret_cast<const uint4 *>(e)[j];
     }
+}
+
+template <typename T, int FMT, int D>
+cudaError_t run_wide(AppendArgs a, bool rotary, cudaStream_t s)
+{
+    // A CTA looks through a few tokens for the first ones of runs, for a few heads: eight tokens and one head are a task
+    // for each warp in a decode step; in a prompt, where a CTA is busy only if a run begins in its tokens, more CTAs than
+    // there is room for come with more tokens and heads each.
+    constexpr int kFill = 148 * 4;
+    const int H = a.c.kv_heads;
+    a.tokens_each = a.tokens >= 2048 ? 16 : 8;
+    const long long chunks = (a.tokens + a.tokens_each - 1) / a.tokens_each;
+    const long long each = chunks * H / (148 * 16);
+    a.heads_each = each < 1 ? 1 : each < H ? (int)each : H;
+    a.groups = (H + a.heads_each - 1) / a.heads_each;
+    a.append_ctas = (int)chunks * a.groups;
+    a.q_groups = 0;
+    if (rotary && a.q.heads > 0) {
+        int g = (kFill + a.tokens - 1) / a.tokens;
+        const int at_least = kWide / (D * (int)sizeof(T) / 32);                      // heads that a CTA has in flight
+        a.q_heads_each = (a.q.heads + g - 1) / g;
+        if (a.q_heads_each < at_least) a.q_heads_each = at_least < a.q.heads ? at_least : a.q.heads;
+        a.q_groups = (a.q.heads + a.q_heads_each - 1) / a.q_heads_each;
+    }
+    const dim3 grid((unsigned)(a.append_ctas + a.tokens * a.q_groups));
+    constexpr int kPass = kWide / (D / 8) * 4;
+    if (rotary) {
+        const size_t smem = sizeof(float2) * (a.rot.rotary_dim / 2) * kPass;         // at most 64 pairs of 64 tokens: 32 KB
+        return launch(append_kernel<T, FMT, D, true>, grid, kWide, smem, s, a);
+    }
+    return launch(append_kernel<T, FMT, D, false>, grid, kWide, 0, s, a);
 }
 
 template <typename T, int FMT>
 cudaError_t run_append(const fluxbin_kv_cache_t &c, int tokens, const int *slots, const Heads &k, const Heads &v, const fluxbin_rotary_t *rot,
                        const int *positions, const Heads &q, const HeadsOut &qo, cudaStream_t s)
 {
+    const int n = 16 / (int)sizeof(T);
+    bool wide = aligned_to(k.p, 16) && aligned_to(v.p, 16) && k.token % n == 0 && k.head % n == 0 && v.token % n == 0 && v.head % n == 0;
+    AppendArgs a = {};
+    if (rot) {
+        a.rot = *rot;
+        a.q = {q.p, qo.p, q.p ? q.heads : 0, q.token, q.head, qo.token, qo.head};
+        wide = wide && rot->rotary_dim % (rot->interleaved ? 8 : 16) == 0 && wide_heads(*rot, sizeof(T) == 4 ? FLUXBIN_TYPE_FP32 : FLUXBIN_TYPE_FP16, a.q);
+    }
+    if (wide) {
+        a.c = c;
+        a.tokens = tokens;
+        a.slots = slots;
+        a.k = k;
+        a.v = v;
+        a.positions = positions;
+        return c.head_dim == 64 ? run_wide<T, FMT, 64>(a, rot, s) : c.head_dim == 128 ? run_wide<T, FMT, 128>(a, rot, s) : run_wide<T, FMT, 256>(a, rot, s);
+    }
     if (rot)
-        return launch(append_kernel<T, FMT, true>, dim3((unsigned)tokens, (unsigned)(c.kv_heads + (q.p ? q.heads : 0))), kThreads, 0, s, c, tokens,
+        return launch(append_any_kernel<T, FMT, true>, dim3((unsigned)tokens, (unsigned)(c.kv_heads + (q.p ? q.heads : 0))), kThreads, 0, s, c, tokens,
                       slots, k, v, *rot, positions, q, qo);
-    return launch(append_kernel<T, FMT, false>, dim3((unsigned)tokens, (unsigned)c.kv_heads), kThreads, 0, s, c, tokens, slots, k, v,
+    return launch(append_any_kernel<T, FMT, false>, dim3((unsigned)tokens, (unsigned)c.kv_heads), kThreads, 0, s, c, tokens, slots, k, v,
                   fluxbin_rotary_t{}, positions, q, qo);
 }
 
 template <typename T>
 cudaError_t run_read(const fluxbin_kv_cache_t &c, int tokens, const int *slots, void *k_out, void *v_out, cudaStream_t s)
 {
-    if (c.format == FLUXBIN_CACHE_INT8)
-        return launch(read_kernel<T, FLUXBIN_CACHE_INT8>, dim3((unsigned)tokens), kThreads, 0, s, c, slots, (T *)k_out, (T *)v_out);
-    return launch(read_kernel<T, FLUXBIN_CACHE_E4M3>, dim3((unsigned)tokens), kThreads, 0, s, c, slots, (T *)k_out, (T *)v_out);
+    const long long n = (long long)tokens * c.kv_heads * (c.head_dim / 8);
+    const dim3 grid((unsigned)((n + kWide - 1) / kWide));
+    if (c.format == FLUXBIN_CACHE_INT8) return launch(read_kernel<T, FLUXBIN_CACHE_INT8>, grid, kWide, 0, s, c, tokens, slots, (T *)k_out, (T *)v_out);
+    return launch(read_kernel<T, FLUXBIN_CACHE_E4M3>, grid, kWide, 0, s, c, tokens, slots, (T *)k_out, (T *)v_out);
 }
 
 } // namespace
@@ -147,7 +530,7 @@ extern "C" fluxbin_status_t fluxbin_kv_append(const fluxbin_kv_cache_t *cache, i
     fluxbin_status_t st = check_cache(cache);
     if (st != FLUXBIN_OK) return st;
     if (!type_known(dtype)) return FLUXBIN_ERR_UNSUPPORTED;
-    if (tokens < 0) return FLUXBIN_ERR_RANGE;
+    if (tokens < 0 || tokens > kMaxTokens) return FLUXBIN_ERR_RANGE;
     if (rotary) {
         st = check_rotary(rotary);
         if (st != FLUXBIN_OK) return st;
@@ -181,7 +564,7 @@ extern "C" fluxbin_status_t fluxbin_kv_read(const fluxbin_kv_cache_t *cache, int
     const fluxbin_status_t st = check_cache(cache);
     if (st != FLUXBIN_OK) return st;
     if (!type_known(dtype)) return FLUXBIN_ERR_UNSUPPORTED;
-    if (tokens < 0) return FLUXBIN_ERR_RANGE;
+    if (tokens < 0 || tokens > kMaxTokens || (int64_t)tokens * cache->kv_heads * (cache->head_dim / 8) / kWide >= INT32_MAX) return FLUXBIN_ERR_RANGE;
     if (tokens == 0 || (!d_k_out && !d_v_out)) return FLUXBIN_OK;
     if (!d_slots) return FLUXBIN_ERR_NULL;
     if (!aligned_to(d_k_out, 16) || !aligned_to(d_v_out, 16) || !aligned_to(d_slots, 4)) return FLUXBIN_ERR_ALIGNMENT;

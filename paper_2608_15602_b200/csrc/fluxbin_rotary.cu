@@ -48,44 +48,46 @@ extern "C" fluxbin_status_t fluxbin_rotary_frequencies(int32_t rotary_dim, doubl
 
 namespace {
 
-struct Side {
-    const void *in;
-    void *out;
-    int heads;
-    long long in_token, in_head, out_token, out_head;
-};
+constexpr int kThreads = 256;
+constexpr int kFewTokens = 148 * 4;              // CTAs that fill the device: fewer tokens split their heads
 
-// one thread per element pair (or per element past the turned part)
-template <typename T>
-__global__ void rotary_kernel(fluxbin_rotary_t rot, int inverse, int tokens, const int *positions, Side q, Side k)
+// One CTA per token, or per token and group of heads where there are few tokens: the angles of a token are formed once and
+// serve all its heads.  Bound by memory for prompts, by its launch and two dependent accesses for decode steps.
+template <typename T, int VE, bool INTER>
+__global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant__ fluxbin_rotary_t rot, float sign, const int *positions,
+                                                          const __grid_constant__ Side q, const __grid_constant__ Side k, int heads_each)
 {
+    __shared__ float2 angles[kMaxPairs];
+    let_successor_start();
     wait_for_predecessor();
-    const int half = rot.rotary_dim / 2, units = rot.head_dim - half;
-    const long long n = (long long)tokens * (q.heads + k.heads) * units;
-    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
-        const int u = (int)(i % units);
-        int h = (int)(i / units % (q.heads + k.heads));
-        const long long t = i / units / (q.heads + k.heads);
-        const Side &S = h < q.heads ? q : k;
-        if (h >= q.heads) h -= q.heads;
-        const T *x = (const T *)S.in + t * S.in_token + h * S.in_head;
-        T *y = (T *)S.out + t * S.out_token + h * S.out_head;
-        if (u >= half) { y[u + half] = x[u + half]; continue; }
-        float c, s, a, b;
-        pair_angle(positions[t], rot.d_turns[u], rot.magnitude, inverse ? -1.f : 1.f, c, s);
-        const int e0 = rot.interleaved ? 2 * u : u, e1 = rot.interleaved ? 2 * u + 1 : u + half;
-        turn_pair(to_float(x[e0]), to_float(x[e1]), c, s, a, b);
-        y[e0] = from_float<T>(a);
-        y[e1] = from_float<T>(b);
-    }
+    const int t = blockIdx.x, h0 = blockIdx.y * heads_each;
+    token_angles(rot, positions[t], sign, angles, threadIdx.x, kThreads);
+    __syncthreads();
+    turn_heads<T, VE, INTER>(rot, angles, q, k, t, h0, min(h0 + heads_each, q.heads + k.heads), threadIdx.x, kThreads);
 }
 
-template <typename T>
-cudaError_t run(const fluxbin_rotary_t &rot, int inverse, int tokens, const int *positions, const Side &q, const Side &k, cudaStream_t s)
+template <typename T, int VE, bool INTER>
+cudaError_t run_as(const fluxbin_rotary_t &rot, int inverse, int tokens, const int *positions, const Side &q, const Side &k, cudaStream_t s)
 {
-    const long long n = (long long)tokens * (q.heads + k.heads) * (rot.head_dim - rot.rotary_dim / 2);
-    const long long grid = (n + 255) / 256;
-    return launch(rotary_kernel<T>, dim3((unsigned)(grid < 65536 ? grid : 65536)), 256, 0, s, rot, inverse, tokens, positions, q, k);
+    const int heads = q.heads + k.heads;
+    int each = heads;
+    if (tokens < kFewTokens) {
+        const int units = rot.rotary_dim / 2 / (INTER ? VE / 2 : VE) + (rot.head_dim - rot.rotary_dim + VE - 1) / VE;
+        const int at_once = kThreads / units > 0 ? kThreads / units : 1, groups = (kFewTokens + tokens - 1) / tokens;
+        each = (heads + groups - 1) / groups;
+        if (each < at_once) each = at_once;
+        if (each > heads) each = heads;
+    }
+    return launch(rotary_kernel<T, VE, INTER>, dim3((unsigned)tokens, (unsigned)((heads + each - 1) / each)), kThreads, 0, s, rot, inverse ? -1.f : 1.f,
+                  positions, q, k, each);
+}
+template <typename T>
+cudaError_t run(const fluxbin_rotary_t &rot, int dtype, int inverse, int tokens, const int *positions, const Side &q, const Side &k, cudaStream_t s)
+{
+    constexpr int WIDE = 16 / sizeof(T);
+    if (wide_heads(rot, dtype, q) && wide_heads(rot, dtype, k))
+        return rot.interleaved ? run_as<T, WIDE, true>(rot, inverse, tokens, positions, q, k, s) : run_as<T, WIDE, false>(rot, inverse, tokens, positions, q, k, s);
+    return rot.interleaved ? run_as<T, 2, true>(rot, inverse, tokens, positions, q, k, s) : run_as<T, 1, false>(rot, inverse, tokens, positions, q, k, s);
 }
 
 } // namespace
@@ -99,7 +101,7 @@ extern "C" fluxbin_status_t fluxbin_rotary(const fluxbin_rotary_t *rotary, int32
     const fluxbin_status_t st = check_rotary(rotary);
     if (st != FLUXBIN_OK) return st;
     if (!type_known(dtype)) return FLUXBIN_ERR_UNSUPPORTED;
-    if (tokens < 0 || q_heads < 1 || (d_k && k_heads < 1)) return FLUXBIN_ERR_RANGE;
+    if (tokens < 0 || q_heads < 1 || q_heads > 65535 || (d_k && (k_heads < 1 || k_heads > 65535))) return FLUXBIN_ERR_RANGE;
     if (tokens == 0) return FLUXBIN_OK;
     if (!d_positions || !d_q || !d_q_out || (d_k && !d_k_out)) return FLUXBIN_ERR_NULL;
     const size_t size = (size_t)type_size(dtype);
@@ -108,8 +110,8 @@ extern "C" fluxbin_status_t fluxbin_rotary(const fluxbin_rotary_t *rotary, int32
     const Side q = {d_q, d_q_out, q_heads, q_token, q_head, qo_token, qo_head};
     const Side k = {d_k, d_k_out, d_k ? k_heads : 0, k_token, k_head, ko_token, ko_head};
     cudaStream_t s = (cudaStream_t)cuda_stream;
-    if (dtype == FLUXBIN_TYPE_FP16) FBD_CUDA(run<__half>(*rotary, inverse, tokens, d_positions, q, k, s));
-    else if (dtype == FLUXBIN_TYPE_BF16) FBD_CUDA(run<__nv_bfloat16>(*rotary, inverse, tokens, d_positions, q, k, s));
-    else FBD_CUDA(run<float>(*rotary, inverse, tokens, d_positions, q, k, s));
+    if (dtype == FLUXBIN_TYPE_FP16) FBD_CUDA(run<__half>(*rotary, dtype, inverse, tokens, d_positions, q, k, s));
+    else if (dtype == FLUXBIN_TYPE_BF16) FBD_CUDA(run<__nv_bfloat16>(*rotary, dtype, inverse, tokens, d_positions, q, k, s));
+    else FBD_CUDA(run<float>(*rotary, dtype, inverse, tokens, d_positions, q, k, s));
     return FLUXBIN_OK;
 }
