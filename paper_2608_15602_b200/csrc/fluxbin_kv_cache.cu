@@ -157,32 +157,42 @@ __device__ __forceinline__ void turned8(const T *x, int e0, const fluxbin_rotary
     Eight<T> other;
     other.load(x + (second ? e0 - half : e0 + half));
     other.get(w);
+    const float4 *pair = reinterpret_cast<const float4 *>(angles + (second ? e0 - half : e0));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float2 a = angles[(second ? e0 - half : e0) + i];
-        float f, g;
-        turn_pair(second ? w[i] : v[i], second ? v[i] : w[i], a.x, a.y, f, g);
-        v[i] = second ? g : f;
+    for (int i = 0; i < 8; i += 2) {
+        const float4 a = pair[i / 2];
+        // (turn_second(other, own) and turn_first(own, other) differ in the sign of the other's product alone)
+        v[i] = fmaf(v[i], a.x, __fmul_rn(w[i], second ? a.y : -a.y));
+        v[i + 1] = fmaf(v[i + 1], a.z, __fmul_rn(w[i + 1], second ? a.w : -a.w));
     }
 }
 
-// |v| of eight elements; a NaN or infinity among them counts as infinity
-__device__ __forceinline__ float largest8(const float (&v)[8])
+// the largest |v| as its bits, which order like the magnitudes; infinities and NaN lie above all others
+__device__ __forceinline__ unsigned largest8(unsigned most, const float (&v)[8])
 {
-    float m = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = fabsf(v[i]) < INFINITY ? fmaxf(m, fabsf(v[i])) : INFINITY;
-    return m;
+    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
+    return most;
 }
+// eight entries; |v * inverse| exceeds the format's largest value by rounding at most
 template <int FMT> __device__ __forceinline__ uint2 entries8(const float (&v)[8], float inverse)
 {
-    unsigned char e[8];
+    uint32_t w[2];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) e[i] = Entry<FMT>::store(__fmul_rn(v[i], inverse));
-    uint2 w;
-    w.x = e[0] | e[1] << 8 | e[2] << 16 | (unsigned)e[3] << 24;
-    w.y = e[4] | e[5] << 8 | e[6] << 16 | (unsigned)e[7] << 24;
-    return w;
+    for (int i = 0; i < 2; ++i) {
+        if constexpr (FMT == FLUXBIN_CACHE_INT8) {
+            // added to 1.5 * 2^23 a value is rounded to a whole number, to nearest even, in the low bits
+            uint32_t e[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] = __float_as_uint(__fadd_rn(__fmul_rn(v[4 * i + j], inverse), 12582912.f));
+            w[i] = __byte_perm(__byte_perm(e[0], e[1], 0x0040), __byte_perm(e[2], e[3], 0x0040), 0x5410);
+        } else {
+            const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(__fmul_rn(v[4 * i], inverse), __fmul_rn(v[4 * i + 1], inverse)), __NV_SATFINITE, __NV_E4M3);
+            const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(__fmul_rn(v[4 * i + 2], inverse), __fmul_rn(v[4 * i + 3], inverse)), __NV_SATFINITE, __NV_E4M3);
+            w[i] = lo | hi << 16;
+        }
+    }
+    return make_uint2(w[0], w[1]);
 }
 template <int FMT> __device__ __forceinline__ void requantise8(unsigned char *p, float ratio)
 {
@@ -213,20 +223,22 @@ __global__ void __launch_bounds__(kWide) append_kernel(const __grid_constant__ A
     constexpr int PIECES = D / 8;                // of eight elements
     constexpr int AT_ONCE = kWide / PIECES;      // tokens a pass has side by side
     constexpr int DEEP = 4, PASS = AT_ONCE * DEEP;
-    extern __shared__ float2 angles[];           // [PASS][pairs], or [kMaxPairs] for the q heads
-    __shared__ float part[2][kWarpsWide];
+    extern __shared__ __align__(16) float2 angles[];           // [PASS][pairs], or [kMaxPairs] for the q heads
+    __shared__ unsigned part[2][kWarpsWide];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     let_successor_start();
     wait_for_predecessor();
 
     if (ROT && (int)blockIdx.x >= a.append_ctas) {
         const int i = blockIdx.x - a.append_ctas, t = i / a.q_groups, h0 = i % a.q_groups * a.q_heads_each;
-        token_angles(a.rot, a.positions[t], 1.f, angles, tid, kWide);
-        __syncthreads();
         const Side none = {};
         const int h1 = min(h0 + a.q_heads_each, a.q.heads);
-        if (a.rot.interleaved) turn_heads<T, 16 / sizeof(T), true>(a.rot, angles, a.q, none, t, h0, h1, tid, kWide);
-        else turn_heads<T, 16 / sizeof(T), false>(a.rot, angles, a.q, none, t, h0, h1, tid, kWide);
+        auto form = [&]() {
+            token_angles(a.rot, a.positions[t], 1.f, angles, tid, kWide);
+            __syncthreads();
+        };
+        if (a.rot.interleaved) turn_heads<T, 16 / sizeof(T), true>(a.rot, angles, a.q, none, t, h0, h1, tid, kWide, form);
+        else turn_heads<T, 16 / sizeof(T), false>(a.rot, angles, a.q, none, t, h0, h1, tid, kWide, form);
         return;
     }
 
@@ -278,7 +290,8 @@ __global__ void __launch_bounds__(kWide) append_kernel(const __grid_constant__ A
             const Heads &src = side ? a.v : a.k;
             float *scale = (side ? a.c.d_v_scale : a.c.d_k_scale) + (long long)block * H + h;
             const float before = offset ? *scale : 0.f;
-            float v[kShortRun][EACH][8], most = 0.f;
+            float v[kShortRun][EACH][8];
+            unsigned most = 0;
 #pragma unroll
             for (int i = 0; i < kShortRun; ++i)
 #pragma unroll
@@ -292,11 +305,11 @@ __global__ void __launch_bounds__(kWide) append_kernel(const __grid_constant__ A
                         w.load(x + e0);
                         w.get(v[i][j]);
                     }
-                    most = fmaxf(most, largest8(v[i][j]));
+                    most = largest8(most, v[i][j]);
                 }
 #pragma unroll
-            for (int o = 8; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));      // of this half
-            const Scale s = scale_of(before, most, top_inverse);
+            for (int o = 8; o; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));        // of this half
+            const Scale s = scale_of(before, __uint_as_float(most), top_inverse);
             unsigned char *cells = (unsigned char *)(side ? a.c.d_v : a.c.d_k) + block * a.c.block_stride + h * a.c.head_stride;
             if (offset && !(s.now == before) && sl < LANES) {
                 const float ratio = __fmul_rn(before, s.inverse);
@@ -345,7 +358,8 @@ __global__ void __launch_bounds__(kWide) append_kernel(const __grid_constant__ A
         };
         if (one_pass) pass_angles(0);
         for (int h = h0; h < h1; ++h) {
-            float kv[DEEP][8], most[2] = {0.f, 0.f};
+            float kv[DEEP][8];
+            unsigned most[2] = {0, 0};
             Eight<T> vv[DEEP];
             auto load = [&](int base) {
 #pragma unroll
@@ -374,14 +388,14 @@ __global__ void __launch_bounds__(kWide) append_kernel(const __grid_constant__ A
                     if (base + sub + j * AT_ONCE >= r.count) continue;
                     float w[8];
                     vv[j].get(w);
-                    most[0] = fmaxf(most[0], largest8(kv[j]));
-                    most[1] = fmaxf(most[1], largest8(w));
+                    most[0] = largest8(most[0], kv[j]);
+                    most[1] = largest8(most[1], w);
                 }
             }
 #pragma unroll
             for (int o = 16; o; o >>= 1)
 #pragma unroll
-                for (int x = 0; x < 2; ++x) most[x] = fmaxf(most[x], __shfl_xor_sync(0xffffffffu, most[x], o));
+                for (int x = 0; x < 2; ++x) most[x] = max(most[x], __shfl_xor_sync(0xffffffffu, most[x], o));
             __syncthreads();                                                         // `part` of the head before has been read
             if (lane == 0) { part[0][warp] = most[0]; part[1][warp] = most[1]; }
             __syncthreads();
@@ -389,12 +403,12 @@ __global__ void __launch_bounds__(kWide) append_kernel(const __grid_constant__ A
             unsigned char *cells[2];
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                float m = 0.f;
+                unsigned m = 0;
 #pragma unroll
-                for (int w = 0; w < kWarpsWide; ++w) m = fmaxf(m, part[x][w]);
+                for (int w = 0; w < kWarpsWide; ++w) m = max(m, part[x][w]);
                 float *scale = (x ? a.c.d_v_scale : a.c.d_k_scale) + (long long)r.block * H + h;
                 const float before = r.offset ? *scale : 0.f;
-                sc[x] = scale_of(before, m, top_inverse);
+                sc[x] = scale_of(before, __uint_as_float(m), top_inverse);
                 cells[x] = (unsigned char *)(x ? a.c.d_v : a.c.d_k) + r.block * a.c.block_stride + h * a.c.head_stride;
                 if (r.offset && !(sc[x].now == before)) {
                     const float ratio = __fmul_rn(before, sc[x].inverse);
@@ -455,19 +469,25 @@ template <typename T, int FMT, int D>
 cudaError_t run_wide(AppendArgs a, bool rotary, cudaStream_t s)
 {
     // A CTA looks through a few tokens for the first ones of runs, for a few heads: eight tokens and one head are a task
-    // for each warp in a decode step; in a prompt, where a CTA is busy only if a run begins in its tokens, more CTAs than
-    // there is room for come with more tokens and heads each.
-    constexpr int kFill = 148 * 4;
+    // for each warp in a decode step.  In a prompt a CTA is busy only if a run begins in its tokens; its heads share the
+    // run's angles, so they are no more cut than it takes to give every SM two CTAs that are busy.
     const int H = a.c.kv_heads;
     a.tokens_each = a.tokens >= 2048 ? 16 : 8;
     const long long chunks = (a.tokens + a.tokens_each - 1) / a.tokens_each;
-    const long long each = chunks * H / (148 * 16);
+    const long long each = (long long)a.tokens / a.c.block_tokens * H / (148 * 2);
     a.heads_each = each < 1 ? 1 : each < H ? (int)each : H;
     a.groups = (H + a.heads_each - 1) / a.heads_each;
     a.append_ctas = (int)chunks * a.groups;
     a.q_groups = 0;
+    if (rotary && a.q.heads > 0 && a.tokens >= kFewTokens) {
+        // a prompt's queries fill the device by themselves, at twice the CTAs on an SM that the rest leaves them
+        const cudaError_t e = launch_rotary(a.rot, std::is_same<T, float>::value ? FLUXBIN_TYPE_FP32 : std::is_same<T, __half>::value ? FLUXBIN_TYPE_FP16 : FLUXBIN_TYPE_BF16,
+                                            0, a.tokens, a.positions, a.q, Side{}, s);
+        if (e != cudaSuccess) return e;
+        a.q.heads = 0;
+    }
     if (rotary && a.q.heads > 0) {
-        int g = (kFill + a.tokens - 1) / a.tokens;
+        int g = (kFewTokens + a.tokens - 1) / a.tokens;
         const int at_least = kWide / (D * (int)sizeof(T) / 32);                      // heads that a CTA has in flight
         a.q_heads_each = (a.q.heads + g - 1) / g;
         if (a.q_heads_each < at_least) a.q_heads_each = at_least < a.q.heads ? at_least : a.q.heads;

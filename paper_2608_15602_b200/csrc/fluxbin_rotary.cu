@@ -49,21 +49,21 @@ extern "C" fluxbin_status_t fluxbin_rotary_frequencies(int32_t rotary_dim, doubl
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kFewTokens = 148 * 4;              // CTAs that fill the device: fewer tokens split their heads
 
 // One CTA per token, or per token and group of heads where there are few tokens: the angles of a token are formed once and
 // serve all its heads.  Bound by memory for prompts, by its launch and two dependent accesses for decode steps.
 template <typename T, int VE, bool INTER>
-__global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant__ fluxbin_rotary_t rot, float sign, const int *positions,
+__global__ void __launch_bounds__(kThreads, 3) rotary_kernel(const __grid_constant__ fluxbin_rotary_t rot, float sign, const int *positions,
                                                           const __grid_constant__ Side q, const __grid_constant__ Side k, int heads_each)
 {
     __shared__ float2 angles[kMaxPairs];
     let_successor_start();
     wait_for_predecessor();
     const int t = blockIdx.x, h0 = blockIdx.y * heads_each;
-    token_angles(rot, positions[t], sign, angles, threadIdx.x, kThreads);
-    __syncthreads();
-    turn_heads<T, VE, INTER>(rot, angles, q, k, t, h0, min(h0 + heads_each, q.heads + k.heads), threadIdx.x, kThreads);
+    turn_heads<T, VE, INTER>(rot, angles, q, k, t, h0, min(h0 + heads_each, q.heads + k.heads), threadIdx.x, kThreads, [&]() {
+        token_angles(rot, positions[t], sign, angles, threadIdx.x, kThreads);
+        __syncthreads();
+    });
 }
 
 template <typename T, int VE, bool INTER>
@@ -92,6 +92,14 @@ cudaError_t run(const fluxbin_rotary_t &rot, int dtype, int inverse, int tokens,
 
 } // namespace
 
+cudaError_t fbd::launch_rotary(const fluxbin_rotary_t &rot, int dtype, int inverse, int tokens, const int *positions, const Side &q, const Side &k,
+                               cudaStream_t s)
+{
+    if (dtype == FLUXBIN_TYPE_FP16) return run<__half>(rot, dtype, inverse, tokens, positions, q, k, s);
+    if (dtype == FLUXBIN_TYPE_BF16) return run<__nv_bfloat16>(rot, dtype, inverse, tokens, positions, q, k, s);
+    return run<float>(rot, dtype, inverse, tokens, positions, q, k, s);
+}
+
 extern "C" fluxbin_status_t fluxbin_rotary(const fluxbin_rotary_t *rotary, int32_t dtype, int32_t inverse, int32_t tokens,
                                            const int32_t *d_positions, const void *d_q, int32_t q_heads, int64_t q_token, int64_t q_head,
                                            void *d_q_out, int64_t qo_token, int64_t qo_head, const void *d_k, int32_t k_heads,
@@ -109,9 +117,6 @@ extern "C" fluxbin_status_t fluxbin_rotary(const fluxbin_rotary_t *rotary, int32
         !aligned_to(d_positions, 4)) return FLUXBIN_ERR_ALIGNMENT;
     const Side q = {d_q, d_q_out, q_heads, q_token, q_head, qo_token, qo_head};
     const Side k = {d_k, d_k_out, d_k ? k_heads : 0, k_token, k_head, ko_token, ko_head};
-    cudaStream_t s = (cudaStream_t)cuda_stream;
-    if (dtype == FLUXBIN_TYPE_FP16) FBD_CUDA(run<__half>(*rotary, dtype, inverse, tokens, d_positions, q, k, s));
-    else if (dtype == FLUXBIN_TYPE_BF16) FBD_CUDA(run<__nv_bfloat16>(*rotary, dtype, inverse, tokens, d_positions, q, k, s));
-    else FBD_CUDA(run<float>(*rotary, dtype, inverse, tokens, d_positions, q, k, s));
+    FBD_CUDA(launch_rotary(*rotary, dtype, inverse, tokens, d_positions, q, k, (cudaStream_t)cuda_stream));
     return FLUXBIN_OK;
 }
