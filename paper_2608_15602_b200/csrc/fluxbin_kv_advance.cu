@@ -1,11 +1,14 @@
 // Block tables and slot maps of a step, from request lengths (fluxbin_kv_advance).
 #include "fluxbin_device.cuh"
 
+#include <atomic>
+
 using namespace fbd;
 
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kMaxBatch = 8192;
+constexpr unsigned kMany = 0xffffffffu;         // sums stay there once they get there: past every size
 
 struct Args {
     int batch, tokens, bs, width, capacity;
@@ -15,100 +18,138 @@ struct Args {
     int *num_free_out, *lengths_out, *granted, *query_start, *positions, *slots, *requests;
 };
 
-// inclusive sum over the CTA
-__device__ __forceinline__ long long block_scan(long long v, long long *scratch)
+// what a step does to one request
+struct Change {
+    long long len, n;            // its length and its new tokens (< 0: dropped ones)
+    int had, want;               // blocks before and after
+    unsigned gone, need, count;  // blocks given back, blocks asked for, tokens added
+    bool fits;
+};
+__device__ __forceinline__ Change change_of(const Args &a, int r)
 {
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long up = __shfl_up_sync(0xffffffffu, v, o);
-        if (lane >= o) v += up;
+    Change c;
+    c.len = max(a.lengths[r], 0);
+    c.n = a.fresh[r];
+    const long long after = max(c.len + c.n, 0ll);
+    const long long had = (c.len + a.bs - 1) / a.bs, want = (after + a.bs - 1) / a.bs;
+    c.fits = want <= a.width && after <= INT32_MAX;
+    c.had = (int)had;
+    c.want = (int)want;
+    c.gone = had > want && had <= a.width ? (unsigned)(had - want) : 0;
+    c.need = c.fits && want > had ? (unsigned)(want - had) : 0;
+    c.count = c.n > 0 ? (unsigned)c.n : 0;
+    return c;
+}
+__device__ __forceinline__ unsigned add(unsigned x, unsigned y) { return x + y < x ? kMany : x + y; }
+
+// the first entry of an ascending array that is above x
+__device__ __forceinline__ int first_above(const unsigned *sums, int n, unsigned x)
+{
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int m = (lo + hi) / 2;
+        if (sums[m] > x) hi = m; else lo = m + 1;
     }
-    __syncthreads();
-    if (lane == 31) scratch[w] = v;
-    __syncthreads();
-    for (int i = 0; i < w; ++i) v += scratch[i];
-    return v;
+    return lo;
 }
 
-// One CTA; a thread per request, in passes of 1024 requests.  Pass 1 returns blocks, pass 2 takes them.
-__global__ void __launch_bounds__(kThreads) advance_kernel(Args a)
+// Three running sums over the requests -- blocks given back, blocks asked for, new tokens -- say where everything goes, so
+// that no block, slot or token waits for another: each is a thread that looks its request up in the sums.  Every CTA
+// forms the sums for itself (a few thousand integers); a block that is given back and taken again in one step is read
+// where its last owner's table has it, not from the free list that another CTA is writing.
+__global__ void __launch_bounds__(1024) advance_kernel(const __grid_constant__ Args a)
 {
-    __shared__ long long scratch[kThreads / 32];
-    __shared__ long long carry[3];
+    extern __shared__ unsigned sums[];           // [3][batch], including the request itself
+    __shared__ unsigned warp_sum[3][32];
+    unsigned *gone = sums, *need = sums + a.batch, *count = sums + 2 * a.batch;
+    const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, warp = tid >> 5;
+    let_successor_start();
     wait_for_predecessor();
-    const int bs = a.bs;
-    const long long nf = min(max(a.num_free[0], 0), a.capacity);
-    if (threadIdx.x < 3) carry[threadIdx.x] = 0;
-    for (int r0 = 0; r0 < a.batch; r0 += kThreads) {
-        const int r = r0 + threadIdx.x;
-        long long gone = 0, had = 0, want = 0;
-        if (r < a.batch) {
-            const long long len = max(a.lengths[r], 0), n = a.fresh[r];
-            had = (len + bs - 1) / bs;
-            want = (max(len + n, 0ll) + bs - 1) / bs;
-            gone = max(had - want, 0ll);
-            if (had > a.width) gone = 0;
+    const int per = (a.batch + threads - 1) / threads, lo = min(tid * per, a.batch), hi = min(lo + per, a.batch);
+    const int nf = min(max(a.num_free[0], 0), a.capacity);
+    unsigned mine[3] = {0, 0, 0};
+    for (int r = lo; r < hi; ++r) {
+        const Change c = change_of(a, r);
+        gone[r] = mine[0] = add(mine[0], c.gone);
+        need[r] = mine[1] = add(mine[1], c.need);
+        count[r] = mine[2] = add(mine[2], c.count);
+    }
+    unsigned upto[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        upto[k] = mine[k];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned x = __shfl_up_sync(0xffffffffu, upto[k], o);
+            if (lane >= o) upto[k] = add(upto[k], x);
         }
-        __syncthreads();
-        const long long base = carry[0], upto = block_scan(gone, scratch) + base;
-        for (long long i = 0; i < gone; ++i) {
-            const long long at = nf + upto - gone + i;
-            if (at < a.capacity) a.free[at] = a.table[r * a.table_stride + want + i];
-        }
-        __syncthreads();
-        if (threadIdx.x == kThreads - 1) carry[0] = upto;
+        if (lane == 31) warp_sum[k][warp] = upto[k];
+        upto[k] = __shfl_up_sync(0xffffffffu, upto[k], 1);       // of the threads before
+        if (lane == 0) upto[k] = 0;
     }
     __syncthreads();
-    const long long end = min(nf + carry[0], (long long)a.capacity);
-    long long taken = 0;
-    for (int r0 = 0; r0 < a.batch; r0 += kThreads) {
-        const int r = r0 + threadIdx.x;
-        long long len = 0, n = 0, had = 0, want = 0, need = 0;
-        bool fits = true;
-        if (r < a.batch) {
-            len = max(a.lengths[r], 0);
-            n = a.fresh[r];
-            had = (len + bs - 1) / bs;
-            want = (max(len + n, 0ll) + bs - 1) / bs;
-            fits = want <= a.width && len + n <= INT32_MAX;
-            need = fits ? max(want - had, 0ll) : 0;
-        }
-        __syncthreads();
-        const long long b1 = carry[1], b2 = carry[2];
-        const long long asked = block_scan(need, scratch) + b1, upto = block_scan(max(n, 0ll), scratch) + b2;
-        const bool ok = n <= 0 || (fits && (need == 0 || asked <= end));
-        if (r < a.batch) {
-            for (long long i = 0; ok && i < need; ++i) a.table[r * a.table_stride + had + i] = a.free[end - 1 - (asked - need) - i];
-            a.lengths_out[r] = (int)(ok ? max(len + n, 0ll) : len);
-            a.granted[r] = ok;
-            const long long first = upto - max(n, 0ll);
-            a.query_start[r] = (int)min(first, (long long)INT32_MAX);
-            for (long long i = 0; i < n && first + i < a.tokens; ++i) {
-                const long long p = len + i;
-                a.positions[first + i] = (int)p;
-                const long long b = ok ? a.table[r * a.table_stride + p / bs] : -1, s = b * bs + p % bs;
-                a.slots[first + i] = b >= 0 && s <= INT32_MAX ? (int)s : -1;
-                a.requests[first + i] = r;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        unsigned x = lane < warp ? warp_sum[k][lane] : 0;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) x = add(x, __shfl_xor_sync(0xffffffffu, x, o));
+        upto[k] = add(upto[k], x);
+    }
+    for (int r = lo; r < hi; ++r) {
+        gone[r] = add(gone[r], upto[0]);
+        need[r] = add(need[r], upto[1]);
+        count[r] = add(count[r], upto[2]);
+    }
+    __syncthreads();
+
+    const unsigned back = min(gone[a.batch - 1], (unsigned)(a.capacity - nf)), end = (unsigned)nf + back;
+    const int over = first_above(need, a.batch, end);            // the first request whose blocks are not there
+    const unsigned taken = over > 0 ? need[over - 1] : 0;
+    const unsigned added = min(count[a.batch - 1], (unsigned)a.tokens);
+    auto given_back = [&](unsigned i) {
+        const int r = first_above(gone, a.batch, i);
+        return a.table[r * a.table_stride + change_of(a, r).want + (i - (r > 0 ? gone[r - 1] : 0))];
+    };
+    auto taken_block = [&](unsigned i) {         // the i-th block asked for, off the end of the list
+        const unsigned at = end - 1 - i;
+        return at >= (unsigned)nf ? given_back(at - nf) : a.free[at];
+    };
+    auto is_granted = [&](const Change &c, int r) { return c.n <= 0 || (c.fits && (c.need == 0 || need[r] <= end)); };
+
+    const unsigned step = gridDim.x * threads, first = blockIdx.x * threads + tid;
+    for (unsigned i = first; i < (unsigned)a.batch; i += step) {
+        const Change c = change_of(a, i);
+        const bool ok = is_granted(c, i);
+        a.lengths_out[i] = (int)(ok ? max(c.len + c.n, 0ll) : c.len);
+        a.granted[i] = ok;
+        a.query_start[i + 1] = (int)min(count[i], (unsigned)INT32_MAX);
+    }
+    for (unsigned i = first; i < (unsigned)a.tokens; i += step) {
+        int p = 0, slot = -1, r = -1;
+        if (i < added) {
+            r = first_above(count, a.batch, i);
+            const Change c = change_of(a, r);
+            const long long at = c.len + (i - (r > 0 ? count[r - 1] : 0));
+            p = (int)min(at, (long long)INT32_MAX);
+            if (is_granted(c, r)) {
+                const int b = (int)(at / a.bs);
+                const long long id = b < c.had ? a.table[r * a.table_stride + b] : taken_block((r > 0 ? need[r - 1] : 0) + (b - c.had));
+                const long long s = id * a.bs + at % a.bs;
+                slot = id >= 0 && s <= INT32_MAX ? (int)s : -1;
             }
-            if (ok && need > 0) taken = asked;
         }
-        __syncthreads();
-        if (threadIdx.x == kThreads - 1) { carry[1] = asked; carry[2] = upto; }
+        a.positions[i] = p;
+        a.slots[i] = slot;
+        a.requests[i] = r;
     }
-    // what the last granted request had asked for in all
-    for (int o = 16; o; o >>= 1) taken = max(taken, __shfl_xor_sync(0xffffffffu, taken, o));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = taken;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < kThreads / 32; ++i) taken = max(taken, scratch[i]);
+    for (unsigned i = first; i < taken; i += step) {
+        const int r = first_above(need, a.batch, i);
+        a.table[r * a.table_stride + change_of(a, r).had + (i - (r > 0 ? need[r - 1] : 0))] = taken_block(i);
+    }
+    for (unsigned i = first; i < back; i += step) a.free[nf + i] = given_back(i);
+    if (first == 0) {
         a.num_free_out[0] = (int)(end - taken);
-        a.query_start[a.batch] = (int)min(carry[2], (long long)INT32_MAX);
-    }
-    for (long long t = carry[2] + threadIdx.x; t < a.tokens; t += kThreads) {
-        a.positions[t] = 0;
-        a.slots[t] = -1;
-        a.requests[t] = -1;
+        a.query_start[0] = 0;
     }
 }
 
@@ -121,7 +162,7 @@ extern "C" fluxbin_status_t fluxbin_kv_advance(int32_t batch, int32_t tokens, in
                                                int32_t *d_query_start, int32_t *d_positions, int32_t *d_slots, int32_t *d_requests,
                                                void *cuda_stream)
 {
-    if (batch < 1 || batch > 8192 || tokens < 0 || block_tokens < 1 || block_tokens > 1024 || table_width < 1 || table_stride < table_width ||
+    if (batch < 1 || batch > kMaxBatch || tokens < 0 || block_tokens < 1 || block_tokens > 1024 || table_width < 1 || table_stride < table_width ||
         free_capacity < 1) return FLUXBIN_ERR_RANGE;
     if (!d_lengths || !d_new || !d_table || !d_free || !d_num_free || !d_num_free_out || !d_lengths_out || !d_granted || !d_query_start ||
         (tokens > 0 && (!d_positions || !d_slots || !d_requests))) return FLUXBIN_ERR_NULL;
@@ -131,6 +172,21 @@ extern "C" fluxbin_status_t fluxbin_kv_advance(int32_t batch, int32_t tokens, in
         if (!aligned_to(p, 4)) return FLUXBIN_ERR_ALIGNMENT;
     const Args a = {batch, tokens, block_tokens, table_width, free_capacity, d_lengths, d_new, d_num_free, d_table, d_free, table_stride,
                     d_num_free_out, d_lengths_out, d_granted, d_query_start, d_positions, d_slots, d_requests};
-    FBD_CUDA(launch(advance_kernel, dim3(1), kThreads, 0, (cudaStream_t)cuda_stream, a));
+    // a small batch is a matter of latency: one CTA, no wider than the batch; else threads for the requests' sums and CTAs
+    // for the tokens (at most one on each of 148 SMs)
+    const int threads = batch <= 256 ? 256 : 1024;
+    const int64_t ctas = ((int64_t)tokens + threads - 1) / threads;
+    const size_t smem = (size_t)batch * 3 * sizeof(unsigned);
+    if (smem > 48 * 1024) {
+        static std::atomic<bool> opted[fb::kMaxDevices];
+        int dev = 0;
+        FBD_CUDA(cudaGetDevice(&dev));
+        if (dev < 0 || dev >= fb::kMaxDevices) return FLUXBIN_ERR_UNSUPPORTED;
+        if (!opted[dev].load(std::memory_order_relaxed)) {
+            FBD_CUDA(cudaFuncSetAttribute(advance_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxBatch * 3 * (int)sizeof(unsigned)));
+            opted[dev].store(true, std::memory_order_relaxed);
+        }
+    }
+    FBD_CUDA(launch(advance_kernel, dim3((unsigned)(ctas < 1 ? 1 : ctas < 148 ? ctas : 148)), threads, smem, (cudaStream_t)cuda_stream, a));
     return FLUXBIN_OK;
 }
