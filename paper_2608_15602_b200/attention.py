@@ -140,10 +140,19 @@ class KVCache:
         self.num_blocks, self.kv_heads, self.block_tokens, self.head_dim, self.device = nb, H, bs, D, k.device
         self.desc = fluxbin.CacheDesc(nb, bs, H, D, _STORED[k.dtype], k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
                                       k_scale.data_ptr(), v_scale.data_ptr())
-        self._ref, self._scale = ctypes.addressof(self.desc), 1.0 / math.sqrt(D)
+        self._ref, self._scale, self._last = ctypes.addressof(self.desc), 1.0 / math.sqrt(D), {}
         status = fluxbin.kv_validate_status(self.desc)
         if status:
             raise fluxbin.FluxBinError(status, "fluxbin_kv_validate")
+
+    def _new(self, shape: tuple, dtype: torch.dtype) -> torch.Tensor:
+        """torch.empty(shape, dtype) on the cache's device; made like the last (small) one of that kind it takes half the time."""
+        if math.prod(shape) > 1 << 16:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        last = self._last.get(dtype)
+        if last is None or last.shape != shape:
+            last = self._last[dtype] = torch.empty(shape, dtype=dtype, device=self.device)
+        return torch.empty_like(last)
 
     def append(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, rotary: Rotary | None = None,
                positions: torch.Tensor | None = None, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None, stream=None):
@@ -175,8 +184,7 @@ class KVCache:
         if dtype not in _TYPES:
             raise TypeError("dtype: fp16, bf16 or fp32 is wanted")
         n = slots.shape[0]
-        both = torch.empty((2, n, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
-        k, v = both.unbind()
+        k, v = self._new((2, n, self.kv_heads, self.head_dim), dtype).unbind()
         fluxbin.kv_read_call(self._ref, _TYPES[dtype], n, _int32(slots, n, "slots"), k.data_ptr(), v.data_ptr(), _stream(slots, stream))
         return k, v
 
@@ -202,7 +210,7 @@ class KVCache:
             raise ValueError("table: a CUDA int32 tensor [batch][max_blocks] with contiguous rows is wanted")
         B, width = table.shape
         out, op, ot, os_ = _output(out, q, qh, "out")
-        lse = torch.empty((n, qh), dtype=torch.float32, device=self.device) if with_lse else None
+        lse = self._new((n, qh), torch.float32) if with_lse else None
         fluxbin.kv_attend_call(self._ref, _TYPES[dt], B, n, qp, qh, qt, qs, 0 if query_start is None else _int32(query_start, B + 1, "query_start"),
                                _int32(lengths, B, "lengths"), table.data_ptr(), max(table.stride(0), width), width,
                                self._scale if scale is None else scale, op, ot, os_, 0 if lse is None else lse.data_ptr(), ws.tensor.data_ptr(),

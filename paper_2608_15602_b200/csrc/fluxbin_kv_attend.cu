@@ -31,16 +31,21 @@ using namespace fbd;
 
 namespace {
 
-// Warps of a CTA, CTAs on an SM, tiles of 16 tokens that a warp has under way.  Measured at head_dim 128 with 8 rows on 64
-// requests of up to 16384 tokens: 4 x 3 with 4 tiles 242 us, 8 x 2 with 3 249, 6 x 2 with 4 257, 4 x 4 with 3 (128
-// registers, spills) 277, 12 x 1 with 4 288: small CTAs, so that the others go on while one ends a job, and tiles on their
-// way rather than warps.
+// Warps of a CTA, CTAs on an SM, tiles of 16 tokens that a warp has under way, whether the queries stay in shared memory (the
+// output takes the registers), by head dimension and tiles of 8 query rows.  Measured at 128 with 8 rows on 64 requests of up
+// to 16384 tokens: 4 x 3 with 4 tiles 242 us, 8 x 2 with 3 249, 6 x 2 with 4 257, 4 x 4 with 3 (128 registers, spills) 277, 12 x
+// 1 with 4 288: small CTAs, so that the others go on while one ends a job, and tiles on their way rather than warps.  With 16
+// rows on 16 requests of up to 8190: 4 x 2 64 us, 8 x 1 74.  With 40 rows there (five drafted tokens): 40 in one tile 119 us, 32
+// 174, 16 175 -- the cache is read once for each tile.
 template <int D, int NT> struct Shape;
-template <> struct Shape<64, 1> { static constexpr int warps = 8, ctas = 2, stages = 6; };
-template <> struct Shape<64, 2> { static constexpr int warps = 8, ctas = 2, stages = 6; };
-template <> struct Shape<128, 1> { static constexpr int warps = 4, ctas = 3, stages = 4; };
-template <> struct Shape<128, 2> { static constexpr int warps = 8, ctas = 1, stages = 6; };
-template <> struct Shape<256, 1> { static constexpr int warps = 8, ctas = 1, stages = 3; };
+template <> struct Shape<64, 1> { static constexpr int warps = 8, ctas = 2, stages = 6; static constexpr bool shared_queries = false; };
+template <> struct Shape<64, 2> { static constexpr int warps = 8, ctas = 2, stages = 6; static constexpr bool shared_queries = false; };
+template <> struct Shape<64, 5> { static constexpr int warps = 8, ctas = 1, stages = 8; static constexpr bool shared_queries = true; };
+template <> struct Shape<128, 1> { static constexpr int warps = 4, ctas = 3, stages = 4; static constexpr bool shared_queries = false; };
+template <> struct Shape<128, 2> { static constexpr int warps = 4, ctas = 2, stages = 6; static constexpr bool shared_queries = false; };
+template <> struct Shape<128, 5> { static constexpr int warps = 8, ctas = 1, stages = 5; static constexpr bool shared_queries = true; };
+template <> struct Shape<256, 1> { static constexpr int warps = 8, ctas = 1, stages = 3; static constexpr bool shared_queries = false; };
+template <> struct Shape<256, 2> { static constexpr int warps = 8, ctas = 1, stages = 3; static constexpr bool shared_queries = true; };
 
 // Units that it costs to begin a job (the chain from the block table to the first tile, the ring that runs dry, the warps'
 // results put together): CTAs that cross from job to job get fewer tokens.  Units are 64 tokens with 4 warps.  Measured 0 / 2 /
@@ -50,8 +55,8 @@ constexpr int kJobCost = 6;
 // The part of a range that is drawn, and the units that it has to have: below that the further partial results cost more
 // than the evener end gives.  10 % of 156 units: 240 -> 226 us; of 37 units (one request of 131071 tokens): 74 -> 86 us.
 constexpr int kTailPercent = 10, kTailMin = 8;
-constexpr int kMaxGrid = 480, kMaxShares = kMaxGrid * 2;
-constexpr int kMaxRows = 16;
+constexpr float kNoRef = -3e38f;                // the reference before the first score: below every one, and finite
+constexpr int kMaxSms = 160, kMaxShares = kMaxSms * 3 * 2;
 
 struct Args {
     fluxbin_kv_cache_t c;
@@ -66,11 +71,20 @@ struct Args {
     float *lse;
     unsigned *drawn;                            // shares drawn so far
     unsigned *arrived;                          // [kMaxShares], by the share in which a cut job begins
-    float *partial_lse;                         // [kMaxShares][2][kMaxRows], base 2
-    float *partial;                             // [kMaxShares][2][rows][D]
+    float *partial_lse;                         // [shares][2][rows], base 2
+    float *partial;                             // [shares][2][rows][D]
 };
 
 // ---- conversions of four 8-bit entries to two pairs of fp16 ---------------------------------------------
+
+// bf16 rows of queries become fp16 exactly, multiplied by the power of two that takes their largest element to 2^14 ..
+// 2^15; elements below 2^-39 of it lose bits that fp32 sums would not keep
+__device__ __forceinline__ int exponent_of(float largest) { return largest > 0.f ? min(max((int)(__float_as_uint(largest) >> 23), 1), 254) - 127 - 14 : 0; }
+__device__ __forceinline__ uint32_t half2_of_bf16(uint32_t w, int e)
+{
+    const __half2 h = __floats2half2_rn(ldexpf(__uint_as_float(w << 16), -e), ldexpf(__uint_as_float(w & 0xffff0000u), -e));
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
 
 template <int FMT> __device__ __forceinline__ void to_half4(uint32_t x, uint32_t &lo, uint32_t &hi);
 // int8: the byte with its sign bit flipped, under the exponent of 1024, is 1024 + 128 + value; fp16 holds that exactly
@@ -154,7 +168,7 @@ template <int ROWS, int kUnit> __device__ __forceinline__ Request request_of(con
 }
 __device__ __forceinline__ long long units_of(const Args &a, const Request &q) { return (long long)q.row_tiles * a.c.kv_heads * (q.pieces + kJobCost); }
 
-template <int D, int ROWS, int WARPS, int STAGES> struct Shared {
+template <int D, int ROWS, int WARPS, int STAGES, bool QSHARED> struct Shared {
     static constexpr int kTile = 32 * D;            // 16 tokens of keys and of values
     union {
         unsigned char ring[WARPS][STAGES][kTile];
@@ -164,6 +178,8 @@ template <int D, int ROWS, int WARPS, int STAGES> struct Shared {
         };
         struct { float join_max[ROWS], join_inv[ROWS], join_lse[ROWS]; };       // after the last part of a cut job
     };
+    uint2 q[QSHARED ? ROWS / 8 : 1][D / 16][32];         // the queries as operands, by lane
+    float factor[ROWS];
     long long scan[WARPS], before;
     int request, last, share;
 };
@@ -176,12 +192,13 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
     constexpr int kWarps = Shape<D, NT>::warps, kThreads = kWarps * 32;
     constexpr int STAGES = Shape<D, NT>::stages;
     constexpr int kUnit = kWarps * 16;           // cached tokens of a unit: 16 for each warp
+    constexpr bool QSHARED = Shape<D, NT>::shared_queries;
     constexpr int KC = D / 64;                   // 64-byte pieces of a key
     constexpr int VW = D >= 128 ? 4 : 2;         // words of a load of values
     constexpr int VC = D / (VW * 32);            // pieces of a value row (eight lanes of VW words each)
     constexpr int MT = D / 16;                   // 16-element tiles of the output
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    Shared<D, ROWS, kWarps, STAGES> &sm = *reinterpret_cast<Shared<D, ROWS, kWarps, STAGES> *>(smem_raw);
+    Shared<D, ROWS, kWarps, STAGES, QSHARED> &sm = *reinterpret_cast<Shared<D, ROWS, kWarps, STAGES, QSHARED> *>(smem_raw);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, lr = lane >> 2, lq = lane & 3;
     const int H = a.c.kv_heads, G = a.q_heads / H, bs = a.c.block_tokens;
 
@@ -306,8 +323,41 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
         }
 
         // ---- the query rows as the 8-column operand: lane (r, q) holds row r, 16 elements of each 64-element piece
-        uint32_t qf[NT][KC * 4][2];
-        float factor[NT][2];
+        uint32_t qf[QSHARED ? 1 : NT][KC * 4][2];
+        float factor[QSHARED ? 1 : NT][2];
+        if constexpr (QSHARED) {
+            // a warp takes every kWarps-th row, a lane four elements at a time
+            for (int row = warp; row < ROWS; row += kWarps) {
+                const bool live = row < rows;
+                const int g = row0 + (live ? row : 0);
+                const T *qp = (const T *)a.q + (rq.first + g / G) * a.q_token + (h * G + g % G) * a.q_head;
+                uint2 w[(D + 127) / 128];
+                float largest = 0.f;
+#pragma unroll
+                for (int i = 0; i < (D + 127) / 128; ++i) {
+                    w[i] = live && i * 128 + lane * 4 < D ? *reinterpret_cast<const uint2 *>(qp + i * 128 + lane * 4) : make_uint2(0, 0);
+                    if constexpr (!std::is_same<T, __half>::value)
+                        largest = fmaxf(largest, fmaxf(fmaxf(fabsf(__uint_as_float(w[i].x << 16)), fabsf(__uint_as_float(w[i].x & 0xffff0000u))),
+                                                       fmaxf(fabsf(__uint_as_float(w[i].y << 16)), fabsf(__uint_as_float(w[i].y & 0xffff0000u)))));
+                }
+                float f = a.scale * 1.4426950408889634f;
+                if constexpr (!std::is_same<T, __half>::value) {
+#pragma unroll
+                    for (int x = 16; x; x >>= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, x));
+                    const int e = exponent_of(largest);
+#pragma unroll
+                    for (int i = 0; i < (D + 127) / 128; ++i) w[i] = make_uint2(half2_of_bf16(w[i].x, e), half2_of_bf16(w[i].y, e));
+                    f = ldexpf(f, e);
+                }
+#pragma unroll
+                for (int i = 0; i < (D + 127) / 128; ++i) {
+                    const int d = i * 128 + lane * 4;
+                    if (d < D) sm.q[row / 8][d / 64 * 4 + d % 16 / 4][row % 8 * 4 + d % 64 / 16] = w[i];
+                }
+                if (lane == 0) sm.factor[row] = f;
+            }
+            __syncthreads();
+        } else {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int row = row0 + t * 8 + lr;
@@ -333,16 +383,13 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
             }
             float f = 1.f;
             if constexpr (!std::is_same<T, __half>::value) {
-                // bf16 rows become fp16 exactly, multiplied by the power of two that takes their largest element to
-                // 2^14 .. 2^15; elements below 2^-39 of it lose bits that fp32 sums would not keep
                 largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, 1));
                 largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, 2));
-                const int e = largest > 0.f ? min(max((int)(__float_as_uint(largest) >> 23), 1), 254) - 127 - 14 : 0;
+                const int e = exponent_of(largest);
 #pragma unroll
                 for (int i = 0; i < KC * 4; ++i)
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)
-                        qf[t][i][k] = pack_half2(ldexpf(__uint_as_float(qf[t][i][k] << 16), -e), ldexpf(__uint_as_float(qf[t][i][k] & 0xffff0000u), -e));
+                    for (int k = 0; k < 2; ++k) qf[t][i][k] = half2_of_bf16(qf[t][i][k], e);
                 f = ldexpf(a.scale * 1.4426950408889634f, e);
             } else {
                 f = a.scale * 1.4426950408889634f;
@@ -351,14 +398,14 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
 #pragma unroll
             for (int e = 0; e < 2; ++e) factor[t][e] = __shfl_sync(0xffffffffu, f, (2 * lq + e) * 4);
         }
+        }
 
-        float o[NT][MT][4], ref[NT][2], top[NT][2], sum[NT][2], vref = 0.f, vref_inverse = 0.f;
+        float o[NT][MT][4], ref[NT][2], sum[NT][2], vref = 0.f, vref_inverse = 0.f;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
             for (int i = 0; i < MT; ++i) o[t][i][0] = o[t][i][1] = o[t][i][2] = o[t][i][3] = 0.f;
-            ref[t][0] = ref[t][1] = 0.f;                 // the reference, and what a score may not pass against it
-            top[t][0] = top[t][1] = -INFINITY;
+            ref[t][0] = ref[t][1] = kNoRef;
             sum[t][0] = sum[t][1] = 0.f;
         }
 
@@ -384,11 +431,11 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
                 for (int c = 0; c < KC; ++c) kw[i][c] = take<4>(k_ring + stage * (32 * D) + (i * KC + c) * 512);
             // ---- scores
             // (two chains of products, so that one is issued while the other's last is under way)
-            float s[NT][4], s2[NT][4];
+            float s[NT][4], s2[QSHARED ? 1 : NT][4];
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[t][e] = s2[t][e] = 0.f;
+                for (int e = 0; e < 4; ++e) s[t][e] = s2[QSHARED ? 0 : t][e] = 0.f;
 #pragma unroll
             for (int c = 0; c < KC; ++c)
 #pragma unroll
@@ -397,7 +444,12 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
                     to_half4<FMT>(kw[0][c].w[w], a0, a2);
                     to_half4<FMT>(kw[1][c].w[w], a1, a3);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) mma(w & 1 ? s2[t] : s[t], a0, a1, a2, a3, qf[t][c * 4 + w][0], qf[t][c * 4 + w][1]);
+                    for (int t = 0; t < NT; ++t) {
+                        uint2 b;
+                        if constexpr (QSHARED) b = sm.q[t][c * 4 + w][lane];
+                        else b = make_uint2(qf[t][c * 4 + w][0], qf[t][c * 4 + w][1]);
+                        mma(!QSHARED && (w & 1) ? s2[QSHARED ? 0 : t] : s[t], a0, a1, a2, a3, b.x, b.y);
+                    }
                 }
             // ---- softmax against a lagging reference
             bool above = false;
@@ -405,7 +457,10 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[t][e] = (s[t][e] + s2[t][e]) * (factor[t][e & 1] * ks);
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (QSHARED) s[t][e] *= sm.factor[t * 8 + 2 * lq + (e & 1)] * ks;
+                    else s[t][e] = (s[t][e] + s2[t][e]) * (factor[t][e & 1] * ks);
+                }
             if (edge) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
@@ -416,7 +471,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) above |= s[t][e] > top[t][e & 1];
+                for (int e = 0; e < 4; ++e) above |= s[t][e] > ref[t][e & 1] + 15.f;
             if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
@@ -426,10 +481,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16)) - 7.f;
-                        if (m > top[t][e] - 15.f) {
-                            const float f = top[t][e] == -INFINITY ? 0.f : exp2_fast(ref[t][e] - m);
+                        if (m > ref[t][e]) {
+                            const float f = exp2_fast(ref[t][e] - m);
                             ref[t][e] = m;
-                            top[t][e] = m + 15.f;
                             sum[t][e] *= f;
 #pragma unroll
                             for (int i = 0; i < MT; ++i) { o[t][i][e] *= f; o[t][i][e + 2] *= f; }
@@ -506,7 +560,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
                 l += __shfl_xor_sync(0xffffffffu, l, 8);
                 l += __shfl_xor_sync(0xffffffffu, l, 16);
                 const int row = t * 8 + 2 * lq + e;
-                if (lr == 0) { sm.m[warp][row] = top[t][e] == -INFINITY ? -INFINITY : ref[t][e]; sm.l[warp][row] = l; }
+                if (lr == 0) { sm.m[warp][row] = ref[t][e]; sm.l[warp][row] = l; }
 #pragma unroll
                 for (int c = 0; c < VC; ++c)
 #pragma unroll
@@ -518,7 +572,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
         __syncthreads();
         const bool whole = p0 == 0 && p1 == rq.pieces;
         const int first_cta_slot = p0 == 0;                  // this job begins here, or goes on from the CTA before
-        float *part = a.partial + (share * 2 + first_cta_slot) * ROWS * D, *part_lse = a.partial_lse + (share * 2 + first_cta_slot) * kMaxRows;
+        float *part = a.partial + (share * 2 + first_cta_slot) * ROWS * D, *part_lse = a.partial_lse + (share * 2 + first_cta_slot) * ROWS;
         auto write_out = [&](int row, int d, float4 v, float lse2) {
             const int g = row0 + row;
             const long long tok = rq.first + g / G;
@@ -534,10 +588,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) m = fmaxf(m, sm.m[w][row]);
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            const float m_safe = m == -INFINITY ? 0.f : m;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {           // a warp without tokens has l = 0; a NaN in l stays
-                const float f = sm.l[w][row] == 0.f ? 0.f : exp2_fast(sm.m[w][row] - m_safe), fv = f * sm.v[w];
+                const float f = sm.l[w][row] == 0.f ? 0.f : exp2_fast(sm.m[w][row] - m), fv = f * sm.v[w];
                 const float4 x = *reinterpret_cast<const float4 *>(&sm.o[w][row][d]);
                 l += f * sm.l[w][row];
                 if (f != 0.f) { v.x += fv * x.x; v.y += fv * x.y; v.z += fv * x.z; v.w += fv * x.w; }
@@ -565,7 +618,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
                 for (int row = warp; row < rows; row += kWarps) {
                     float m = -INFINITY, l = 0.f;
                     for (int c = lane; c < parts; c += 32) {
-                        const float x = __ldcg(a.partial_lse + slot_of(c) * kMaxRows + row), m_now = fmaxf(m, x);
+                        const float x = __ldcg(a.partial_lse + slot_of(c) * ROWS + row), m_now = fmaxf(m, x);
                         l = l * (m == -INFINITY ? 0.f : exp2_fast(m - m_now)) + (x == -INFINITY ? 0.f : exp2_fast(x - m_now));
                         m = m_now;
                     }
@@ -589,7 +642,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
 #pragma unroll
                     for (int k = 0; k < kEach; ++k) {
                         const int i = min(tid + k * kThreads, kItems - 1), row = i / (D / 4);
-                        const float f = exp2_fast(__ldcg(a.partial_lse + slot_of(c) * kMaxRows + row) - sm.join_max[row]);
+                        const float f = exp2_fast(__ldcg(a.partial_lse + slot_of(c) * ROWS + row) - sm.join_max[row]);
                         const float4 y = __ldcg(reinterpret_cast<const float4 *>(a.partial + slot_of(c) * (ROWS * D)) + i);
                         v[k].x += f * y.x; v[k].y += f * y.y; v[k].z += f * y.z; v[k].w += f * y.w;
                     }
@@ -630,7 +683,7 @@ int num_sms()
 template <int D, int FMT, int NT, typename T>
 cudaError_t run(const Args &a, cudaStream_t s)
 {
-    const size_t smem = sizeof(Shared<D, 8 * NT, Shape<D, NT>::warps, Shape<D, NT>::stages>);
+    const size_t smem = sizeof(Shared<D, 8 * NT, Shape<D, NT>::warps, Shape<D, NT>::stages, Shape<D, NT>::shared_queries>);
     static std::atomic<bool> opted[fb::kMaxDevices];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -643,16 +696,17 @@ cudaError_t run(const Args &a, cudaStream_t s)
     }
     const int sms = num_sms();
     if (sms == 0) return cudaErrorInvalidDevice;
-    const int grid = sms * Shape<D, NT>::ctas;
-    return launch(attend_kernel<D, FMT, NT, T>, dim3((unsigned)(grid < kMaxGrid ? grid : kMaxGrid)), Shape<D, NT>::warps * 32, smem, s, a);
+    const int grid = (sms < kMaxSms ? sms : kMaxSms) * Shape<D, NT>::ctas;
+    return launch(attend_kernel<D, FMT, NT, T>, dim3((unsigned)grid), Shape<D, NT>::warps * 32, smem, s, a);
 }
 template <int D, int FMT, typename T> cudaError_t run_rows(const Args &a, cudaStream_t s)
 {
     // rows that share a key head in an average request
     const long long rows = (long long)(a.q_heads / a.c.kv_heads) * ((a.tokens + a.batch - 1) / a.batch);
     if constexpr (D != 256) {
-        if (rows > 8) return run<D, FMT, 2, T>(a, s);
+        if (rows > 16) return run<D, FMT, 5, T>(a, s);
     }
+    if (rows > 8) return run<D, FMT, 2, T>(a, s);
     return run<D, FMT, 1, T>(a, s);
 }
 template <int D, typename T> cudaError_t run_format(const Args &a, cudaStream_t s)
@@ -664,7 +718,9 @@ template <typename T> cudaError_t run_dim(const Args &a, cudaStream_t s)
     return a.c.head_dim == 64 ? run_format<64, T>(a, s) : a.c.head_dim == 128 ? run_format<128, T>(a, s) : run_format<256, T>(a, s);
 }
 
-constexpr size_t kCounterBytes = ((1 + kMaxShares) * sizeof(unsigned) + 255) / 256 * 256, kLseBytes = (size_t)kMaxShares * 2 * kMaxRows * sizeof(float);
+constexpr size_t kCounterBytes = ((1 + kMaxShares) * sizeof(unsigned) + 255) / 256 * 256;
+// the most rows that partial results of a launch take: those of the CTAs on an SM, two shares each, two parts a share
+constexpr size_t kPartRows = (size_t)kMaxSms * 40 * 2 * 2, kLseBytes = kPartRows * sizeof(float);
 
 } // namespace
 
