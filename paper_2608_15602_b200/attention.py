@@ -263,3 +263,35 @@ class BlockTables:
         step.pointers = tuple(first + 4 * sum(sizes[:i]) for i in range(7))
         step.first, step.last = first, first + 4 * sum(sizes)
         return step
+
+
+class AttentionBlock:
+    """The attention block of a decoder layer on packed linears: q/k/v projections, positions, cache, attention, output
+    projection.  `q`, `k`, `v`, `o` are FluxBinLinear layers; the cache and the block tables may serve a whole batch of requests."""
+
+    def __init__(self, q, k, v, o, cache: KVCache, rotary: Rotary):
+        D = cache.head_dim
+        if k.M != cache.kv_heads * D or v.M != k.M or q.M % k.M or o.N != q.M or not q.N == k.N == v.N == o.M:
+            raise ValueError("the layers do not fit the cache's heads and each other")
+        self.q, self.k, self.v, self.o, self.cache, self.rotary, self.q_heads = q, k, v, o, cache, rotary, q.M // D
+
+    def buffers(self, batch: int, tokens: int) -> SimpleNamespace:
+        """What forward() works in for up to `tokens` new tokens of `batch` requests, and its input x [tokens][hidden]
+        and output y: q, k and v run as one plan, so the buffers are theirs."""
+        from .layer import FluxBinPlan
+        new = lambda n: torch.empty((tokens, n), dtype=torch.float16, device=self.cache.device)  # noqa: E731
+        b = SimpleNamespace(x=new(self.q.N), q=new(self.q.M), k=new(self.k.M), v=new(self.v.M), a=new(self.q.M), y=new(self.o.M))
+        b.plan = FluxBinPlan([(self.q, b.x, b.q), (self.k, b.x, b.k), (self.v, b.x, b.v)], device=self.cache.device)
+        b.linear_ws, b.ws = self.o.workspace(tokens), self.cache.workspace(batch, tokens, self.q_heads)
+        return b
+
+    def forward(self, b: SimpleNamespace, tables: BlockTables, step: SimpleNamespace, stream=None) -> torch.Tensor:
+        """y = o(attention(x)) for the new tokens of `step` (BlockTables.advance) in b.x; the result is b.y.  Three launches
+        besides the output projection, nothing allocated: a decode step can be captured into a graph."""
+        n, D = b.x.shape[0], self.cache.head_dim
+        b.plan.run(stream)
+        q, a = b.q.view(n, self.q_heads, D), b.a.view(n, self.q_heads, D)
+        k, v = b.k.view(n, -1, D), b.v.view(n, -1, D)
+        self.cache.append(k, v, step.slots, rotary=self.rotary, positions=step.positions, q=q, q_out=q, stream=stream)
+        self.cache.attend(q, tables.table, step.lengths, b.ws, query_start=step.query_start, out=a, stream=stream)
+        return self.o.forward(b.a, b.linear_ws, out=b.y, stream=stream)
