@@ -573,7 +573,7 @@ fluxbin_status_t fluxbin_kv_read(const fluxbin_kv_cache_t *cache, int32_t dtype,
  *                   query_start[r + 1] - 1 of q, which are its last ones (already appended).  NULL: one token a request
  *                   (tokens == batch).  Entries are clamped to [0, tokens].
  *   d_lengths       DEVICE int32 [batch]: cached tokens of each request, the new ones included.  0 (or less) leaves the
- *                   request's rows empty; a length past block_table_width * block_tokens is cut to that.
+ *                   request's rows empty; a length past block_table_width * block_tokens, or 2^31 - 4096, is cut to that.
  *   d_block_table   DEVICE int32 [batch][block_table_stride]: block of tokens 0.., block_tokens.., ...; entries past the
  *                   length are not read; tokens of a block id outside the cache are masked out.
  *   d_q, d_out      fp16 or bf16 heads; 16-byte aligned, strides multiples of 8 elements
@@ -581,10 +581,12 @@ fluxbin_status_t fluxbin_kv_read(const fluxbin_kv_cache_t *cache, int32_t dtype,
  * A row that sees nothing gets out = 0 and lse = -inf.  What lies in the cache past a request's length (NaN patterns
  * included) has no influence.  Scores, maxima, sums and accumulators are fp32; the probabilities of a step and the
  * 8-bit entries enter the matrix instructions as fp16 (8-bit entries exactly).  Results do not depend on timing: sums
- * are joined in a fixed order.
- * d_workspace: fluxbin_kv_attend_workspace_size bytes, zeroed once with fluxbin_workspace_init; calls leave its counters
- * zeroed, and calls that share one must be ordered on a stream.
- * Errors: as fluxbin_kv_validate; NULL, RANGE (q_heads no multiple of kv_heads, tokens != batch without query_start),
+ * are joined in a fixed order (which depends on the lengths of the whole batch).
+ * d_workspace: fluxbin_kv_attend_workspace_size bytes (13 MB at head_dim 128: the partial results of jobs that several CTAs
+ * work at; it depends on head_dim alone, so one serves all calls), zeroed once with fluxbin_workspace_init; calls leave its
+ * counters zeroed, and calls that share one must be ordered on a stream.
+ * Errors: as fluxbin_kv_validate; NULL, RANGE (q_heads no multiple of kv_heads, tokens != batch without query_start, 2^31
+ * rows or more for a key head),
  * UNSUPPORTED (dtype), ALIGNMENT, BUFFER_TOO_SMALL, CUDA.
  */
 size_t fluxbin_kv_attend_workspace_size(int32_t batch, int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim);

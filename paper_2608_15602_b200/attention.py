@@ -27,15 +27,18 @@ _KINDS = {"none": fluxbin.ROPE_NONE, "linear": fluxbin.ROPE_LINEAR, "base": flux
           "bands": fluxbin.ROPE_BANDS}
 
 
-def _stream(x: torch.Tensor, stream) -> int:
-    """The raw stream of a call: `stream`, or the current one of the tensor's device."""
-    return torch._C._cuda_getCurrentRawStream(x.device.index) if stream is None else _stream_ptr(stream)
+_device = torch._C._cuda_getDevice               # the current device: every tensor of a call has to lie on it
+
+
+def _stream(stream) -> int:
+    """The raw stream of a call: `stream`, or the current one."""
+    return torch._C._cuda_getCurrentRawStream(_device()) if stream is None else _stream_ptr(stream)
 
 
 def _heads(x: torch.Tensor, tokens: int, dim: int, dtype: torch.dtype, what: str):
     """(pointer, heads, token stride, head stride) of a [tokens][heads][dim] tensor with contiguous heads."""
-    if x.dtype is not dtype or x.dim() != 3 or not x.is_cuda:
-        raise TypeError(f"{what}: a CUDA tensor [tokens][heads][dim] of {dtype} is wanted")
+    if x.dtype is not dtype or x.dim() != 3 or x.get_device() != _device():
+        raise TypeError(f"{what}: a tensor [tokens][heads][dim] of {dtype} on the current CUDA device is wanted")
     t, h, d = x.shape
     if t != tokens or d != dim:
         raise ValueError(f"{what}: shape {tuple(x.shape)}, wanted [{tokens}][heads][{dim}]")
@@ -46,14 +49,18 @@ def _heads(x: torch.Tensor, tokens: int, dim: int, dtype: torch.dtype, what: str
 
 
 def _int32(x: torch.Tensor, n: int, what: str) -> int:
-    if x.dtype is not torch.int32 or not x.is_cuda or x.shape != (n,) or (n > 1 and x.stride(0) != 1):
-        raise ValueError(f"{what}: a contiguous CUDA int32 tensor of {n} elements is wanted")
+    if x.dtype is not torch.int32 or x.get_device() != _device() or x.shape != (n,) or (n > 1 and x.stride(0) != 1):
+        raise ValueError(f"{what}: a contiguous int32 tensor of {n} elements on the current CUDA device is wanted")
     return x.data_ptr()
 
 
-def _output(given: torch.Tensor | None, like: torch.Tensor, heads: int, what: str):
+def _output(given: torch.Tensor | None, like: torch.Tensor, heads: int, what: str, stream):
     """An output like a [tokens][heads][dim] input: (tensor, pointer, token stride, head stride)."""
-    y = torch.empty_like(like) if given is None else given
+    y = given
+    if y is None:
+        y = torch.empty_like(like)
+        if stream is not None:                   # made on the current stream, written on another
+            y.record_stream(stream)
     p, h, st, sh = _heads(y, like.shape[0], like.shape[2], like.dtype, what)
     if h != heads:
         raise ValueError(f"{what}: {heads} heads are wanted")
@@ -87,16 +94,18 @@ class Rotary:
         n, dt = q.shape[0], q.dtype
         if dt not in _TYPES:
             raise TypeError("q: fp16, bf16 or fp32 is wanted")
+        if self.turns.get_device() != _device():
+            raise ValueError("the frequencies have to lie on the current CUDA device")
         qp, qh, qt, qs = _heads(q, n, self.head_dim, dt, "q")
-        q_out, op, ot, os_ = _output(q_out, q, qh, "q_out")
+        q_out, op, ot, os_ = _output(q_out, q, qh, "q_out", stream)
         kp = kh = kt = ks = kop = kot = kos = 0
         if k is None:
             k_out = None
         else:
             kp, kh, kt, ks = _heads(k, n, self.head_dim, dt, "k")
-            k_out, kop, kot, kos = _output(k_out, k, kh, "k_out")
+            k_out, kop, kot, kos = _output(k_out, k, kh, "k_out", stream)
         fluxbin.rotary_call(self._ref, _TYPES[dt], inverse, n, _int32(positions, n, "positions"), qp, qh, qt, qs, op, ot, os_,
-                            kp, kh, kt, ks, kop, kot, kos, _stream(q, stream))
+                            kp, kh, kt, ks, kop, kot, kos, _stream(stream))
         return q_out, k_out
 
 
@@ -145,20 +154,25 @@ class KVCache:
         if status:
             raise fluxbin.FluxBinError(status, "fluxbin_kv_validate")
 
-    def _new(self, shape: tuple, dtype: torch.dtype) -> torch.Tensor:
+    def _new(self, shape: tuple, dtype: torch.dtype, stream) -> torch.Tensor:
         """torch.empty(shape, dtype) on the cache's device; made like the last (small) one of that kind it takes half the time."""
-        if math.prod(shape) > 1 << 16:
-            return torch.empty(shape, dtype=dtype, device=self.device)
         last = self._last.get(dtype)
         if last is None or last.shape != shape:
-            last = self._last[dtype] = torch.empty(shape, dtype=dtype, device=self.device)
-        return torch.empty_like(last)
+            last = torch.empty(shape, dtype=dtype, device=self.device)
+            if last.numel() <= 1 << 16:
+                self._last[dtype] = last
+        new = torch.empty_like(last)
+        if stream is not None:
+            new.record_stream(stream)
+        return new
 
     def append(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, rotary: Rotary | None = None,
                positions: torch.Tensor | None = None, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None, stream=None):
         """fluxbin_kv_append: quantise and store k, v [tokens][kv_heads][head_dim] at `slots` [tokens] (int32).  With `rotary` the
         keys, and the q heads if given, are turned to `positions` on the way; returns the turned q (else None)."""
         n, dt = k.shape[0], k.dtype
+        if self.k.get_device() != _device():
+            raise ValueError("the cache has to lie on the current CUDA device")
         if dt not in _TYPES:
             raise TypeError("k: fp16, bf16 or fp32 is wanted")
         kp, kh, kt, ks = _heads(k, n, self.head_dim, dt, "k")
@@ -169,23 +183,27 @@ class KVCache:
         if rotary is not None:
             if positions is None:
                 raise ValueError("positions are wanted with rotary")
+            if rotary.turns.get_device() != _device():
+                raise ValueError("rotary: the frequencies have to lie on the current CUDA device")
             rp, pp = rotary._ref, _int32(positions, n, "positions")
             if q is not None:
                 qp, qh, qt, qs = _heads(q, n, self.head_dim, dt, "q")
-                q_out, op, ot, os_ = _output(q_out, q, qh, "q_out")
+                q_out, op, ot, os_ = _output(q_out, q, qh, "q_out", stream)
         elif q is not None:
             raise ValueError("q is only turned with rotary")
         fluxbin.kv_append_call(self._ref, _TYPES[dt], n, _int32(slots, n, "slots"), kp, kt, ks, vp, vt, vs, rp, pp, qp, qh, qt, qs,
-                               op, ot, os_, _stream(k, stream))
+                               op, ot, os_, _stream(stream))
         return None if q is None else q_out
 
     def read(self, slots: torch.Tensor, dtype: torch.dtype = torch.float16, stream=None):
         """fluxbin_kv_read: the keys and values that the entries at `slots` stand for, two [tokens][kv_heads][head_dim] tensors."""
         if dtype not in _TYPES:
             raise TypeError("dtype: fp16, bf16 or fp32 is wanted")
+        if self.k.get_device() != _device():
+            raise ValueError("the cache has to lie on the current CUDA device")
         n = slots.shape[0]
-        k, v = self._new((2, n, self.kv_heads, self.head_dim), dtype).unbind()
-        fluxbin.kv_read_call(self._ref, _TYPES[dtype], n, _int32(slots, n, "slots"), k.data_ptr(), v.data_ptr(), _stream(slots, stream))
+        k, v = self._new((2, n, self.kv_heads, self.head_dim), dtype, stream).unbind()
+        fluxbin.kv_read_call(self._ref, _TYPES[dtype], n, _int32(slots, n, "slots"), k.data_ptr(), v.data_ptr(), _stream(stream))
         return k, v
 
     def workspace(self, batch: int, tokens: int, q_heads: int) -> Workspace:
@@ -206,15 +224,17 @@ class KVCache:
         if dt is not torch.float16 and dt is not torch.bfloat16:
             raise TypeError("q: fp16 or bf16 is wanted")
         qp, qh, qt, qs = _heads(q, n, self.head_dim, dt, "q")
-        if table.dtype is not torch.int32 or table.dim() != 2 or not table.is_cuda or (table.shape[1] > 1 and table.stride(1) != 1):
-            raise ValueError("table: a CUDA int32 tensor [batch][max_blocks] with contiguous rows is wanted")
+        if table.dtype is not torch.int32 or table.dim() != 2 or table.get_device() != _device() or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("table: an int32 tensor [batch][max_blocks] with contiguous rows on the current CUDA device is wanted")
+        if self.k.get_device() != _device():
+            raise ValueError("the cache has to lie on the current CUDA device")
         B, width = table.shape
-        out, op, ot, os_ = _output(out, q, qh, "out")
-        lse = self._new((n, qh), torch.float32) if with_lse else None
+        out, op, ot, os_ = _output(out, q, qh, "out", stream)
+        lse = self._new((n, qh), torch.float32, stream) if with_lse else None
         fluxbin.kv_attend_call(self._ref, _TYPES[dt], B, n, qp, qh, qt, qs, 0 if query_start is None else _int32(query_start, B + 1, "query_start"),
                                _int32(lengths, B, "lengths"), table.data_ptr(), max(table.stride(0), width), width,
                                self._scale if scale is None else scale, op, ot, os_, 0 if lse is None else lse.data_ptr(), ws.tensor.data_ptr(),
-                               ws.nbytes, _stream(q, stream))
+                               ws.nbytes, _stream(stream))
         return (out, lse) if with_lse else out
 
 
@@ -245,13 +265,15 @@ class BlockTables:
         sets in turn, so that a step's outputs can be the next step's inputs; keep a copy of what has to live longer."""
         B = self.batch
         lp, np_, fp = _int32(lengths, B, "lengths"), _int32(new_tokens, B, "new_tokens"), _int32(num_free, 1, "num_free")
+        if self.table.get_device() != _device():
+            raise ValueError("the tables have to lie on the current CUDA device")
         if tokens != self._tokens:                       # (a decode loop keeps one size)
             self._tokens, self._sets = tokens, [self._outputs(tokens), self._outputs(tokens)]
         step, other = self._sets
         self._sets = [other, step]
         if step.first <= lp < step.last or step.first <= np_ < step.last or step.first <= fp < step.last:
             step = self._sets[1] = self._outputs(tokens)  # an input of this step is an output of the last but one: keep that
-        fluxbin.kv_advance_call(B, tokens, self.block_tokens, lp, np_, *self._args, fp, *step.pointers, _stream(self.table, stream))
+        fluxbin.kv_advance_call(B, tokens, self.block_tokens, lp, np_, *self._args, fp, *step.pointers, _stream(stream))
         return step
 
     def _outputs(self, tokens: int) -> SimpleNamespace:

@@ -55,6 +55,7 @@ constexpr int kJobCost = 6;
 // The part of a range that is drawn, and the units that it has to have: below that the further partial results cost more
 // than the evener end gives.  10 % of 156 units: 240 -> 226 us; of 37 units (one request of 131071 tokens): 74 -> 86 us.
 constexpr int kTailPercent = 10, kTailMin = 8;
+constexpr int kMaxLength = INT32_MAX - 4095;    // rounded up to units it is still an int
 constexpr float kNoRef = -3e38f;                // the reference before the first score: below every one, and finite
 constexpr int kMaxSms = 160, kMaxShares = kMaxSms * 3 * 2;
 
@@ -161,7 +162,7 @@ template <int ROWS, int kUnit> __device__ __forceinline__ Request request_of(con
         q.first = r;
         q.count = 1;
     }
-    q.length = (int)min((long long)max(a.lengths[r], 0), (long long)a.width * a.c.block_tokens);
+    q.length = (int)min((long long)min(max(a.lengths[r], 0), kMaxLength), (long long)a.width * a.c.block_tokens);
     q.row_tiles = (int)(((long long)q.count * (a.q_heads / a.c.kv_heads) + ROWS - 1) / ROWS);
     q.pieces = max((q.length + kUnit - 1) / kUnit, 1);          // an empty request still has rows to write
     return q;
@@ -741,7 +742,8 @@ extern "C" fluxbin_status_t fluxbin_kv_attend(const fluxbin_kv_cache_t *cache, i
     if (st != FLUXBIN_OK) return st;
     if (dtype != FLUXBIN_TYPE_FP16 && dtype != FLUXBIN_TYPE_BF16) return FLUXBIN_ERR_UNSUPPORTED;
     if (batch < 1 || tokens < 0 || q_heads < 1 || q_heads > 65535 || q_heads % cache->kv_heads != 0 || block_table_width < 1 ||
-        block_table_stride < block_table_width || (!d_query_start && tokens != batch)) return FLUXBIN_ERR_RANGE;
+        block_table_stride < block_table_width || (!d_query_start && tokens != batch) ||
+        (int64_t)tokens * (q_heads / cache->kv_heads) > INT32_MAX) return FLUXBIN_ERR_RANGE;
     if (tokens == 0) return FLUXBIN_OK;
     if (!d_q || !d_out || !d_lengths || !d_block_table || !d_workspace) return FLUXBIN_ERR_NULL;
     if (!aligned_to(d_q, 16) || !aligned_to(d_out, 16) || q_token % 8 || q_head % 8 || out_token % 8 || out_head % 8 ||
