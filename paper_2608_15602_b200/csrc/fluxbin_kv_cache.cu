@@ -109,6 +109,8 @@ __global__ void append_any_kernel(fluxbin_kv_cache_t c, int tokens, const int *s
 // is stored; both halves of the work read the values once, into registers.
 //   short runs (a decode step: one token a run): a warp per head, half its lanes the keys, half the values;
 //   long runs (a prompt: whole blocks): the CTA on one head at a time, four pieces of eight elements a thread and pass.
+//   Bound by latency, not by bytes: three CTAs on an SM (80 registers) 43 us for 9 K tokens of 8 heads, two 53, one that has
+//   the next head's loads under way (204 registers) 72.
 // Keys are turned in fp32 on the way; the angles of a run's tokens are formed once for all heads of the CTA.  The q heads of
 // the same tokens are turned by CTAs of the same launch.
 
@@ -218,7 +220,7 @@ struct AppendArgs {
 };
 
 template <typename T, int FMT, int D, bool ROT>
-__global__ void __launch_bounds__(kWide) append_kernel(const __grid_constant__ AppendArgs a)
+__global__ void __launch_bounds__(kWide, D == 256 ? 2 : 3) append_kernel(const __grid_constant__ AppendArgs a)
 {
     constexpr int PIECES = D / 8;                // of eight elements
     constexpr int AT_ONCE = kWide / PIECES;      // tokens a pass has side by side

@@ -49,31 +49,113 @@ extern "C" fluxbin_status_t fluxbin_rotary_frequencies(int32_t rotary_dim, doubl
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kCtas = 148 * 3;                   // that are resident at once
+constexpr int kCtas = 148 * 4;                   // of a prompt: those that are resident at once
 
-// A CTA takes a token at a time, or a group of its heads where there are few tokens: the angles of a token are formed once
-// and serve all its heads, while the first heads are on their way.  Bound by memory for prompts, by its launch and two
-// dependent accesses for decode steps.  Prompts: the CTAs that are resident go over the tokens, so that what a thread
-// works out about its place is worked out once (8191 tokens of 80 heads: 71 us; a CTA a token 78; the angles of two or four
-// tokens behind one barrier 80).
+// Few tokens, or accesses of single elements: a CTA takes a token, or a group of its heads.  Bound by its launch and two
+// dependent accesses.
 template <typename T, int VE, bool INTER>
-__global__ void __launch_bounds__(kThreads, 3) rotary_kernel(const __grid_constant__ fluxbin_rotary_t rot, float sign, int tokens, const int *positions,
+__global__ void __launch_bounds__(kThreads, 3) rotary_kernel(const __grid_constant__ fluxbin_rotary_t rot, float sign, const int *positions,
                                                              const __grid_constant__ Side q, const __grid_constant__ Side k, int heads_each)
 {
+    __shared__ float2 angles[kMaxPairs];
+    let_successor_start();
+    wait_for_predecessor();
+    const int t = blockIdx.x, h0 = blockIdx.y * heads_each, h1 = min(h0 + heads_each, q.heads + k.heads);
+    turn_heads<T, VE, INTER>(rot, angles, q, k, t, h0, h1, threadIdx.x, kThreads, [&]() {
+        token_angles(rot, positions[t], sign, angles, threadIdx.x, kThreads);
+        __syncthreads();
+    });
+}
+
+// Prompts, 16-byte accesses: the CTAs that are resident go over the tokens, all heads of a token at a time, so that what a
+// thread works out about its place is worked out once.  The angles of a token are formed while its first heads are on
+// their way.  Bound by memory and, nearly as much, by instructions (two conversions, two products and two sums a pair).
+// 8191 tokens of 80 heads, half of each turned: 57 us (5.9 TB/s); three CTAs on an SM 62, a CTA a token that works its place
+// out again 71 to 78.  Whole heads in halves (two accesses each): one head under way at a time 65 us for 9216 tokens of 72
+// heads, two 67.
+template <typename T, int VE, bool INTER>
+__global__ void __launch_bounds__(kThreads, 4) rotary_prompt_kernel(const __grid_constant__ fluxbin_rotary_t rot, float sign, int tokens, const int *positions,
+                                                                    const __grid_constant__ Side q, const __grid_constant__ Side k)
+{
+    constexpr int NA = INTER ? VE / 2 : VE, BATCH = INTER ? 4 : 1;
     __shared__ float2 angles[2][kMaxPairs];
     let_successor_start();
     wait_for_predecessor();
-    const int h0 = blockIdx.y * heads_each, h1 = min(h0 + heads_each, q.heads + k.heads);
+    const int half = rot.rotary_dim / 2, turning = half / NA, units = turning + (rot.head_dim - rot.rotary_dim) / VE, rows = kThreads / units;
+    const int u = threadIdx.x % units, row = threadIdx.x / units, e0 = u < turning ? u * (INTER ? VE : NA) : rot.rotary_dim + (u - turning) * VE;
+    const bool turns = u < turning;
+    Elements<T, VE> a[BATCH], b[BATCH];
+    float c[NA], s[NA];
+    // `left` heads, one in every `rows`, from x to y; the first of them may be loaded already
+    auto heads = [&](const T *x, T *y, long long xs, long long ys, int left, bool copies, bool loaded) {
+        for (; left > 0; left -= BATCH) {
+            if (!loaded) {
+#pragma unroll
+                for (int j = 0; j < BATCH; ++j)
+                    if (j < left) {
+                        a[j].load(x + j * xs, VE);
+                        if (!INTER && turns) b[j].load(x + j * xs + half, VE);
+                    }
+            }
+            loaded = false;
+            x += BATCH * xs;
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j, y += ys) {
+                if (j >= left) break;
+                if (!turns) {
+                    if (copies) a[j].store(y, VE);
+                    continue;
+                }
+                float f[NA], g[NA];
+#pragma unroll
+                for (int i = 0; i < NA; ++i)
+                    turn_pair(to_float(a[j].e[INTER ? 2 * i : i]), to_float(INTER ? a[j].e[INTER ? 2 * i + 1 : 0] : b[j].e[i]), c[i], s[i], f[i], g[i]);
+                if constexpr (INTER) {
+#pragma unroll
+                    for (int i = 0; i < NA; ++i) a[j].set(2 * i, f[i], g[i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < NA; i += 2) {
+                        a[j].set(i, f[i], f[i + 1]);
+                        b[j].set(i, g[i], g[i + 1]);
+                    }
+                    b[j].store(y + half, VE);
+                }
+                a[j].store(y, VE);
+            }
+        }
+    };
+    const int nq = row < rows && row < q.heads ? (q.heads - row + rows - 1) / rows : 0, nk = row < rows && row < k.heads ? (k.heads - row + rows - 1) / rows : 0;
+    const bool q_copies = q.in != q.out, k_copies = k.in != k.out;
+    const long long qs = rows * q.in_head, qos = rows * q.out_head, ks = rows * k.in_head, kos = rows * k.out_head;
+    const T *xq = (const T *)q.in + blockIdx.x * q.in_token + row * q.in_head + e0, *xk = (const T *)k.in + blockIdx.x * k.in_token + row * k.in_head + e0;
+    T *yq = (T *)q.out + blockIdx.x * q.out_token + row * q.out_head + e0, *yk = (T *)k.out + blockIdx.x * k.out_token + row * k.out_head + e0;
     int position = positions[blockIdx.x], buffer = 0;
     // two sets of angles: a thread may form those of the next token while another still reads these, but not those of the
     // one after that, which it does behind the next token's barrier
     for (int t = blockIdx.x; t < tokens; t += gridDim.x, buffer ^= 1) {
         const int next = t + (int)gridDim.x < tokens ? positions[t + gridDim.x] : 0;
-        turn_heads<T, VE, INTER>(rot, angles[buffer], q, k, t, h0, h1, threadIdx.x, kThreads, [&]() {
-            token_angles(rot, position, sign, angles[buffer], threadIdx.x, kThreads);
-            __syncthreads();
-        });
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j)
+            if (j < nq) {
+                a[j].load(xq + j * qs, VE);
+                if (!INTER && turns) b[j].load(xq + j * qs + half, VE);
+            }
+        token_angles(rot, position, sign, angles[buffer], threadIdx.x, kThreads);
+        __syncthreads();
         position = next;
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const float2 x = turns ? angles[buffer][u * NA + i] : make_float2(1.f, 0.f);
+            c[i] = x.x;
+            s[i] = x.y;
+        }
+        heads(xq, yq, qs, qos, nq, q_copies, true);
+        heads(xk, yk, ks, kos, nk, k_copies, false);
+        xq += gridDim.x * q.in_token;
+        yq += gridDim.x * q.out_token;
+        xk += gridDim.x * k.in_token;
+        yk += gridDim.x * k.out_token;
     }
 }
 
@@ -81,6 +163,10 @@ template <typename T, int VE, bool INTER>
 cudaError_t run_as(const fluxbin_rotary_t &rot, int inverse, int tokens, const int *positions, const Side &q, const Side &k, cudaStream_t s)
 {
     const int heads = q.heads + k.heads;
+    const float sign = inverse ? -1.f : 1.f;
+    if constexpr (VE * sizeof(T) == 16) {
+        if (tokens >= kFewTokens) return launch(rotary_prompt_kernel<T, VE, INTER>, dim3((unsigned)(tokens < kCtas ? tokens : kCtas)), kThreads, 0, s, rot, sign, tokens, positions, q, k);
+    }
     int each = heads;
     if (tokens < kFewTokens) {
         const int units = rot.rotary_dim / 2 / (INTER ? VE / 2 : VE) + (rot.head_dim - rot.rotary_dim + VE - 1) / VE;
@@ -89,9 +175,7 @@ cudaError_t run_as(const fluxbin_rotary_t &rot, int inverse, int tokens, const i
         if (each < at_once) each = at_once;
         if (each > heads) each = heads;
     }
-    const int ctas = tokens < kCtas ? tokens : kCtas;
-    return launch(rotary_kernel<T, VE, INTER>, dim3((unsigned)ctas, (unsigned)((heads + each - 1) / each)), kThreads, 0, s, rot, inverse ? -1.f : 1.f, tokens,
-                  positions, q, k, each);
+    return launch(rotary_kernel<T, VE, INTER>, dim3((unsigned)tokens, (unsigned)((heads + each - 1) / each)), kThreads, 0, s, rot, sign, positions, q, k, each);
 }
 template <typename T>
 cudaError_t run(const fluxbin_rotary_t &rot, int dtype, int inverse, int tokens, const int *positions, const Side &q, const Side &k, cudaStream_t s)
