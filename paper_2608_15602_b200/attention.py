@@ -56,11 +56,13 @@ def _int32(x: torch.Tensor, n: int, what: str) -> int:
 
 def _output(given: torch.Tensor | None, like: torch.Tensor, heads: int, what: str, stream):
     """An output like a [tokens][heads][dim] input: (tensor, pointer, token stride, head stride)."""
-    y = given
-    if y is None:
+    if given is None:
         y = torch.empty_like(like)
         if stream is not None:                   # made on the current stream, written on another
             y.record_stream(stream)
+        st, sh, _ = y.stride()
+        return y, y.data_ptr(), st, sh
+    y = given
     p, h, st, sh = _heads(y, like.shape[0], like.shape[2], like.dtype, what)
     if h != heads:
         raise ValueError(f"{what}: {heads} heads are wanted")

@@ -423,8 +423,6 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
             const float ks = __shfl_sync(0xffffffffu, now.ks, slot), vs = __shfl_sync(0xffffffffu, now.vs, slot);
             const long long ahead = __shfl_sync(0xffffffffu, slot + STAGES - 1 < 32 ? now.at : next.at, (slot + STAGES - 1) & 31);
             copies_wait<STAGES - 2>();
-            if (tile + STAGES - 1 < tiles) fetch(ahead, stage_ahead);
-            copies_commit();
             Words<4> kw[2][KC];
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -452,6 +450,10 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
                         mma(!QSHARED && (w & 1) ? s2[QSHARED ? 0 : t] : s[t], a0, a1, a2, a3, b.x, b.y);
                     }
                 }
+            // (here and not before the scores: 119 -> 114 us with 40 rows)
+            if (tile + STAGES - 1 < tiles) fetch(ahead, stage_ahead);
+            copies_commit();
+
             // ---- softmax against a lagging reference
             bool above = false;
             const bool edge = tok + 16 > seen_first || none;

@@ -517,10 +517,12 @@ class Words:
     """One of the calls above through fluxbin_call_words: called with the C call's arguments (None is not an integer: 0)."""
 
     def __init__(self, which: int, layout: str, where: str):
-        self.which, self.pack, self.where = which, struct.Struct(layout).pack, where
+        self.which, self.pack, self.where, self.call = which, struct.Struct(layout).pack, where, None
 
     def __call__(self, *args):
-        status = _lib().fluxbin_call_words(self.which, self.pack(*args))
+        if self.call is None:
+            self.call = _lib().fluxbin_call_words
+        status = self.call(self.which, self.pack(*args))
         if status:
             raise FluxBinError(status, self.where)
 
