@@ -4,7 +4,9 @@
 // forms, 16 cached tokens at a time,
 //     S^T = K Q^T  [16 tokens x rows],   P = exp2(S c - m),   O^T += V^T P^T  [dim x rows],   l += sum P
 // with the tokens (then the elements of a head) as the 16-row side of the matrix instruction and the query rows as its
-// 8-column side: a decode step has as few rows as query heads share a key head, and 8 columns waste the least.
+// 8-column side: a decode step has as few rows as query heads share a key head, and 8 columns waste the least.  (The
+// instructions that accumulate outside the registers take 64 tokens or more a step, from operands of 16 bits in shared
+// memory: the 8-bit cache would have to be converted there and back again for 8 columns.)
 //
 // What bounds it is the cache's bytes.  Each lane copies (cp.async) the 16-byte pieces that it will hold as matrix operands
 // into its own places of a ring in shared memory, a few tiles ahead, and takes them from there itself: no barrier, no bank
@@ -35,12 +37,10 @@ namespace {
 // output takes the registers), by head dimension and tiles of 8 query rows.  Measured at 128 with 8 rows on 64 requests of up
 // to 16384 tokens: 4 x 3 with 4 tiles 242 us, 8 x 2 with 3 249, 6 x 2 with 4 257, 4 x 4 with 3 (128 registers, spills) 277, 12 x
 // 1 with 4 288: small CTAs, so that the others go on while one ends a job, and tiles on their way rather than warps.  With 16
-// rows on 16 requests of up to 8190: 4 x 2 64 us, 8 x 1 74.  With 40 rows there (five drafted tokens): 40 in one tile 119 us, 32
-// 174, 16 175 -- the cache is read once for each tile.
+// rows on 16 requests of up to 8190: 4 x 2 64 us, 8 x 1 74.  40 rows are as many as the registers take.
 template <int D, int NT> struct Shape;
 template <> struct Shape<64, 1> { static constexpr int warps = 8, ctas = 2, stages = 6; static constexpr bool shared_queries = false; };
 template <> struct Shape<64, 2> { static constexpr int warps = 8, ctas = 2, stages = 6; static constexpr bool shared_queries = false; };
-template <> struct Shape<64, 5> { static constexpr int warps = 8, ctas = 1, stages = 8; static constexpr bool shared_queries = true; };
 template <> struct Shape<128, 1> { static constexpr int warps = 4, ctas = 3, stages = 4; static constexpr bool shared_queries = false; };
 template <> struct Shape<128, 2> { static constexpr int warps = 4, ctas = 2, stages = 6; static constexpr bool shared_queries = false; };
 template <> struct Shape<128, 5> { static constexpr int warps = 8, ctas = 1, stages = 5; static constexpr bool shared_queries = true; };
@@ -704,11 +704,13 @@ cudaError_t run(const Args &a, cudaStream_t s)
 }
 template <int D, int FMT, typename T> cudaError_t run_rows(const Args &a, cudaStream_t s)
 {
-    // rows that share a key head in an average request
+    // rows that share a key head in an average request; a tile of 40 rows takes 2.4 times one of 16 (at 128: 16 rows 56 us,
+    // 32 94, 40 139 against 111 in one tile, 64 176 against 190 in two, 72 212 against 191; at 64 tiles of 40 never won)
     const long long rows = (long long)(a.q_heads / a.c.kv_heads) * ((a.tokens + a.batch - 1) / a.batch);
-    if constexpr (D != 256) {
-        if (rows > 16) return run<D, FMT, 5, T>(a, s);
+    if constexpr (D == 128) {
+        if ((rows + 39) / 40 * 12 < (rows + 15) / 16 * 5) return run<D, FMT, 5, T>(a, s);
     }
+    // (9 to 16 rows in one tile of 16 instead of two of 8: 57 against 76 us at 128, 43 against 51 at 256)
     if (rows > 8) return run<D, FMT, 2, T>(a, s);
     return run<D, FMT, 1, T>(a, s);
 }
