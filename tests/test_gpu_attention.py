@@ -119,6 +119,21 @@ def test_rotary_no_tokens_and_head_major_input(at):
     check_turn(r.apply(q, None, dev([3, 1, 4, 1, 5]))[0], q, [3, 1, 4, 1, 5], r, "fp16")
 
 
+@pytest.mark.parametrize("T,hq,hk,D,d,inter,dtype", [(148, 5, 3, 128, 128, False, "fp16"), (700, 3, 0, 128, 64, True, "bf16"), (333, 40, 2, 64, 32, False, "fp32"),
+                                                       (601, 1, 1, 256, 256, True, "fp16"), (149, 70, 1, 96, 96, True, "fp32"), (650, 2, 2, 80, 40, False, "bf16")])
+def test_rotary_prompts(at, T, hq, hk, D, d, inter, dtype):
+    """Enough tokens for the kernels that go over them (and, with the last, heads that allow no wide access to both halves)."""
+    r = rope(at, D, d, inter, "none")
+    pos = np.random.default_rng(T).integers(0, 131072, T)
+    q, k = normal(1, (T, hq, D), dtype), normal(2, (T, hk, D), dtype) if hk else None
+    qo, ko = r.apply(q, k, dev(pos))
+    check_turn(qo, q, pos, r, dtype)
+    if hk:
+        check_turn(ko, k, pos, r, dtype)
+    back, _ = r.apply(qo, None, dev(pos), inverse=True, q_out=qo)
+    assert back is qo and (np.abs(f64(qo) - f64(q)) <= 4 * U[dtype] * np.abs(f64(q)).max()).all()
+
+
 # ---- append and read ----------------------------------------------------------------------------------------------
 
 def run_starts(slots, bs, t):
@@ -222,6 +237,33 @@ def test_append_with_positions(at, fmt, bs, H, D, major, dtype, part, inter):
     assert c.append(k, v, dev(slots), rotary=r, positions=dev(pos)) is None
     for a, b in zip(before, (c.k.view(torch.uint8), c.v.view(torch.uint8), c.k_scale, c.v_scale)):
         assert torch.equal(a, b)                          # the same tokens again change nothing
+
+
+@pytest.mark.parametrize("fmt,bs,H,D,T,dtype", [("int8", 128, 2, 128, 300, "fp16"), ("e4m3", 256, 1, 256, 601, "bf16"), ("int8", 48, 3, 256, 130, "fp32"), ("e4m3", 16, 1, 64, 4100, "fp16"),
+                                                 ("int8", 1024, 1, 64, 1500, "fp16")])
+@pytest.mark.parametrize("turn", [False, True])
+def test_append_prompts_in_wide_blocks(at, fmt, bs, H, D, T, dtype, turn):
+    """Runs of more tokens than a pass holds, and enough tokens for every way a launch is cut; then one token more."""
+    nb = -(-(T + 1) // bs) + 1
+    c = at.KVCache(nb, bs, H, D, fmt)
+    fill(c, 5)
+    want = [oa.Cache(e, f64(s), fmt) for e, s in zip(entries_of(c), (c.k_scale, c.v_scale))]
+    r = rope(at, D, D, False, "none") if turn else None
+    f, m = oa.frequencies(D)
+    order = np.random.default_rng(T).permutation(nb)
+    q = normal(7, (T, 2, D), dtype) if turn else None
+    for lo, hi in ((0, T), (T, T + 1)):
+        pos = np.arange(lo, hi)
+        slots = (order[pos // bs] * bs + pos % bs).astype(np.int32)
+        k, v = normal(3 + lo, (hi - lo, H, D), dtype), normal(4 + lo, (hi - lo, H, D), dtype, 5.0)
+        out = c.append(k, v, dev(slots), rotary=r, positions=dev(pos) if turn else None, q=q[:hi - lo] if turn else None)
+        if turn:
+            check_turn(out, q[:hi - lo], pos, r, dtype)
+        want[0].append(oa.rotary(f64(k), pos, f, m, D, False) if turn else f64(k), slots)
+        want[1].append(f64(v), slots)
+        check_cache(c, want, fmt, turn)
+        for w, e, s in zip(want, entries_of(c), (c.k_scale, c.v_scale)):
+            w.entries, w.quotients, w.scale = e, e.copy(), f64(s)
 
 
 def test_append_equals_turning_first_in_fp32(at):
@@ -365,6 +407,42 @@ def test_attend_long_context_split_over_the_device(at, Hq, H, D, length, fmt):
     # a workspace serves smaller calls after larger ones
     out = c.attend(q[1:2], dev(table[1:2]), dev(lengths[1:2]), ws)
     check_attend(c, q[1:2], table[1:2], lengths[1:2], [0, 1], D ** -0.5, out, None, "fp16")
+
+
+@pytest.mark.parametrize("Hq,H,D,new", [(8, 1, 128, 5), (40, 1, 128, 1), (16, 2, 128, 2), (9, 1, 128, 4), (7, 1, 64, 5), (6, 2, 256, 4)])
+def test_attend_row_tiles(at, Hq, H, D, new):
+    """33 to 40, 9 to 16 and just above as many query rows of a key head."""
+    lengths = [61, 300, 5]
+    c, table = setup(at, "int8", 16, H, D, lengths, Hq + new)
+    q = normal(31, (3 * new, Hq, D), "bf16")
+    starts = np.arange(4) * new
+    out, lse = c.attend(q, dev(table), dev(lengths), c.workspace(3, 3 * new, Hq), query_start=dev(starts), with_lse=True)
+    check_attend(c, q, table, lengths, starts, D ** -0.5, out, lse, "bf16")
+
+
+def test_attend_shares_that_are_drawn(at):
+    """Long enough that the ends of the ranges are drawn: against 64 bits on the GPU, and twice the same."""
+    B, Hq, H, D, bs, fmt = 7, 8, 8, 64, 128, "int8"
+    lengths = [90001, 3, 89000, 90500, 1, 89999, 88000]        # 95 units for each of 296 CTAs: nine of them are drawn
+    c, table = setup(at, fmt, bs, H, D, lengths, 41)
+    q = normal(42, (B, Hq, D), "fp16")
+    ws = c.workspace(B, B, Hq)
+    first = c.attend(q, dev(table), dev(lengths), ws, with_lse=True)
+    for _ in range(3):
+        again = c.attend(q, dev(table), dev(lengths), ws, with_lse=True)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    for r, L in enumerate(lengths):
+        ids = dev(table[r, :-(-L // bs)]).long()
+        k, v = (x[ids].double() * s[ids].double()[..., None, None] for x, s in ((c.k, c.k_scale), (c.v, c.v_scale)))
+        k, v = (x.transpose(0, 1).reshape(H, -1, D)[:, :L] for x in (k, v))
+        x = torch.einsum("hd,hld->hl", q[r].double(), k) * D ** -0.5
+        p = torch.softmax(x, -1)
+        want, mean = torch.einsum("hl,hld->hd", p, v), torch.einsum("hl,hld->hd", p, v.abs())
+        S = (q[r].double().abs()[:, None, :] * k.abs()).sum(-1).amax(-1)[:, None] * D ** -0.5
+        bound = U["fp16"] * want.abs() + (2.0 ** -11 + 2.0 ** -19 + (2 * D + 8) * 2.0 ** -24 * S + L * 2.0 ** -23) * mean + 1e-7
+        assert ((first[0][r].double() - want).abs() <= bound).all()
+        lse = torch.logsumexp(x, -1)
+        assert ((first[1][r].double() - lse).abs() <= (D + 4) * 2.0 ** -24 * S[:, 0] + 2.0 ** -20 + L * 2.0 ** -24 + 2.0 ** -23 * lse.abs()).all()
 
 
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
