@@ -157,13 +157,12 @@ class KVCache:
             raise fluxbin.FluxBinError(status, "fluxbin_kv_validate")
 
     def _new(self, shape: tuple, dtype: torch.dtype, stream) -> torch.Tensor:
-        """torch.empty(shape, dtype) on the cache's device; made like the last (small) one of that kind it takes half the time."""
+        """torch.empty(shape, dtype) on the cache's device, made like the last one of that type (one element seen as many): half
+        the time."""
         last = self._last.get(dtype)
         if last is None or last.shape != shape:
-            last = torch.empty(shape, dtype=dtype, device=self.device)
-            if last.numel() <= 1 << 16:
-                self._last[dtype] = last
-        new = torch.empty_like(last)
+            last = self._last[dtype] = torch.empty((1,) * len(shape), dtype=dtype, device=self.device).expand(shape)
+        new = torch.empty_like(last, memory_format=torch.contiguous_format)
         if stream is not None:
             new.record_stream(stream)
         return new

@@ -581,7 +581,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
             const long long tok = rq.first + g / G;
             const int head = h * G + g % G;
             T *op = (T *)a.out + tok * a.out_token + head * a.out_head + d;
-            T e[4] = {from_float<T>(v.x), from_float<T>(v.y), from_float<T>(v.z), from_float<T>(v.w)};
+            __align__(8) T e[4] = {from_float<T>(v.x), from_float<T>(v.y), from_float<T>(v.z), from_float<T>(v.w)};
             *reinterpret_cast<uint2 *>(op) = *reinterpret_cast<const uint2 *>(e);
             if (d == 0 && a.lse) a.lse[tok * a.q_heads + head] = lse2 * 0.6931471805599453f;
         };

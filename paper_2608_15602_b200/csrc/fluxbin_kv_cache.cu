@@ -126,7 +126,7 @@ template <typename T> struct Eight {
     }
     __device__ __forceinline__ void get(float (&v)[8]) const
     {
-        T e[8];
+        __align__(16) T e[8];
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(e)[i] = w[i];
 #pragma unroll
@@ -459,7 +459,7 @@ __global__ void __launch_bounds__(kWide) read_kernel(fluxbin_kv_cache_t c, int t
         if (!out) continue;
         const uint2 w = *reinterpret_cast<const uint2 *>((const unsigned char *)(side ? c.d_v : c.d_k) + at);
         const float scale = (side ? c.d_v_scale : c.d_k_scale)[sc];
-        T e[8];
+        __align__(16) T e[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) e[j] = from_float<T>(live ? Entry<FMT>::load((unsigned char)((j < 4 ? w.x : w.y) >> (j % 4 * 8))) * scale : 0.f);
 #pragma unroll
