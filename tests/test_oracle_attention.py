@@ -169,3 +169,20 @@ def test_refused_calls():
         b, t, bs, ln, P, tb, st, w, fr, cap, nf, nfo, lo, P, P, po, P, P, None)
     assert adv(b=0) == 3 and adv(b=8193) == 3 and adv(t=-1) == 3 and adv(bs=0) == 3 and adv(w=0) == 3 and adv(st=3) == 3 and adv(cap=0) == 3
     assert adv(ln=None) == 1 and adv(po=None) == 1 and adv(lo=P) == 3 and adv(nfo=P) == 3 and adv(ln=P + 2) == 6
+
+
+def test_calls_by_words_refuse_what_the_calls_refuse():
+    lib = fluxbin.library()
+    assert lib.fluxbin_call_words(0, None) == 1 and lib.fluxbin_call_words(5, bytes(200)) == 7 and lib.fluxbin_call_words(-1, bytes(200)) == 7
+    assert lib.fluxbin_call_words(0, bytes(200)) == 1 and lib.fluxbin_call_words(1, bytes(200)) == 1        # no descriptor
+    assert lib.fluxbin_call_words(3, bytes(200)) == 1 and lib.fluxbin_call_words(4, bytes(200)) == 3        # no cache; no request
+    c = cache()
+    P = 1 << 25
+    ws = fluxbin.kv_attend_workspace_size(2, 2, 4, 2, 64)
+    good = dict(desc=ctypes.addressof(c), dtype=0, batch=2, tokens=0, q=P, heads=4, qt=256, qh=64, start=P, lengths=P, table=P, stride=8, width=8, scale=0.5,
+                out=P, ot=256, oh=64, lse=0, ws=P, bytes=ws, stream=0)
+    fluxbin.kv_attend_call(*good.values())                                                                   # no tokens: nothing to do
+    for name, value, status in [("dtype", 1, 7), ("batch", 0, 3), ("heads", 3, 3), ("width", 9, 3), ("desc", 0, 1)]:
+        with pytest.raises(fluxbin.FluxBinError) as e:
+            fluxbin.kv_attend_call(*{**good, name: value}.values())
+        assert e.value.status == status, name
