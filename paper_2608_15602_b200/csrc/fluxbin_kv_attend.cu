@@ -14,14 +14,15 @@
 // takes 16 consecutive bytes wherever the instruction would want scattered pairs.
 //   keys:    lane (r, q) = (lane / 4, lane % 4) reads elements 16 q .. + 15 of each 64-byte piece of tokens r and r + 8
 //   values:  the same lane reads elements 16 r .. + 15 (of 128) of tokens 2q, 2q + 1, 2q + 8, 2q + 9 and interleaves the
-//            bytes of two tokens, which the conversion to fp16 does on the way
+//            bytes of two tokens, which the conversion to bf16 does on the way
 // P leaves the first product with a lane per token and enters the second with a lane per row: movmatrix turns it.
-// 8-bit entries are exact in fp16.  The block's key scale multiplies the score in fp32; the value scale, relative to the
-// largest one met so far (vref), multiplies P before P is rounded to fp16.  That rounding (2^-11 of each probability,
-// against 2^-9 of bf16; with the rest of it as a second operand 40 rows take 10 % more time, 8 rows 1.5 %) is the only one
-// below 32 bits; probabilities are held between 2^15 and fp16's smallest steps by
-// letting the reference m lag: it is raised to (row maximum - 7) only when a P would pass 2^15, so that most steps need no
-// reduction over lanes and what is flushed to zero is below 2^-31 of the largest probability.
+// 8-bit entries are exact in fp16 and in bf16.  The block's key scale multiplies the score in fp32.  A probability times its
+// block's value scale (over the largest one met so far, vref) is the sum of two bf16 operands, the second of which rounds what
+// the first left: 2^-16 of it is lost, and nothing is flushed to zero short of fp32's own range, so a result does not suffer
+// where small probabilities or blocks of small values decide it.  (One fp16 operand: 2^-11 lost, and all of it 2^-31 below the
+// largest.  With two products in the place of one 8 rows of 128 take 1 to 2 % more time, 16 rows 2 to 11 %, 40 rows 11 %.)
+// The reference m lags: it is raised to (row maximum - 7) only when a P would pass 2^15, so that most steps need no reduction
+// over lanes.
 //
 // Work is cut evenly whatever the lengths are: all (request, head, rows) jobs in units of cached tokens form a line, which is
 // cut into a range for each CTA (the lengths are read on the device: a captured graph serves every step).  A job cut between
@@ -77,10 +78,10 @@ struct Args {
     float *partial;                             // [shares][2][rows][D]
 };
 
-// ---- conversions of four 8-bit entries to two pairs of fp16 ---------------------------------------------
+// ---- conversions of 8-bit entries ------------------------------------------------------------------------
 
-// bf16 rows of queries become fp16 exactly, multiplied by the power of two that takes their largest element to 2^14 ..
-// 2^15; elements below 2^-39 of it lose bits that fp32 sums would not keep
+// bf16 rows of queries become fp16, multiplied by the power of two that takes their largest element to 2^14 .. 2^15: exactly
+// down to 2^-31 of that element, what is smaller to 2^-39 of it (fp16's smallest steps)
 __device__ __forceinline__ int exponent_of(float largest) { return largest > 0.f ? min(max((int)(__float_as_uint(largest) >> 23), 1), 254) - 127 - 14 : 0; }
 __device__ __forceinline__ uint32_t half2_of_bf16(uint32_t w, int e)
 {
@@ -88,6 +89,7 @@ __device__ __forceinline__ uint32_t half2_of_bf16(uint32_t w, int e)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
+// four entries of a key to two pairs of fp16
 template <int FMT> __device__ __forceinline__ void to_half4(uint32_t x, uint32_t &lo, uint32_t &hi);
 // int8: the byte with its sign bit flipped, under the exponent of 1024, is 1024 + 128 + value; fp16 holds that exactly
 template <> __device__ __forceinline__ void to_half4<FLUXBIN_CACHE_INT8>(uint32_t x, uint32_t &lo, uint32_t &hi)
@@ -104,10 +106,54 @@ template <> __device__ __forceinline__ void to_half4<FLUXBIN_CACHE_E4M3>(uint32_
     asm("{ .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n cvt.rn.f16x2.e4m3x2 %1, b;\n }" : "=r"(lo), "=r"(hi) : "r"(x));
 }
 
+// four entries of two tokens' values to four pairs (x, y) of bf16, as parts 1 / kPart of them
+template <int FMT> constexpr float kPart = FMT == FLUXBIN_CACHE_INT8 ? 64.f : 1.f;
+template <int FMT> __device__ __forceinline__ void to_bfloat2x4(uint32_t x, uint32_t y, uint32_t (&pair)[4]);
+__device__ __forceinline__ uint32_t bfloat2_of_half2(__half2 h)      // exact for 8-bit entries
+{
+    const float2 f = __half22float2(h);
+    const __nv_bfloat162 r = __floats2bfloat162_rn(f.x, f.y);
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+// int8: the byte with its sign bit flipped, u = 128 + value, is as a bf16 pattern u * 2^-133 (the smallest numbers and the
+// first normal ones have one step); times 2^127, less 128 * 2^-6, that is value * 2^-6 exactly
+template <> __device__ __forceinline__ void to_bfloat2x4<FLUXBIN_CACHE_INT8>(uint32_t x, uint32_t y, uint32_t (&pair)[4])
+{
+    x ^= 0x80808080u;
+    y ^= 0x80808080u;
+    const __nv_bfloat162 up = __bfloat162bfloat162(__ushort_as_bfloat16(0x7f00)), down = __bfloat162bfloat162(__ushort_as_bfloat16(0xc000));     // 2^127, -2
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+        const uint32_t z = __byte_perm(x, y, i ? 0x7362 : 0x5140);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t u = __byte_perm(z, 0, k ? 0x4342 : 0x4140);
+            const __nv_bfloat162 r = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&u), up, down);
+            pair[i + k] = *reinterpret_cast<const uint32_t *>(&r);
+        }
+    }
+}
+// e4m3: by way of fp16 and fp32, both exact (a NaN stays one)
+template <> __device__ __forceinline__ void to_bfloat2x4<FLUXBIN_CACHE_E4M3>(uint32_t x, uint32_t y, uint32_t (&pair)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+        uint32_t h[2];
+        to_half4<FLUXBIN_CACHE_E4M3>(__byte_perm(x, y, i ? 0x7362 : 0x5140), h[0], h[1]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) pair[i + k] = bfloat2_of_half2(*reinterpret_cast<const __half2 *>(&h[k]));
+    }
+}
+
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&x)[4], const uint32_t (&y)[4], int i, const uint32_t (&b)[2])
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(x[i]), "r"(x[i + 1]), "r"(y[i]), "r"(y[i + 1]), "r"(b[0]), "r"(b[1]));
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t v)
 {
@@ -115,10 +161,13 @@ __device__ __forceinline__ uint32_t transposed(uint32_t v)
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(t) : "r"(v));
     return t;
 }
-__device__ __forceinline__ uint32_t pack_half2(float lo, float hi)
+// two values as bf16, and what that rounding left of them as another two
+__device__ __forceinline__ void split_bfloat2(float x, float y, uint32_t &upper, uint32_t &rest)
 {
-    const __half2 h = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&h);
+    const __nv_bfloat162 u = __floats2bfloat162_rn(x, y);
+    upper = *reinterpret_cast<const uint32_t *>(&u);
+    const __nv_bfloat162 r = __floats2bfloat162_rn(x - __uint_as_float(upper << 16), y - __uint_as_float(upper & 0xffff0000u));
+    rest = *reinterpret_cast<const uint32_t *>(&r);
 }
 __device__ __forceinline__ float exp2_fast(float x)         // relative error 2^-22, exp2(-inf) = 0
 {
@@ -497,7 +546,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
             if (vs > vref && vs >= 7.888609052210118e-31f) {
                 const float f = vref / vs;
                 vref = vs;
-                vref_inverse = 1.f / vs;
+                vref_inverse = kPart<FMT> / vs;
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -506,7 +555,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
                         for (int e = 0; e < 4; ++e) o[t][i][e] *= f;
             }
             const float vf = vs * vref_inverse;
-            uint32_t pf[NT][2];
+            uint32_t pf[NT][2], pr[NT][2];       // probabilities times scales as the second operand, and what bf16 left of them
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 float p[4];
@@ -515,8 +564,13 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
                     p[e] = exp2_fast(s[t][e] - ref[t][e & 1]);
                     sum[t][e & 1] += p[e];
                 }
-                pf[t][0] = transposed(pack_half2(p[0] * vf, p[1] * vf));
-                pf[t][1] = transposed(pack_half2(p[2] * vf, p[3] * vf));
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) {
+                    uint32_t upper, rest;
+                    split_bfloat2(p[e] * vf, p[e + 1] * vf, upper, rest);
+                    pf[t][e / 2] = transposed(upper);
+                    pr[t][e / 2] = transposed(rest);
+                }
             }
             Words<VW> vw[4][VC];
 #pragma unroll
@@ -535,17 +589,15 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
             for (int c = 0; c < VC; ++c)
 #pragma unroll
                 for (int w = 0; w < VW; ++w) {
-                    uint32_t f[2][4];
+                    uint32_t f[2][4];            // tokens 2q, 2q + 1, then 2q + 8, 2q + 9
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {            // tokens 2q, 2q + 1, then 2q + 8, 2q + 9
-                        const uint32_t x = vw[2 * i][c].w[w], y = vw[2 * i + 1][c].w[w];
-                        to_half4<FMT>(__byte_perm(x, y, 0x5140), f[i][0], f[i][1]);
-                        to_half4<FMT>(__byte_perm(x, y, 0x7362), f[i][2], f[i][3]);
-                    }
+                    for (int i = 0; i < 2; ++i) to_bfloat2x4<FMT>(vw[2 * i][c].w[w], vw[2 * i + 1][c].w[w], f[i]);
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
-                        mma(o[t][(c * VW + w) * 2], f[0][0], f[0][1], f[1][0], f[1][1], pf[t][0], pf[t][1]);
-                        mma(o[t][(c * VW + w) * 2 + 1], f[0][2], f[0][3], f[1][2], f[1][3], pf[t][0], pf[t][1]);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) mma_bf16(o[t][(c * VW + w) * 2 + i], f[0], f[1], 2 * i, pf[t]);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) mma_bf16(o[t][(c * VW + w) * 2 + i], f[0], f[1], 2 * i, pr[t]);
                     }
                 }
             stage = stage + 1 == STAGES ? 0 : stage + 1;
