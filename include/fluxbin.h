@@ -578,11 +578,12 @@ fluxbin_status_t fluxbin_kv_read(const fluxbin_kv_cache_t *cache, int32_t dtype,
  *                   length are not read; tokens of a block id outside the cache are masked out.
  *   d_q, d_out      fp16 or bf16 heads; 16-byte aligned, strides multiples of 8 elements
  *   d_lse           DEVICE fp32 [tokens][q_heads] or NULL: log of the sum of exp(scale * q . k) (natural)
- * A row that sees nothing gets out = 0 and lse = -inf.  What lies in the cache past a request's length (NaN patterns
- * included) has no influence.  Scores, maxima, sums and accumulators are fp32.  8-bit entries enter the matrix instructions
- * exactly; a probability, times its value's scale, as two bf16 numbers whose sum is off by 2^-16 of it; bf16 queries as fp16
- * times a power of two, elements below 2^-31 of their row's largest held to 2^-39 of it.  Results do not depend on timing: sums
- * are joined in a fixed order (which depends on the lengths of the whole batch).
+ * A row that sees nothing gets out = 0 and lse = -inf.  What lies in the cache past a request's length, or in tokens that a
+ * row does not see (NaN patterns and NaN scales included), has no influence on it.  Scores, maxima, sums and accumulators are
+ * fp32.  8-bit entries enter the matrix instructions exactly; a probability, times its value's scale, as two bf16 numbers
+ * whose sum is off by 2^-16 of it; bf16 queries as fp16 times a power of two, elements below 2^-31 of their row's largest held
+ * to 2^-39 of it.  Results do not depend on timing: sums are joined in a fixed order (which depends on the lengths of the whole
+ * batch).
  * d_workspace: fluxbin_kv_attend_workspace_size bytes (13 MB at head_dim 128: the partial results of jobs that several CTAs
  * work at; it depends on head_dim alone, so one serves all calls), zeroed once with fluxbin_workspace_init; calls leave its
  * counters zeroed, and calls that share one must be ordered on a stream.

@@ -232,7 +232,8 @@ template <int D, int ROWS, int WARPS, int STAGES, bool QSHARED> struct Shared {
     uint2 q[QSHARED ? ROWS / 8 : 1][D / 16][32];         // the queries as operands, by lane
     float factor[ROWS];
     long long scan[WARPS], before;
-    int request, last, share;
+    int request, last, share, any_nan;
+    uint32_t nan[ROWS][D / 32];                          // elements of this job's rows that see a NaN (see hide_nan)
 };
 
 // one CTA: its part of the line, job after job
@@ -266,6 +267,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
         if (lane >= o) upto += x;
     }
     if (lane == 31) sm.scan[warp] = upto;
+    for (int i = tid; i < ROWS * (D / 32); i += kThreads) sm.nan[i / (D / 32)][i % (D / 32)] = 0;
+    if (tid == 0) sm.any_nan = 0;
     __syncthreads();
     long long total = 0;
     for (int w = 0; w < kWarps; ++w) {
@@ -460,6 +463,41 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
             sum[t][0] = sum[t][1] = 0.f;
         }
 
+        // On tiles that not all rows see to their end: what must not meet the probability 0 of a row that does not see its token
+        // is taken out of the values, and noted for the rows that do.  Each lane looks through its own places of the ring.
+        //   values past the request's length, or in no block of its own (e4m3: may be NaN patterns): become 0
+        //   a NaN entry of a new token: becomes 0; its element is NaN in every row that sees the token
+        //   a scale that is no number: the caller takes 0 for it; all elements are NaN in every row that sees a token of the tile
+        auto hide_nan = [&](int tok, int stage, bool none, float vs) {
+            auto sees = [&](int row) { return rq.length - (rq.count - 1 - (row0 + row) / G); };
+            if (!(vs < INFINITY)) {
+                for (int row = lane; row < rows; row += 32)
+                    if (tok < sees(row)) {
+                        for (int d = 0; d < D / 32; ++d) atomicOr(&sm.nan[row][d], 0xffffffffu);
+                        sm.any_nan = 1;
+                    }
+            }
+            if (FMT != FLUXBIN_CACHE_E4M3) return;
+#pragma unroll 1
+            for (int i = 0; i < 4 * VC * VW; ++i) {
+                const int part = i / VW, token = tok + 2 * lq + (part / VC & 1) + (part / VC >> 1) * 8;
+                const uint32_t at = v_ring + stage * (32 * D) + part * (VW * 128) + i % VW * 4;
+                uint32_t x;
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+                uint32_t nan = ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;        // the top bits of the bytes that are NaN
+                if (none || token >= rq.length) x = nan = 0;
+                else if (nan) x &= ~(nan | (nan - (nan >> 7)));
+                else continue;
+                asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(x) : "memory");
+                for (; nan; nan &= nan - 1) {
+                    const int d = part % VC * (VW * 32) + lr * (VW * 4) + i % VW * 4 + (__ffs(nan) - 1) / 8;
+                    for (int row = 0; row < rows; ++row)
+                        if (token < sees(row)) atomicOr(&sm.nan[row][d / 32], 1u << (d % 32));
+                    sm.any_nan = 1;
+                }
+            }
+        };
+
         int stage = 0, stage_ahead = STAGES - 1;
         for (int tile = 0; tile < tiles; ++tile) {
             const int tok = tok0 + tile * kUnit, slot = tile & 31;
@@ -543,7 +581,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
                         }
                     }
             }
-            if (vs > vref && vs >= 7.888609052210118e-31f) {
+            if (vs > vref && vs >= 7.888609052210118e-31f && vs < INFINITY) {
                 const float f = vref / vs;
                 vref = vs;
                 vref_inverse = kPart<FMT> / vs;
@@ -554,7 +592,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[t][i][e] *= f;
             }
-            const float vf = vs * vref_inverse;
+            const float vf = edge && !(vs < INFINITY) ? 0.f : vs * vref_inverse;
             uint32_t pf[NT][2], pr[NT][2];       // probabilities times scales as the second operand, and what bf16 left of them
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
@@ -572,19 +610,13 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
                     pr[t][e / 2] = transposed(rest);
                 }
             }
+            // ---- values
+            if (edge && (FMT == FLUXBIN_CACHE_E4M3 || !(vs < INFINITY))) hide_nan(tok, stage, none, vs);
             Words<VW> vw[4][VC];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int c = 0; c < VC; ++c) vw[i][c] = take<VW>(v_ring + stage * (32 * D) + (i * VC + c) * (VW * 128));
-            // ---- values: what lies past the request's length, or in no block of its own, may be a NaN pattern
-            if (FMT == FLUXBIN_CACHE_E4M3 && (none || tok + 16 > rq.length)) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (none || tok + 2 * lq + (i & 1) + (i >> 1) * 8 >= rq.length)
-#pragma unroll
-                        for (int c = 0; c < VC; ++c) vw[i][c] = Words<VW>{};
-            }
 #pragma unroll
             for (int c = 0; c < VC; ++c)
 #pragma unroll
@@ -626,7 +658,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
             }
         if (lane == 0) sm.v[warp] = vref;
         __syncthreads();
-        const bool whole = p0 == 0 && p1 == rq.pieces;
+        const bool whole = p0 == 0 && p1 == rq.pieces, any_nan = sm.any_nan;
         const int first_cta_slot = p0 == 0;                  // this job begins here, or goes on from the CTA before
         float *part = a.partial + (share * 2 + first_cta_slot) * ROWS * D, *part_lse = a.partial_lse + (share * 2 + first_cta_slot) * ROWS;
         auto write_out = [&](int row, int d, float4 v, float lse2) {
@@ -649,10 +681,17 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
                 const float f = sm.l[w][row] == 0.f ? 0.f : exp2_fast(sm.m[w][row] - m), fv = f * sm.v[w];
                 const float4 x = *reinterpret_cast<const float4 *>(&sm.o[w][row][d]);
                 l += f * sm.l[w][row];
-                if (f != 0.f) { v.x += fv * x.x; v.y += fv * x.y; v.z += fv * x.z; v.w += fv * x.w; }
+                v.x += fv * x.x; v.y += fv * x.y; v.z += fv * x.z; v.w += fv * x.w;
             }
             const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m + log2f(l);
             v.x *= inv; v.y *= inv; v.z *= inv; v.w *= inv;
+            if (any_nan) {
+                const uint32_t nan = sm.nan[row][d / 32] >> (d % 32);
+                if (nan & 1) v.x = NAN;
+                if (nan & 2) v.y = NAN;
+                if (nan & 4) v.z = NAN;
+                if (nan & 8) v.w = NAN;
+            }
             if (whole) {
                 if (row < rows) write_out(row, d, v, lse2);
             } else {
@@ -713,6 +752,11 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
             }
         }
         __syncthreads();                          // the shared arrays are free again
+        if (any_nan) {
+            for (int i = tid; i < ROWS * (D / 32); i += kThreads) sm.nan[i / (D / 32)][i % (D / 32)] = 0;
+            if (tid == 0) sm.any_nan = 0;
+            __syncthreads();
+        }
     }
     if (extra == 0) return;
     // every CTA draws until one draw is past the end: after as many draws as there are, the counter is 0 again
