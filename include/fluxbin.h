@@ -574,8 +574,8 @@ fluxbin_status_t fluxbin_kv_read(const fluxbin_kv_cache_t *cache, int32_t dtype,
  *                   (tokens == batch).  Entries are clamped to [0, tokens].
  *   d_lengths       DEVICE int32 [batch]: cached tokens of each request, the new ones included.  0 (or less) leaves the
  *                   request's rows empty; a length past block_table_width * block_tokens, or 2^31 - 4096, is cut to that.
- *   d_block_table   DEVICE int32 [batch][block_table_stride]: block of tokens 0.., block_tokens.., ...; entries past the
- *                   length are not read; tokens of a block id outside the cache are masked out.
+ *   d_block_table   DEVICE int32 [batch][block_table_stride]: block of tokens 0.., block_tokens.., ...; a stride of 0 is one
+ *                   row for all requests, else it is at least the width; entries past the length are not read; tokens of a block id outside the cache are masked out.
  *   d_q, d_out      fp16 or bf16 heads; 16-byte aligned, strides multiples of 8 elements
  *   d_lse           DEVICE fp32 [tokens][q_heads] or NULL: log of the sum of exp(scale * q . k) (natural)
  * A row that sees nothing gets out = 0 and lse = -inf.  What lies in the cache past a request's length, or in tokens that a

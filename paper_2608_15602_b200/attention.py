@@ -54,6 +54,11 @@ def _int32(x: torch.Tensor, n: int, what: str) -> int:
     return x.data_ptr()
 
 
+def _row_stride(table: torch.Tensor) -> int:
+    """The stride between a block table's rows; that of a single row says nothing, and is not used."""
+    return table.stride(0) if table.shape[0] > 1 else table.shape[1]
+
+
 def _output(given: torch.Tensor | None, like: torch.Tensor, heads: int, what: str, stream):
     """An output like a [tokens][heads][dim] input: (tensor, pointer, token stride, head stride)."""
     if given is None:
@@ -218,7 +223,7 @@ class KVCache:
                scale: float | None = None, out: torch.Tensor | None = None, with_lse: bool = False, stream=None):
         """fluxbin_kv_attend: q [tokens][q_heads][head_dim] (fp16 or bf16) over the cached tokens of its requests.
 
-        `table` int32 [batch][max_blocks], `lengths` int32 [batch] (the new tokens included), `query_start` int32
+        `table` int32 [batch][max_blocks] (its rows may be one row expanded over the batch), `lengths` int32 [batch] (the new tokens included), `query_start` int32
         [batch + 1] or None for one token a request, `scale` head_dim ** -0.5 if not given.  Returns out [tokens][q_heads]
         [head_dim], with `with_lse` also the natural log of each row's sum, fp32 [tokens][q_heads]."""
         n, dt = q.shape[0], q.dtype
@@ -233,7 +238,7 @@ class KVCache:
         out, op, ot, os_ = _output(out, q, qh, "out", stream)
         lse = self._new((n, qh), torch.float32, stream) if with_lse else None
         fluxbin.kv_attend_call(self._ref, _TYPES[dt], B, n, qp, qh, qt, qs, 0 if query_start is None else _int32(query_start, B + 1, "query_start"),
-                               _int32(lengths, B, "lengths"), table.data_ptr(), max(table.stride(0), width), width,
+                               _int32(lengths, B, "lengths"), table.data_ptr(), _row_stride(table), width,
                                self._scale if scale is None else scale, op, ot, os_, 0 if lse is None else lse.data_ptr(), ws.tensor.data_ptr(),
                                ws.nbytes, _stream(stream))
         return (out, lse) if with_lse else out
@@ -246,13 +251,15 @@ class BlockTables:
     number of free blocks go in and come out."""
 
     def __init__(self, table: torch.Tensor, free: torch.Tensor, block_tokens: int):
-        if table.dtype is not torch.int32 or table.dim() != 2 or not table.is_cuda or (table.shape[1] > 1 and table.stride(1) != 1):
-            raise ValueError("table: a CUDA int32 tensor [batch][max_blocks] with contiguous rows is wanted")
+        if table.dtype is not torch.int32 or table.dim() != 2 or table.get_device() != _device() or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("table: an int32 tensor [batch][max_blocks] with contiguous rows on the current CUDA device is wanted")
+        if _row_stride(table) < table.shape[1]:
+            raise ValueError("table: rows that do not overlap are wanted (they are written)")
         self.table, self.free, self.block_tokens = table, free, block_tokens
         self._tokens = self._sets = None
         self._free = _int32(free, free.shape[0], "free")
         self.batch, self.max_blocks = table.shape
-        self._args = (table.data_ptr(), max(table.stride(0), table.shape[1]), table.shape[1], self._free, free.shape[0])
+        self._args = (table.data_ptr(), _row_stride(table), table.shape[1], self._free, free.shape[0])
 
     @classmethod
     def empty(cls, batch: int, max_blocks: int, num_blocks: int, block_tokens: int, device="cuda") -> "BlockTables":

@@ -843,7 +843,7 @@ extern "C" fluxbin_status_t fluxbin_kv_attend(const fluxbin_kv_cache_t *cache, i
     if (st != FLUXBIN_OK) return st;
     if (dtype != FLUXBIN_TYPE_FP16 && dtype != FLUXBIN_TYPE_BF16) return FLUXBIN_ERR_UNSUPPORTED;
     if (batch < 1 || tokens < 0 || q_heads < 1 || q_heads > 65535 || q_heads % cache->kv_heads != 0 || block_table_width < 1 ||
-        block_table_stride < block_table_width || (!d_query_start && tokens != batch) ||
+        (block_table_stride != 0 && block_table_stride < block_table_width) || (!d_query_start && tokens != batch) ||
         (int64_t)tokens * (q_heads / cache->kv_heads) > INT32_MAX) return FLUXBIN_ERR_RANGE;
     if (tokens == 0) return FLUXBIN_OK;
     if (!d_q || !d_out || !d_lengths || !d_block_table || !d_workspace) return FLUXBIN_ERR_NULL;

@@ -1,0 +1,93 @@
+"""What the torch wrapper of the attention side hands to the C calls, on CPU tensors: the calls are taken down in the place of
+being made (they go by addresses and sizes alone)."""
+import pytest
+
+from paper_2608_15602_b200 import build, fluxbin
+
+torch = pytest.importorskip("torch")
+build.build()
+from paper_2608_15602_b200 import attention as at  # noqa: E402
+
+CALLS = ("rotary_call", "kv_append_call", "kv_read_call", "kv_attend_call", "kv_advance_call")
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The words of every call that would have been made, by name; device -1 (the CPU's) counts as the current one."""
+    got = []
+    monkeypatch.setattr(at, "_device", lambda: -1)
+    monkeypatch.setattr(at, "_stream", lambda stream: 0)
+    for name in CALLS:
+        monkeypatch.setattr(fluxbin, name, lambda *words, name=name: got.append((name, words)))
+    return got
+
+
+class Scratch:
+    tensor, nbytes = torch.empty(1, dtype=torch.uint8), 1
+
+
+def ints(*shape):
+    return torch.zeros(shape, dtype=torch.int32)
+
+
+def attend(table, n=None):
+    c = at.KVCache(8, 16, 2, 64, device="cpu")
+    n = table.shape[0] if n is None else n
+    return c.attend(torch.zeros(n, 4, 64, dtype=torch.float16), table, ints(table.shape[0]), Scratch)
+
+
+def last_read(words):
+    """The last element of the table that the call's kernel may read: (batch - 1) * stride + width - 1."""
+    batch, stride, width = words[2], words[11], words[12]
+    return (batch - 1) * stride + width - 1
+
+
+def elements(t):
+    return t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+
+
+def test_the_rows_of_a_table_are_read_where_they_lie(calls):
+    wide = ints(4, 9)
+    for table in (ints(4, 5), wide[:, :5], wide[:, 3:8], ints(1, 5), wide[1:2, :5], ints(5)[None], wide[::2, :5]):
+        attend(table)
+        words = calls[-1][1]
+        assert words[11] == table.stride(0) or table.shape[0] == 1
+        assert words[11] >= words[12] and last_read(words) < elements(table)
+
+
+def test_one_row_for_all_requests(calls):
+    """Several samples of one prompt: a row expanded over the batch is read again for each, not past its end."""
+    row = ints(1, 5)
+    attend(row.expand(4, 5))
+    words = calls[-1][1]
+    assert words[11] == 0 and last_read(words) < elements(row)
+    attend(torch.as_strided(ints(1), (4, 1), (0, 1)))
+    assert calls[-1][1][11] == 0
+
+
+def test_overlapping_rows_are_handed_over_as_they_are(calls):
+    """(and refused by the call)"""
+    table = torch.as_strided(ints(20), (4, 8), (4, 1))
+    attend(table)
+    words = calls[-1][1]
+    assert words[11] == 4 and last_read(words) < 20
+
+
+def test_tables_that_advance_writes_have_rows_of_their_own(calls):
+    for table in (ints(1, 5).expand(4, 5), torch.as_strided(ints(20), (4, 8), (4, 1))):
+        with pytest.raises(ValueError, match="rows"):
+            at.BlockTables(table, ints(9), 16)
+    for table in (ints(4, 5), ints(4, 9)[:, :5], ints(1, 5), torch.as_strided(ints(5), (1, 5), (0, 1))):
+        b = table.shape[0]
+        at.BlockTables(table, ints(9), 16).advance(ints(b), ints(b), ints(1), 0)
+        batch, stride, width = calls[-1][1][0], *calls[-1][1][6:8]
+        assert stride >= width and (batch - 1) * stride + width <= elements(table)
+
+
+def test_strides_that_the_call_takes_and_refuses():
+    desc = fluxbin.CacheDesc(num_blocks=8, block_tokens=16, kv_heads=2, head_dim=64, format=0, d_k=1 << 20, d_v=1 << 21, block_stride=2048, head_stride=1024,
+                             token_stride=64, d_k_scale=1 << 22, d_v_scale=1 << 23)
+    import ctypes
+    P = 1 << 25
+    for stride, status in ((0, 5), (8, 5), (9, 5), (7, 3), (1, 3), (-8, 3)):                # 5: taken as far as the workspace, which is too small
+        assert fluxbin.kv_attend_status(ctypes.addressof(desc), 0, 2, 2, P, 4, 256, 64, None, P, P, stride, 8, 0.125, P, 256, 64, None, P, 16, None) == status
