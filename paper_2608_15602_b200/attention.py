@@ -35,6 +35,14 @@ def _stream(stream) -> int:
     return torch._C._cuda_getCurrentRawStream(_device()) if stream is None else _stream_ptr(stream)
 
 
+def _capturing(stream) -> bool:
+    """Whether a call on `stream` becomes part of a graph."""
+    if stream is None:
+        return torch._C._cuda_isCurrentStreamCapturing()
+    with torch.cuda.stream(stream):
+        return torch._C._cuda_isCurrentStreamCapturing()
+
+
 def _heads(x: torch.Tensor, tokens: int, dim: int, dtype: torch.dtype, what: str):
     """(pointer, heads, token stride, head stride) of a [tokens][heads][dim] tensor with contiguous heads."""
     if x.dtype is not dtype or x.dim() != 3 or x.get_device() != _device():
@@ -257,6 +265,7 @@ class BlockTables:
             raise ValueError("table: rows that do not overlap are wanted (they are written)")
         self.table, self.free, self.block_tokens = table, free, block_tokens
         self._tokens = self._sets = None
+        self._captured = []                              # sets that graphs write: as long as this object, whatever else it is asked
         self._free = _int32(free, free.shape[0], "free")
         self.batch, self.max_blocks = table.shape
         self._args = (table.data_ptr(), _row_stride(table), table.shape[1], self._free, free.shape[0])
@@ -270,17 +279,22 @@ class BlockTables:
     def advance(self, lengths: torch.Tensor, new_tokens: torch.Tensor, num_free: torch.Tensor, tokens: int, stream=None) -> SimpleNamespace:
         """One step: `new_tokens` int32 [batch] tokens to add (> 0) or drop (< 0), `tokens` the sum of those to add.  Returns
         lengths, num_free, granted, query_start, positions, slots, requests: int32 tensors that belong to this object, two
-        sets in turn, so that a step's outputs can be the next step's inputs; keep a copy of what has to live longer."""
+        sets in turn, so that a step's outputs can be the next step's inputs; keep a copy of what has to live longer.  A step
+        captured into a graph has a set of its own, which lives as long as this object."""
         B = self.batch
         lp, np_, fp = _int32(lengths, B, "lengths"), _int32(new_tokens, B, "new_tokens"), _int32(num_free, 1, "num_free")
         if self.table.get_device() != _device():
             raise ValueError("the tables have to lie on the current CUDA device")
-        if tokens != self._tokens:                       # (a decode loop keeps one size)
-            self._tokens, self._sets = tokens, [self._outputs(tokens), self._outputs(tokens)]
-        step, other = self._sets
-        self._sets = [other, step]
-        if step.first <= lp < step.last or step.first <= np_ < step.last or step.first <= fp < step.last:
-            step = self._sets[1] = self._outputs(tokens)  # an input of this step is an output of the last but one: keep that
+        if _capturing(stream):
+            step = self._outputs(tokens)
+            self._captured.append(step)
+        else:
+            if tokens != self._tokens:                   # (a decode loop keeps one size)
+                self._tokens, self._sets = tokens, [self._outputs(tokens), self._outputs(tokens)]
+            step, other = self._sets
+            self._sets = [other, step]
+            if step.first <= lp < step.last or step.first <= np_ < step.last or step.first <= fp < step.last:
+                step = self._sets[1] = self._outputs(tokens)  # an input of this step is an output of the last but one: keep that
         fluxbin.kv_advance_call(B, tokens, self.block_tokens, lp, np_, *self._args, fp, *step.pointers, _stream(stream))
         return step
 

@@ -17,6 +17,7 @@ def calls(monkeypatch):
     got = []
     monkeypatch.setattr(at, "_device", lambda: -1)
     monkeypatch.setattr(at, "_stream", lambda stream: 0)
+    monkeypatch.setattr(at, "_capturing", lambda stream: False, raising=False)
     for name in CALLS:
         monkeypatch.setattr(fluxbin, name, lambda *words, name=name: got.append((name, words)))
     return got
@@ -91,3 +92,29 @@ def test_strides_that_the_call_takes_and_refuses():
     P = 1 << 25
     for stride, status in ((0, 5), (8, 5), (9, 5), (7, 3), (1, 3), (-8, 3)):                # 5: taken as far as the workspace, which is too small
         assert fluxbin.kv_attend_status(ctypes.addressof(desc), 0, 2, 2, P, 4, 256, 64, None, P, P, stride, 8, 0.125, P, 256, 64, None, P, 16, None) == status
+
+
+def outputs(words):
+    """The addresses that an advance writes besides its tables: num_free, lengths, granted, query_start, positions, slots, requests."""
+    return words[11:18]
+
+
+def test_a_captured_step_keeps_its_outputs(calls, monkeypatch):
+    """A graph holds the addresses of a step's outputs, and nobody else may: neither another size of step nor the steps outside
+    the graph may get that memory, and it may not go back to the allocator."""
+    B, T = 3, 5
+    t = at.BlockTables(ints(B, 4), ints(9), 16)
+    inputs = ints(B), ints(B), ints(1)
+    t.advance(*inputs, T)                                 # the warm-up before a capture
+    monkeypatch.setattr(at, "_capturing", lambda stream: True)
+    for _ in range(2):
+        t.advance(*inputs, T)                             # (the captured function keeps nothing)
+    monkeypatch.setattr(at, "_capturing", lambda stream: False)
+    sizes = (1, B, B, B + 1, T, T, T)
+    held = [(p, p + 4 * n) for _, words in calls[-2:] for p, n in zip(outputs(words), sizes)]
+    for tokens in (T, T, 7, 7, T, T):
+        t.advance(*inputs, tokens)
+        assert not any(lo <= p < hi for p in outputs(calls[-1][1]) for lo, hi in held)
+    others = [torch.full((sum(sizes),), 7, dtype=torch.int32) for _ in range(2000)]
+    assert not any(lo <= o.data_ptr() < hi for o in others for lo, hi in held)
+    assert len({lo for lo, _ in held}) == len(held)
