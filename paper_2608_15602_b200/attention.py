@@ -8,6 +8,10 @@ over it and the block tables both go by.  torch owns the memory and the stream, 
     step = tables.advance(lengths, new_tokens, num_free, tokens)          # blocks, positions and slots of the new tokens
     q = cache.append(k, v, step.slots, rotary=rope, positions=step.positions, q=q)
     out = cache.attend(q, tables.table, step.lengths, ws, query_start=step.query_start)
+
+`stream` (a torch stream, else the current one): what a call allocates comes from that stream's memory, so nothing queued
+elsewhere still uses it, and is recorded on the current stream too, so it may be dropped there.  The tensors given to the call
+have to be ready on `stream` and are the caller's to keep until it is through, as with any torch call on another stream.
 """
 from __future__ import annotations
 
@@ -43,6 +47,16 @@ def _capturing(stream) -> bool:
         return torch._C._cuda_isCurrentStreamCapturing()
 
 
+def _made(stream, make):
+    """The new tensor make() for a call on `stream`."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        y = make()
+    y.record_stream(torch.cuda.current_stream())
+    return y
+
+
 def _heads(x: torch.Tensor, tokens: int, dim: int, dtype: torch.dtype, what: str):
     """(pointer, heads, token stride, head stride) of a [tokens][heads][dim] tensor with contiguous heads."""
     if x.dtype is not dtype or x.dim() != 3 or x.get_device() != _device():
@@ -70,9 +84,7 @@ def _row_stride(table: torch.Tensor) -> int:
 def _output(given: torch.Tensor | None, like: torch.Tensor, heads: int, what: str, stream):
     """An output like a [tokens][heads][dim] input: (tensor, pointer, token stride, head stride)."""
     if given is None:
-        y = torch.empty_like(like)
-        if stream is not None:                   # made on the current stream, written on another
-            y.record_stream(stream)
+        y = _made(stream, lambda: torch.empty_like(like))
         st, sh, _ = y.stride()
         return y, y.data_ptr(), st, sh
     y = given
@@ -175,10 +187,7 @@ class KVCache:
         last = self._last.get(dtype)
         if last is None or last.shape != shape:
             last = self._last[dtype] = torch.empty((1,) * len(shape), dtype=dtype, device=self.device).expand(shape)
-        new = torch.empty_like(last, memory_format=torch.contiguous_format)
-        if stream is not None:
-            new.record_stream(stream)
-        return new
+        return _made(stream, lambda: torch.empty_like(last, memory_format=torch.contiguous_format))
 
     def append(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, rotary: Rotary | None = None,
                positions: torch.Tensor | None = None, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None, stream=None):
@@ -286,26 +295,29 @@ class BlockTables:
         if self.table.get_device() != _device():
             raise ValueError("the tables have to lie on the current CUDA device")
         if _capturing(stream):
-            step = self._outputs(tokens)
+            step = self._outputs(tokens, stream)
             self._captured.append(step)
         else:
             if tokens != self._tokens:                   # (a decode loop keeps one size)
-                self._tokens, self._sets = tokens, [self._outputs(tokens), self._outputs(tokens)]
+                self._tokens, self._sets = tokens, [self._outputs(tokens, stream), self._outputs(tokens, stream)]
             step, other = self._sets
             self._sets = [other, step]
             if step.first <= lp < step.last or step.first <= np_ < step.last or step.first <= fp < step.last:
-                step = self._sets[1] = self._outputs(tokens)  # an input of this step is an output of the last but one: keep that
-        fluxbin.kv_advance_call(B, tokens, self.block_tokens, lp, np_, *self._args, fp, *step.pointers, _stream(stream))
+                step = self._sets[1] = self._outputs(tokens, stream)  # an input of this step is an output of the last but one: keep that
+        on = _stream(stream)
+        if on != step.made_on:                           # a set may be dropped while another stream still writes it
+            step.num_free.record_stream(torch.cuda.current_stream() if stream is None else stream)
+        fluxbin.kv_advance_call(B, tokens, self.block_tokens, lp, np_, *self._args, fp, *step.pointers, on)
         return step
 
-    def _outputs(self, tokens: int) -> SimpleNamespace:
+    def _outputs(self, tokens: int, stream) -> SimpleNamespace:
         B = self.batch
         sizes = (1, B, B, B + 1, tokens, tokens, tokens)
-        parts = torch.empty(sum(sizes), dtype=torch.int32, device=self.table.device).split(sizes)
+        parts = _made(stream, lambda: torch.empty(sum(sizes), dtype=torch.int32, device=self.table.device)).split(sizes)
         step = SimpleNamespace(**dict(zip(("num_free", "lengths", "granted", "query_start", "positions", "slots", "requests"), parts)))
         first = parts[0].data_ptr()
         step.pointers = tuple(first + 4 * sum(sizes[:i]) for i in range(7))
-        step.first, step.last = first, first + 4 * sum(sizes)
+        step.first, step.last, step.made_on = first, first + 4 * sum(sizes), _stream(stream)
         return step
 
 

@@ -118,3 +118,75 @@ def test_a_captured_step_keeps_its_outputs(calls, monkeypatch):
     others = [torch.full((sum(sizes),), 7, dtype=torch.int32) for _ in range(2000)]
     assert not any(lo <= o.data_ptr() < hi for o in others for lo, hi in held)
     assert len({lo for lo, _ in held}) == len(held)
+
+
+class FakeStream:
+    cuda_stream = 5
+
+
+@pytest.fixture
+def memory(calls, monkeypatch):
+    """Allocations as (stream that was current, tensor), and (tensor's address, stream) of every record_stream."""
+    current, made, recorded = ["the current one"], [], []
+
+    class Under:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            current.append(self.stream)
+
+        def __exit__(self, *_):
+            current.pop()
+
+    def taken_down(make):
+        def f(*a, **k):
+            y = make(*a, **k)
+            made.append((current[-1], y))
+            return y
+        return f
+
+    monkeypatch.setattr(torch.cuda, "stream", Under)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *_: current[-1])
+    monkeypatch.setattr(at, "_stream", lambda stream: 0 if stream is None and current[-1] == "the current one" else 5)
+    monkeypatch.setattr(torch, "empty", taken_down(torch.empty))
+    monkeypatch.setattr(torch, "empty_like", taken_down(torch.empty_like))
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, s: recorded.append((self.untyped_storage().data_ptr(), s)), raising=False)
+    return made, recorded
+
+
+def test_what_a_call_on_another_stream_allocates_is_that_streams(memory):
+    """Memory of the current stream may still be in use there when the other stream writes it."""
+    made, recorded = memory
+    s = FakeStream()
+    c, r = at.KVCache(8, 16, 2, 64, device="cpu"), at.Rotary(64, device="cpu")
+    t = at.BlockTables(ints(3, 4), ints(9), 16)
+    q, k = torch.zeros(3, 4, 64, dtype=torch.float16), torch.zeros(3, 2, 64, dtype=torch.float16)
+    for what in (lambda: r.apply(q, k, ints(3), stream=s), lambda: c.append(k, k, ints(3), rotary=r, positions=ints(3), q=q, stream=s)[None],
+                 lambda: c.read(ints(3), stream=s), lambda: c.attend(q, t.table, ints(3), Scratch, with_lse=True, stream=s),
+                 lambda: [t.advance(ints(3), ints(3), ints(1), 3, stream=s).slots], lambda: [t.advance(ints(3), ints(3), ints(1), 4, stream=s).slots]):
+        made.clear()
+        recorded.clear()
+        results = what()
+        storages = {y.untyped_storage().data_ptr(): stream for stream, y in made}
+        for y in results:
+            assert storages[y.untyped_storage().data_ptr()] is s
+            assert (y.untyped_storage().data_ptr(), "the current one") in recorded
+    for what in (lambda: r.apply(q, k, ints(3)), lambda: c.read(ints(3)), lambda: c.attend(q, t.table, ints(3), Scratch, with_lse=True)):
+        made.clear()
+        recorded.clear()
+        what()
+        assert all(stream == "the current one" for stream, _ in made) and not recorded
+
+
+def test_a_set_of_outputs_written_on_another_stream_is_recorded_there(memory):
+    made, recorded = memory
+    s = FakeStream()
+    t = at.BlockTables(ints(3, 4), ints(9), 16)
+    t.advance(ints(3), ints(3), ints(1), 3)               # both sets are the current stream's
+    assert not recorded
+    step = t.advance(ints(3), ints(3), ints(1), 3, stream=s)
+    assert recorded == [(step.slots.untyped_storage().data_ptr(), s)]
+    with torch.cuda.stream(s):
+        step = t.advance(ints(3), ints(3), ints(1), 3)
+    assert recorded[1:] == [(step.slots.untyped_storage().data_ptr(), s)]

@@ -57,3 +57,35 @@ def test_a_captured_step_and_steps_of_other_sizes(at):  # noqa: F811
     used = t.table.cpu().numpy()
     held = [b for r, n in enumerate(s.lengths.tolist()) for b in used[r, :-(-n // bs)]]
     assert len(set(held)) == len(held) == 24 - int(s.num_free[0])
+
+
+def test_calls_on_a_stream_of_their_own_while_the_current_one_is_busy(at):  # noqa: F811
+    """The current stream still has to read tensors that were dropped: what a call on another stream allocates is not theirs."""
+    B, Hq, H, D, bs = 6, 8, 2, 64, 16
+    c, plain = at.KVCache(40, bs, H, D), at.KVCache(40, bs, H, D)
+    r = at.Rotary(D)
+    tables, other = at.BlockTables.empty(B, 4, 40, bs), at.BlockTables.empty(B, 4, 40, bs)
+    ws, ws2 = c.workspace(B, B, Hq), plain.workspace(B, B, Hq)
+    q, k, v = normal(1, (B, Hq, D), "fp16"), normal(2, (B, H, D), "fp16"), normal(3, (B, H, D), "fp16")
+    lengths, ones, nf = dev([0] * B), dev([1] * B), dev([40])
+    s = torch.cuda.Stream()
+
+    def step(c, tables, ws, **kw):
+        st = tables.advance(lengths, ones, nf, B, **kw)
+        qr = c.append(k, v, st.slots, rotary=r, positions=st.positions, q=q, **kw)
+        qk = r.apply(q, k, st.positions, **kw)
+        out = c.attend(qr, tables.table, st.lengths, ws, query_start=st.query_start, with_lse=True, **kw)
+        return [st.lengths, st.slots, qr, *qk, *out, *c.read(st.slots, **kw)]
+
+    want = step(plain, other, ws2)
+    sizes = [w.numel() * w.element_size() for w in want] + [4 * (2 + 3 * B + 3 * B)]
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)                        # about a tenth of a second
+    dropped = [torch.full((n,), 9, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(4)]
+    copies = [d.clone() for d in dropped]
+    del dropped
+    got = step(c, tables, ws, stream=s)
+    torch.cuda.synchronize()
+    assert all((x == 9).all() for x in copies)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
