@@ -7,7 +7,7 @@ using namespace fbd;
 
 namespace {
 
-constexpr int kMaxBatch = 8192;
+constexpr int kMaxBatch = 8192, kWarpSums = 3 * 32;
 constexpr unsigned kMany = 0xffffffffu;         // sums stay there once they get there: past every size
 
 struct Args {
@@ -59,9 +59,9 @@ __device__ __forceinline__ int first_above(const unsigned *sums, int n, unsigned
 // where its last owner's table has it, not from the free list that another CTA is writing.
 __global__ void __launch_bounds__(1024) advance_kernel(const __grid_constant__ Args a)
 {
-    extern __shared__ unsigned sums[];           // [3][batch], including the request itself
-    __shared__ unsigned warp_sum[3][32];
-    unsigned *gone = sums, *need = sums + a.batch, *count = sums + 2 * a.batch;
+    extern __shared__ unsigned sums[];           // [3][32] of the warps, then [3][batch], including the request itself
+    unsigned (&warp_sum)[3][32] = *reinterpret_cast<unsigned (*)[3][32]>(sums);
+    unsigned *gone = sums + kWarpSums, *need = gone + a.batch, *count = need + a.batch;
     const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, warp = tid >> 5;
     let_successor_start();
     wait_for_predecessor();
@@ -177,14 +177,14 @@ extern "C" fluxbin_status_t fluxbin_kv_advance(int32_t batch, int32_t tokens, in
     // 19.1, 8000 63 against 29)
     const int threads = batch <= 2048 ? 256 : 1024;
     const int64_t ctas = ((int64_t)tokens + threads - 1) / threads;
-    const size_t smem = (size_t)batch * 3 * sizeof(unsigned);
+    const size_t smem = ((size_t)batch * 3 + kWarpSums) * sizeof(unsigned);
     if (smem > 48 * 1024) {
         static std::atomic<bool> opted[fb::kMaxDevices];
         int dev = 0;
         FBD_CUDA(cudaGetDevice(&dev));
         if (dev < 0 || dev >= fb::kMaxDevices) return FLUXBIN_ERR_UNSUPPORTED;
         if (!opted[dev].load(std::memory_order_relaxed)) {
-            FBD_CUDA(cudaFuncSetAttribute(advance_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxBatch * 3 * (int)sizeof(unsigned)));
+            FBD_CUDA(cudaFuncSetAttribute(advance_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (kMaxBatch * 3 + kWarpSums) * (int)sizeof(unsigned)));
             opted[dev].store(true, std::memory_order_relaxed);
         }
     }
