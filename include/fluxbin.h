@@ -571,7 +571,8 @@ fluxbin_status_t fluxbin_kv_read(const fluxbin_kv_cache_t *cache, int32_t dtype,
  *
  *   d_query_start   DEVICE int32 [batch + 1], ascending: request r asks with tokens query_start[r] ..
  *                   query_start[r + 1] - 1 of q, which are its last ones (already appended).  NULL: one token a request
- *                   (tokens == batch).  Entries are clamped to [0, tokens].
+ *                   (tokens == batch).  Entries are clamped to [0, tokens]; a token before the first entry or from the
+ *                   last one on is no request's, and its rows are empty.
  *   d_lengths       DEVICE int32 [batch]: cached tokens of each request, the new ones included.  0 (or less) leaves the
  *                   request's rows empty; a length past block_table_width * block_tokens, or 2^31 - 4096, is cut to that.
  *   d_block_table   DEVICE int32 [batch][block_table_stride]: block of tokens 0.., block_tokens.., ...; a stride of 0 is one
@@ -613,7 +614,8 @@ fluxbin_status_t fluxbin_kv_attend(const fluxbin_kv_cache_t *cache, int32_t dtyp
  * A request that grows is granted its blocks if those of all growing requests up to and including it fit into the free
  * list (one that needs no further block always is), and its table has room for them; a request whose table has no room
  * is left out of that count.  A request that is not granted keeps its length, and its tokens get slot -1 (and are
- * skipped by fluxbin_kv_append).  A length that does not fit the table's width gives nothing back.
+ * skipped by fluxbin_kv_append) but keep their places among the new tokens, d_query_start included: what fluxbin_kv_attend
+ * answers there is what the request's last cached tokens see, and of no use; d_granted says whose rows those are.  A length that does not fit the table's width gives nothing back.
  *
  *   d_num_free_out, d_lengths_out, d_granted   int32 [1], [batch], [batch] (0 or 1)
  *   d_query_start                              int32 [batch + 1]: first token of each request among the new ones

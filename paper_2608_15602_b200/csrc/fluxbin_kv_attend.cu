@@ -236,6 +236,19 @@ template <int D, int ROWS, int WARPS, int STAGES, bool QSHARED> struct Shared {
     uint32_t nan[ROWS][D / 32];                          // elements of this job's rows that see a NaN (see hide_nan)
 };
 
+// the rows of tokens that are no request's
+template <int D, typename T> __device__ __noinline__ void empty_rows(const Args &a, int tid, int threads)
+{
+    const int from = min(max(a.query_start[0], 0), a.tokens), to = min(max(a.query_start[a.batch], from), a.tokens), n = a.tokens - (to - from);
+    if (n == 0) return;
+    for (long long i = (long long)blockIdx.x * threads + tid; i < (long long)n * a.q_heads * (D / 4); i += (long long)gridDim.x * threads) {
+        const int row = (int)(i / (D / 4)), nth = row / a.q_heads, h = row % a.q_heads, d = (int)(i % (D / 4)) * 4;
+        const long long t = nth < from ? nth : nth + (to - from);
+        *reinterpret_cast<uint2 *>((T *)a.out + t * a.out_token + h * a.out_head + d) = make_uint2(0, 0);
+        if (d == 0 && a.lse) a.lse[t * a.q_heads + h] = -INFINITY;
+    }
+}
+
 // one CTA: its part of the line, job after job
 template <int D, int FMT, int NT, typename T>
 __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) attend_kernel(const __grid_constant__ Args a)
@@ -256,6 +269,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
 
     let_successor_start();
     wait_for_predecessor();
+
+    if (a.query_start) empty_rows<D, T>(a, tid, kThreads);
 
     // ---- where this CTA's part begins: a sum over the requests, each thread over a run of them
     const int per = (a.batch + kThreads - 1) / kThreads, r_lo = min(tid * per, a.batch), r_hi = min(r_lo + per, a.batch);

@@ -89,3 +89,40 @@ def test_calls_on_a_stream_of_their_own_while_the_current_one_is_busy(at):  # no
     assert all((x == 9).all() for x in copies)
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("Hq,H,D,dtype", [(8, 2, 64, "fp16"), (16, 1, 128, "bf16"), (4, 4, 256, "fp16"), (40, 1, 128, "fp16")])
+@pytest.mark.parametrize("before,after", [(0, 3), (2, 0), (1, 700), (0, 0)])
+def test_tokens_of_no_request_get_empty_rows(at, Hq, H, D, dtype, before, after):  # noqa: F811
+    lengths, new = [40, 3, 90], [1, 2, 0]
+    c, table = setup(at, "int8", 16, H, D, lengths, 4)
+    starts = before + np.concatenate([[0], np.cumsum(new)])
+    n = before + 3 + after
+    q = normal(71, (n, Hq, D), dtype)
+    out = torch.full((Hq, n, D), float("nan"), dtype=q.dtype, device="cuda").transpose(0, 1)
+    ws = c.workspace(3, n, Hq)
+    _, lse = c.attend(q, dev(table), dev(lengths), ws, query_start=dev(starts), out=out, with_lse=True)
+    check_attend(c, q, table, lengths, starts, D ** -0.5, out, lse, dtype)        # (the definition's rows of no request: 0 and -inf)
+    nobody = torch.ones(n, dtype=torch.bool)
+    nobody[before:before + 3] = False
+    assert (out[nobody] == 0).all() and (lse[nobody] == float("-inf")).all()
+    # no request asks at all
+    out.fill_(float("nan"))
+    _, lse = c.attend(q, dev(table), dev(lengths), ws, query_start=dev([n] * 4 if before else [0] * 4), out=out, with_lse=True)
+    assert (out == 0).all() and (lse == float("-inf")).all()
+
+
+def test_a_block_with_room_for_more_tokens_than_there_are(at):  # noqa: F811
+    """A graph's fixed number of tokens: rows past the last request's come out as the output projection of 0."""
+    from paper_2608_15602_b200 import layer, synth
+    hq, hk, dim, hidden, B, T, room = 4, 2, 64, 128, 2, 5, 9
+    L = [synth.make_linear(5, i, M, N) for i, (M, N) in enumerate([(hq * dim, hidden), (hk * dim, hidden), (hk * dim, hidden), (hidden, hq * dim)])]
+    rows = []
+    for n in (T, room):
+        block = at.AttentionBlock(*[layer.FluxBinLinear(x) for x in L], at.KVCache(8, 16, hk, dim), at.Rotary(dim))
+        tables = at.BlockTables.empty(B, 4, 8, 16)
+        buf = block.buffers(B, n)
+        buf.x.copy_(normal(81, (room, hidden), "fp16")[:n])
+        buf.a.fill_(float("nan"))
+        rows.append(block.forward(buf, tables, tables.advance(dev([0] * B), dev([3, 2]), dev([8]), n)).clone())
+    assert torch.equal(rows[0], rows[1][:T]) and (rows[1][T:] == 0).all()
