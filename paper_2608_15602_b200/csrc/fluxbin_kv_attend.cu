@@ -687,19 +687,23 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
         };
         for (int i = tid; i < ROWS * (D / 4); i += kThreads) {
             const int row = i / (D / 4), d = i % (D / 4) * 4;
-            float m = -INFINITY, l = 0.f;
+            float m = -INFINITY, l = 0.f, f[kWarps];
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) m = fmaxf(m, sm.m[w][row]);
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {           // a warp without tokens has l = 0; a NaN in l stays
-                const float f = sm.l[w][row] == 0.f ? 0.f : exp2_fast(sm.m[w][row] - m), fv = f * sm.v[w];
-                const float4 x = *reinterpret_cast<const float4 *>(&sm.o[w][row][d]);
-                l += f * sm.l[w][row];
-                v.x += fv * x.x; v.y += fv * x.y; v.z += fv * x.z; v.w += fv * x.w;
+                f[w] = sm.l[w][row] == 0.f ? 0.f : exp2_fast(sm.m[w][row] - m);
+                l += f[w] * sm.l[w][row];
             }
             const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m + log2f(l);
-            v.x *= inv; v.y *= inv; v.z *= inv; v.w *= inv;
+            // (divided before the value scale comes in: the mean is no larger than the values, the sums are)
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float fv = f[w] * sm.v[w];
+                const float4 x = *reinterpret_cast<const float4 *>(&sm.o[w][row][d]);
+                v.x += fv * (x.x * inv); v.y += fv * (x.y * inv); v.z += fv * (x.z * inv); v.w += fv * (x.w * inv);
+            }
             if (any_nan) {
                 const uint32_t nan = sm.nan[row][d / 32] >> (d % 32);
                 if (nan & 1) v.x = NAN;
@@ -752,7 +756,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
 #pragma unroll
                     for (int k = 0; k < kEach; ++k) {
                         const int i = min(tid + k * kThreads, kItems - 1), row = i / (D / 4);
-                        const float f = exp2_fast(__ldcg(a.partial_lse + slot_of(c) * ROWS + row) - sm.join_max[row]);
+                        const float f = exp2_fast(__ldcg(a.partial_lse + slot_of(c) * ROWS + row) - sm.join_max[row]) * sm.join_inv[row];
                         const float4 y = __ldcg(reinterpret_cast<const float4 *>(a.partial + slot_of(c) * (ROWS * D)) + i);
                         v[k].x += f * y.x; v[k].y += f * y.y; v[k].z += f * y.z; v[k].w += f * y.w;
                     }
@@ -760,8 +764,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
                 for (int k = 0; k < kEach; ++k) {
                     const int i = tid + k * kThreads, row = i / (D / 4);
                     if (i >= kItems || row >= rows) continue;
-                    const float inv = sm.join_inv[row];
-                    write_out(row, i % (D / 4) * 4, make_float4(v[k].x * inv, v[k].y * inv, v[k].z * inv, v[k].w * inv), sm.join_lse[row]);
+                    write_out(row, i % (D / 4) * 4, v[k], sm.join_lse[row]);
                 }
                 if (tid == 0) a.arrived[c0] = 0;
             }

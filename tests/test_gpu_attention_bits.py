@@ -120,3 +120,19 @@ def test_the_smallest_e4m3_entries(at):  # noqa: F811
     q = normal(52, (1, Hq, D), "fp16")
     out = c.attend(q, dev(table), dev([L]), c.workspace(1, 1, Hq))
     check(c, q, table, [L], [0, 1], D ** -0.5, out, "fp16")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("L", [20, 3000])
+@pytest.mark.parametrize("size", [2.0 ** 100, 2.0 ** 126, 2.0 ** -80])
+@pytest.mark.parametrize("Hq,H,D,new", ROWS)
+def test_values_near_the_ends_of_the_range(at, Hq, H, D, new, L, size, fmt):  # noqa: F811
+    """A weighted mean is no larger than its values, so bf16 holds it whatever the sums on the way are."""
+    c, table = flat(at, fmt, H, D, 16, L, 12)
+    c.v_scale.fill_(size / 128)                           # entries up to 100
+    c.k_scale.fill_(0.01)
+    rng = np.random.default_rng(13)
+    c.k.copy_(torch.from_numpy(rng.integers(-100, 101, c.k.shape).astype(np.float32)).cuda().to(c.k.dtype))
+    q = normal(53, (new, Hq, D), "bf16")
+    out = c.attend(q, dev(table), dev([L]), c.workspace(1, new, Hq), query_start=dev([0, new]))
+    check(c, q, table, [L], [0, new], D ** -0.5, out, "bf16")
