@@ -527,7 +527,7 @@ fluxbin_status_t fluxbin_rotary(const fluxbin_rotary_t *rotary, int32_t dtype, i
 typedef struct {
     int32_t num_blocks, block_tokens, kv_heads, head_dim, format;
     void *d_k, *d_v;                                        /* DEVICE, 16-byte aligned */
-    int64_t block_stride, head_stride, token_stride;        /* multiples of 16 */
+    int64_t block_stride, head_stride, token_stride;        /* multiples of 16 (that of an axis of one: any) */
     float *d_k_scale, *d_v_scale;                           /* DEVICE [num_blocks][kv_heads] */
 } fluxbin_kv_cache_t;
 #define FLUXBIN_CACHE_INT8 0
@@ -577,7 +577,7 @@ fluxbin_status_t fluxbin_kv_read(const fluxbin_kv_cache_t *cache, int32_t dtype,
  *                   request's rows empty; a length past block_table_width * block_tokens, or 2^31 - 4096, is cut to that.
  *   d_block_table   DEVICE int32 [batch][block_table_stride]: block of tokens 0.., block_tokens.., ...; a stride of 0 is one
  *                   row for all requests, else it is at least the width; entries past the length are not read; tokens of a block id outside the cache are masked out.
- *   d_q, d_out      fp16 or bf16 heads; 16-byte aligned, strides multiples of 8 elements
+ *   d_q, d_out      fp16 or bf16 heads; 16-byte aligned, strides multiples of 8 elements (that of one token or head: any)
  *   d_lse           DEVICE fp32 [tokens][q_heads] or NULL: log of the sum of exp(scale * q . k) (natural)
  * A row that sees nothing gets out = 0 and lse = -inf.  What lies in the cache past a request's length, or in tokens that a
  * row does not see (NaN patterns and NaN scales included), has no influence on it.  Scores, maxima, sums and accumulators are

@@ -164,7 +164,7 @@ class KVCache:
     def _set(self, k, v, k_scale, v_scale):
         if k.dtype not in _STORED or v.dtype is not k.dtype:
             raise TypeError("k, v: int8 or float8_e4m3fn is wanted")
-        if k.dim() != 4 or v.shape != k.shape or v.stride() != k.stride() or k.stride(3) != 1:
+        if k.dim() != 4 or v.shape != k.shape or any(a != b for a, b, n in zip(k.stride(), v.stride(), k.shape) if n > 1) or k.stride(3) != 1:
             raise ValueError("k, v: [num_blocks][kv_heads][block_tokens][head_dim] with the same strides and contiguous elements are wanted")
         nb, H, bs, D = k.shape
         for s in (k_scale, v_scale):

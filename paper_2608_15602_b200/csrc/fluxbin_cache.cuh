@@ -17,7 +17,8 @@ inline fluxbin_status_t check_cache(const fluxbin_kv_cache_t *c)
     if (c->block_tokens % 16 != 0 || c->block_tokens > 1024) return FLUXBIN_ERR_UNSUPPORTED;
     if ((int64_t)c->num_blocks * c->block_tokens > INT32_MAX) return FLUXBIN_ERR_RANGE;
     if (!aligned_to(c->d_k, 16) || !aligned_to(c->d_v, 16) || !aligned_to(c->d_k_scale, 4) || !aligned_to(c->d_v_scale, 4)) return FLUXBIN_ERR_ALIGNMENT;
-    if (c->block_stride % 16 || c->head_stride % 16 || c->token_stride % 16) return FLUXBIN_ERR_ALIGNMENT;
+    // (the stride of an axis of one is never used)
+    if ((c->num_blocks > 1 && c->block_stride % 16) || (c->kv_heads > 1 && c->head_stride % 16) || c->token_stride % 16) return FLUXBIN_ERR_ALIGNMENT;
     // entries do not overlap: sorted by size, each stride covers what the smaller ones span
     int64_t s[3] = {c->block_stride, c->head_stride, c->token_stride}, n[3] = {c->num_blocks, c->kv_heads, c->block_tokens};
     for (int i = 0; i < 2; ++i)
@@ -25,7 +26,7 @@ inline fluxbin_status_t check_cache(const fluxbin_kv_cache_t *c)
             if (s[j] > s[j + 1]) { int64_t t = s[j]; s[j] = s[j + 1]; s[j + 1] = t; t = n[j]; n[j] = n[j + 1]; n[j + 1] = t; }
     int64_t span = c->head_dim;
     for (int i = 0; i < 3; ++i) {
-        if (n[i] == 1) continue;                     // the stride of an axis of one is never used
+        if (n[i] == 1) continue;
         if (s[i] < span || s[i] > (int64_t)1 << 44) return FLUXBIN_ERR_RANGE;
         span = s[i] * (n[i] - 1) + span;
     }

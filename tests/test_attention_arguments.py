@@ -1,5 +1,7 @@
 """What the torch wrapper of the attention side hands to the C calls, on CPU tensors: the calls are taken down in the place of
 being made (they go by addresses and sizes alone)."""
+import ctypes
+
 import pytest
 
 from paper_2608_15602_b200 import build, fluxbin
@@ -85,13 +87,41 @@ def test_tables_that_advance_writes_have_rows_of_their_own(calls):
         assert stride >= width and (batch - 1) * stride + width <= elements(table)
 
 
+P = 1 << 25
+
+
+def a_cache(**kw):
+    d = dict(num_blocks=8, block_tokens=16, kv_heads=2, head_dim=64, format=0, d_k=1 << 20, d_v=1 << 21, block_stride=2048, head_stride=1024,
+             token_stride=64, d_k_scale=1 << 22, d_v_scale=1 << 23)
+    d.update(kw)
+    return fluxbin.CacheDesc(**d)
+
+
+def attend_status(cache=None, batch=2, tokens=2, heads=4, q=(256, 64), out=(256, 64), stride=8):
+    """5 for what is taken as far as the workspace, which is too small."""
+    cache = cache or a_cache()
+    return fluxbin.kv_attend_status(ctypes.addressof(cache), 0, batch, tokens, P, heads, *q, None, P, P, stride, 8, 0.125, P, *out, None, P, 16, None)
+
+
 def test_strides_that_the_call_takes_and_refuses():
-    desc = fluxbin.CacheDesc(num_blocks=8, block_tokens=16, kv_heads=2, head_dim=64, format=0, d_k=1 << 20, d_v=1 << 21, block_stride=2048, head_stride=1024,
-                             token_stride=64, d_k_scale=1 << 22, d_v_scale=1 << 23)
-    import ctypes
-    P = 1 << 25
     for stride, status in ((0, 5), (8, 5), (9, 5), (7, 3), (1, 3), (-8, 3)):                # 5: taken as far as the workspace, which is too small
-        assert fluxbin.kv_attend_status(ctypes.addressof(desc), 0, 2, 2, P, 4, 256, 64, None, P, P, stride, 8, 0.125, P, 256, 64, None, P, 16, None) == status
+        assert attend_status(stride=stride) == status
+
+
+def test_the_stride_of_an_axis_of_one_is_not_looked_at():
+    one = a_cache(kv_heads=1)
+    for kw, status in ((dict(q=(260, 64)), 6), (dict(out=(260, 64)), 6), (dict(q=(256, 65)), 6), (dict(out=(256, 65)), 6),
+                       (dict(batch=1, tokens=1, q=(261, 64)), 5), (dict(batch=1, tokens=1, out=(0, 64)), 5), (dict(cache=one, heads=1, q=(64, 3)), 5),
+                       (dict(cache=one, heads=1, out=(64, 1)), 5), (dict(cache=one, batch=1, tokens=1, heads=1, q=(1, 1), out=(1, 1)), 5)):
+        assert attend_status(**kw) == status, kw
+    for kw in (dict(num_blocks=1, block_stride=1), dict(kv_heads=1, head_stride=7), dict(num_blocks=1, kv_heads=1, block_stride=3, head_stride=5)):
+        assert fluxbin.kv_validate_status(a_cache(**kw)) == 0, kw
+    k = torch.zeros(1, 2, 16, 64, dtype=torch.int8)
+    v = torch.as_strided(torch.zeros(4096, dtype=torch.int8), (1, 2, 16, 64), (9, 1024, 64, 1))
+    s = torch.zeros(1, 2)
+    assert at.KVCache.wrap(k, v, s, s.clone()).num_blocks == 1
+    with pytest.raises(ValueError):
+        at.KVCache.wrap(torch.zeros(2, 2, 16, 64, dtype=torch.int8), torch.zeros(2, 16, 2, 64, dtype=torch.int8).transpose(1, 2), torch.zeros(2, 2), torch.zeros(2, 2))
 
 
 def outputs(words):

@@ -126,3 +126,27 @@ def test_a_block_with_room_for_more_tokens_than_there_are(at):  # noqa: F811
         buf.a.fill_(float("nan"))
         rows.append(block.forward(buf, tables, tables.advance(dev([0] * B), dev([3, 2]), dev([8]), n)).clone())
     assert torch.equal(rows[0], rows[1][:T]) and (rows[1][T:] == 0).all()
+
+
+def test_strides_of_axes_of_one(at):  # noqa: F811
+    D, L = 64, 40
+    c, table = setup(at, "int8", 16, 1, D, [L], 9)
+    for Hq in (1, 4):
+        q = normal(91, (1, Hq, D), "fp16")
+        odd = torch.as_strided(q, (1, Hq, D), (3, D if Hq > 1 else 5, 1))
+        out = torch.empty(Hq * D, dtype=q.dtype, device="cuda")
+        ws = c.workspace(1, 1, Hq)
+        want = c.attend(q, dev(table), dev([L]), ws)
+        c.attend(odd, dev(table), dev([L]), ws, out=torch.as_strided(out, (1, Hq, D), (1, D if Hq > 1 else 7, 1)))
+        assert torch.equal(out.view(1, Hq, D), want)
+    one = at.KVCache.wrap(torch.as_strided(torch.zeros(1024, dtype=torch.int8, device="cuda"), (1, 1, 16, D), (1, 7, D, 1)),
+                          torch.as_strided(torch.zeros(1024, dtype=torch.int8, device="cuda"), (1, 1, 16, D), (2, 9, D, 1)),
+                          *(torch.zeros(1, 1, device="cuda") for _ in range(2)))
+    plain = at.KVCache(1, 16, 1, D)
+    k, v = normal(92, (5, 1, D), "fp16"), normal(93, (5, 1, D), "fp16")
+    for x in (one, plain):
+        x.append(k, v, dev(np.arange(5)))
+    for a, b in zip(one.read(dev(np.arange(5))), plain.read(dev(np.arange(5)))):
+        assert torch.equal(a, b)
+    q = normal(94, (1, 2, D), "fp16")
+    assert torch.equal(*(x.attend(q, dev([[0]]), dev([5]), x.workspace(1, 1, 2)) for x in (one, plain)))
