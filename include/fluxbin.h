@@ -451,6 +451,7 @@ fluxbin_status_t fluxbin_pack_device(const fluxbin_layer_desc_t *d_desc, const i
  *   - Heads come as [token][head][dim]: a pointer, a stride between tokens and a stride between heads, both in
  *     elements; the elements of a head are contiguous.  A projection's output y [B][ldy] is such a tensor with a token
  *     stride of ldy and a head stride of head_dim.
+ *     The heads of an output may not overlap each other (RANGE); inputs may, an expanded one (stride 0) included.
  *   - dtype: FLUXBIN_TYPE_FP16, _FP32 or _BF16.  Arithmetic is fp32; results are rounded once, to nearest even.
  *   - Every call is asynchronous on cuda_stream, allocates nothing, does not synchronise and can be captured into a
  *     graph.  Kernels are launched with programmatic stream serialization and wait on the device before they read.

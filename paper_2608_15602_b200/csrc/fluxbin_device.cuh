@@ -26,6 +26,15 @@ inline int type_size(int dtype) { return dtype == FLUXBIN_TYPE_FP32 ? 4 : 2; }
 inline bool type_known(int dtype) { return dtype == FLUXBIN_TYPE_FP16 || dtype == FLUXBIN_TYPE_FP32 || dtype == FLUXBIN_TYPE_BF16; }
 inline bool aligned_to(const void *p, size_t n) { return ((uintptr_t)p % n) == 0; }
 
+// whether the heads of an output lie apart: the larger stride covers what the smaller one spans
+inline bool heads_apart(int64_t tokens, int64_t heads, int64_t token, int64_t head, int64_t dim)
+{
+    token = token < 0 ? -token : token;
+    head = head < 0 ? -head : head;
+    if (tokens < 2 || heads < 2) return tokens > 1 ? token >= dim : heads < 2 || head >= dim;
+    return token < head ? token >= dim && head >= token * (tokens - 1) + dim : head >= dim && token >= head * (heads - 1) + dim;
+}
+
 // ---- launches ------------------------------------------------------------------------------------------
 
 // Programmatic stream serialization, as for the layer kernels: the kernel may be set up while its predecessor drains;

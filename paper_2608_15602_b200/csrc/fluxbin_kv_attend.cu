@@ -868,6 +868,7 @@ extern "C" fluxbin_status_t fluxbin_kv_attend(const fluxbin_kv_cache_t *cache, i
     if (!aligned_to(d_q, 16) || !aligned_to(d_out, 16) || (tokens > 1 && (q_token % 8 || out_token % 8)) || (q_heads > 1 && (q_head % 8 || out_head % 8)) ||
         !aligned_to(d_query_start, 4) || !aligned_to(d_lengths, 4) || !aligned_to(d_block_table, 4) || !aligned_to(d_lse, 4) ||
         !aligned_to(d_workspace, 16)) return FLUXBIN_ERR_ALIGNMENT;
+    if (!heads_apart(tokens, q_heads, out_token, out_head, cache->head_dim)) return FLUXBIN_ERR_RANGE;
     if (ws_bytes < fluxbin_kv_attend_workspace_size(batch, tokens, q_heads, cache->kv_heads, cache->head_dim)) return FLUXBIN_ERR_BUFFER_TOO_SMALL;
     const Args a = {*cache, batch, tokens, q_heads, block_table_width, d_q, q_token, q_head, d_query_start, d_lengths, d_block_table,
                     block_table_stride, scale, d_out, out_token, out_head, d_lse,

@@ -570,6 +570,7 @@ extern "C" fluxbin_status_t fluxbin_kv_append(const fluxbin_kv_cache_t *cache, i
     const size_t size = (size_t)type_size(dtype);
     if (!aligned_to(d_k, size) || !aligned_to(d_v, size) || !aligned_to(d_q, size) || !aligned_to(d_q ? d_q_out : nullptr, size) ||
         !aligned_to(d_slots, 4) || (rotary && !aligned_to(d_positions, 4))) return FLUXBIN_ERR_ALIGNMENT;
+    if (d_q && !heads_apart(tokens, q_heads, qo_token, qo_head, cache->head_dim)) return FLUXBIN_ERR_RANGE;
     const Heads k = {d_k, k_token, k_head, cache->kv_heads}, v = {d_v, v_token, v_head, cache->kv_heads}, q = {d_q, q_token, q_head, q_heads};
     const HeadsOut qo = {d_q_out, qo_token, qo_head};
     cudaStream_t s = (cudaStream_t)cuda_stream;

@@ -213,6 +213,8 @@ extern "C" fluxbin_status_t fluxbin_rotary(const fluxbin_rotary_t *rotary, int32
     const size_t size = (size_t)type_size(dtype);
     if (!aligned_to(d_q, size) || !aligned_to(d_q_out, size) || !aligned_to(d_k, size) || !aligned_to(d_k ? d_k_out : nullptr, size) ||
         !aligned_to(d_positions, 4)) return FLUXBIN_ERR_ALIGNMENT;
+    if (!heads_apart(tokens, q_heads, qo_token, qo_head, rotary->head_dim) || (d_k && !heads_apart(tokens, k_heads, ko_token, ko_head, rotary->head_dim)))
+        return FLUXBIN_ERR_RANGE;
     const Side q = {d_q, d_q_out, q_heads, q_token, q_head, qo_token, qo_head};
     const Side k = {d_k, d_k_out, d_k ? k_heads : 0, k_token, k_head, ko_token, ko_head};
     FBD_CUDA(launch_rotary(*rotary, dtype, inverse, tokens, d_positions, q, k, (cudaStream_t)cuda_stream));

@@ -220,3 +220,18 @@ def test_a_set_of_outputs_written_on_another_stream_is_recorded_there(memory):
     with torch.cuda.stream(s):
         step = t.advance(ints(3), ints(3), ints(1), 3)
     assert recorded[1:] == [(step.slots.untyped_storage().data_ptr(), s)]
+
+
+def test_outputs_whose_heads_overlap_are_refused():
+    """They would be written by several threads at once: an expanded output, for instance."""
+    r, c = fluxbin.RotaryDesc(64, 64, 0, 1.0, 1 << 24), a_cache()
+    R, C = ctypes.addressof(r), ctypes.addressof(c)
+    for strides, apart in (((256, 64), True), ((64, 192), True), ((0, 64), False), ((256, 0), False), ((64, 64), False), ((256, 32), False), ((192, 64), False)):
+        if apart:
+            assert attend_status(tokens=2, heads=4 if strides[0] > 64 else 2, out=strides) == 5
+            continue
+        assert attend_status(out=strides) == 3
+        rot = lambda q, k: fluxbin.rotary_status(R, 0, 0, 2, P, P, 4, 256, 64, P, *q, P, 4, 256, 64, P, *k, None)  # noqa: E731
+        assert rot(strides, (256, 64)) == 3 and rot((256, 64), strides) == 3
+        assert fluxbin.kv_append_status(C, 0, 2, P, P, 128, 64, P, 128, 64, R, P, P, 4, 256, 64, P, *strides, None) == 3
+    assert attend_status(batch=1, tokens=1, out=(0, 64)) == 5             # one token
