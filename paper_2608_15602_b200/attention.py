@@ -12,6 +12,8 @@ over it and the block tables both go by.  torch owns the memory and the stream, 
 `stream` (a torch stream, else the current one): what a call allocates comes from that stream's memory, so nothing queued
 elsewhere still uses it, and is recorded on the current stream too, so it may be dropped there.  The tensors given to the call
 have to be ready on `stream` and are the caller's to keep until it is through, as with any torch call on another stream.
+
+Rotary.apply carries gradients.  The other calls are those of answering: their results have none.
 """
 from __future__ import annotations
 
@@ -94,6 +96,24 @@ def _output(given: torch.Tensor | None, like: torch.Tensor, heads: int, what: st
     return y, p, st, sh
 
 
+class _Turned(torch.autograd.Function):
+    """Rotary.apply for heads that want a gradient: that of a turn is the turn back."""
+
+    @staticmethod
+    def forward(ctx, rotary, q, k, positions, inverse, stream):
+        ctx.rotary, ctx.inverse = rotary, inverse
+        ctx.save_for_backward(positions)
+        return rotary._turn(q, k, positions, inverse, None, None, stream)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        # (a gradient may come expanded, and one of the two may not be there)
+        heads = [None if g is None or not wanted else g if g.stride(2) == 1 else g.contiguous() for g, wanted in zip(grads, ctx.needs_input_grad[1:3])]
+        there = [g for g in heads if g is not None]
+        back = iter(ctx.rotary.apply(*there, *[None] * (2 - len(there)), *ctx.saved_tensors, inverse=not ctx.inverse) if there else ())
+        return (None, *(None if g is None else next(back) for g in heads), None, None, None)
+
+
 class Rotary:
     """Rotary positions (fluxbin_rotary): the frequencies live on the device, angles are formed in the kernels.
 
@@ -117,7 +137,13 @@ class Rotary:
     def apply(self, q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor, inverse: bool = False,
               q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, stream=None):
         """q, k [tokens][heads][head_dim] turned to positions [tokens] (int32); outputs may be the inputs.  `inverse` turns
-        back: the gradient of the turned heads with respect to q and k.  Returns (q_out, k_out), k_out None without k."""
+        back: the gradient of the turned heads with respect to q and k.  Returns (q_out, k_out), k_out None without k.  New
+        outputs of heads that require a gradient carry it; outputs that were given are written without one."""
+        if q_out is None and k_out is None and (q.requires_grad or (k is not None and k.requires_grad)) and torch.is_grad_enabled():
+            return _Turned.apply(self, q, k, positions, inverse, stream)
+        return self._turn(q, k, positions, inverse, q_out, k_out, stream)
+
+    def _turn(self, q, k, positions, inverse, q_out, k_out, stream):
         n, dt = q.shape[0], q.dtype
         if dt not in _TYPES:
             raise TypeError("q: fp16, bf16 or fp32 is wanted")
