@@ -125,7 +125,7 @@ class Rotary:
                  low: float = 1.0, high: float = 4.0, device="cuda"):
         if scaling not in _KINDS:
             raise ValueError(f"scaling: one of {sorted(_KINDS)} is wanted")
-        self.head_dim, self.rotary_dim, self.interleaved = head_dim, rotary_dim or head_dim, bool(interleaved)
+        self.head_dim, self.rotary_dim, self.interleaved = head_dim, head_dim if rotary_dim is None else rotary_dim, bool(interleaved)
         if self.rotary_dim > head_dim:
             raise fluxbin.FluxBinError(3, "Rotary: rotary_dim past head_dim")
         a, b = (fast, slow) if scaling == "ramp" else (low, high)

@@ -235,3 +235,11 @@ def test_outputs_whose_heads_overlap_are_refused():
         assert rot(strides, (256, 64)) == 3 and rot((256, 64), strides) == 3
         assert fluxbin.kv_append_status(C, 0, 2, P, P, 128, 64, P, 128, 64, R, P, P, 4, 256, 64, P, *strides, None) == 3
     assert attend_status(batch=1, tokens=1, out=(0, 64)) == 5             # one token
+
+
+def test_a_turned_part_of_no_elements_is_refused():
+    """(and not taken for the whole head)"""
+    for d in (0, -2, 1, 66):
+        with pytest.raises(fluxbin.FluxBinError, match="range"):
+            at.Rotary(64, d, device="cpu")
+    assert at.Rotary(64, device="cpu").rotary_dim == 64 and at.Rotary(64, None, device="cpu").rotary_dim == 64 and at.Rotary(64, 2, device="cpu").rotary_dim == 2
