@@ -277,6 +277,8 @@ class KVCache:
             raise ValueError("table: an int32 tensor [batch][max_blocks] with contiguous rows on the current CUDA device is wanted")
         if self.k.get_device() != _device():
             raise ValueError("the cache has to lie on the current CUDA device")
+        if ws.tensor.get_device() != _device():
+            raise ValueError("the workspace has to lie on the current CUDA device")
         B, width = table.shape
         out, op, ot, os_ = _output(out, q, qh, "out", stream)
         lse = self._new((n, qh), torch.float32, stream) if with_lse else None

@@ -17,7 +17,7 @@ CALLS = ("rotary_call", "kv_append_call", "kv_read_call", "kv_attend_call", "kv_
 def calls(monkeypatch):
     """The words of every call that would have been made, by name; device -1 (the CPU's) counts as the current one."""
     got = []
-    monkeypatch.setattr(at, "_device", lambda: -1)
+    monkeypatch.setattr(at, "_device", lambda: -1)        # (get_device() of a CPU tensor)
     monkeypatch.setattr(at, "_stream", lambda stream: 0)
     monkeypatch.setattr(at, "_capturing", lambda stream: False, raising=False)
     for name in CALLS:
@@ -243,3 +243,17 @@ def test_a_turned_part_of_no_elements_is_refused():
         with pytest.raises(fluxbin.FluxBinError, match="range"):
             at.Rotary(64, d, device="cpu")
     assert at.Rotary(64, device="cpu").rotary_dim == 64 and at.Rotary(64, None, device="cpu").rotary_dim == 64 and at.Rotary(64, 2, device="cpu").rotary_dim == 2
+
+
+def test_a_workspace_elsewhere_is_refused(calls):
+    class OfAnother(torch.Tensor):
+        def get_device(self):
+            return 1
+
+    class Elsewhere:
+        tensor, nbytes = torch.empty(1, dtype=torch.uint8).as_subclass(OfAnother), 1
+
+    c = at.KVCache(8, 16, 2, 64, device="cpu")
+    with pytest.raises(ValueError, match="workspace"):
+        c.attend(torch.zeros(1, 4, 64, dtype=torch.float16), ints(1, 2), ints(1), Elsewhere)
+    assert not calls
