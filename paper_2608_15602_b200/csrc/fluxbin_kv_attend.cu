@@ -36,7 +36,8 @@ using namespace fbd;
 namespace {
 
 // Warps of a CTA, CTAs on an SM, tiles of 16 tokens that a warp has under way, whether the queries stay in shared memory (the
-// output takes the registers), by head dimension and tiles of 8 query rows.  Measured at 128 with 8 rows on 64 requests of up
+// output takes the registers), by head dimension and tiles of 8 query rows.  Measured, as the figures below up to kTailMin, while
+// the probabilities were one operand of the second product: at 128 with 8 rows on 64 requests of up
 // to 16384 tokens: 4 x 3 with 4 tiles 242 us, 8 x 2 with 3 249, 6 x 2 with 4 257, 4 x 4 with 3 (128 registers, spills) 277, 12 x
 // 1 with 4 288: small CTAs, so that the others go on while one ends a job, and tiles on their way rather than warps.  With 16
 // rows on 16 requests of up to 8190: 4 x 2 64 us, 8 x 1 74.  40 rows are as many as the registers take.
@@ -91,7 +92,8 @@ __device__ __forceinline__ uint32_t half2_of_bf16(uint32_t w, int e)
 
 // four entries of a key to two pairs of fp16
 template <int FMT> __device__ __forceinline__ void to_half4(uint32_t x, uint32_t &lo, uint32_t &hi);
-// int8: the byte with its sign bit flipped, under the exponent of 1024, is 1024 + 128 + value; fp16 holds that exactly
+// int8: the byte with its sign bit flipped, under the exponent of 1024, is 1024 + 128 + value; fp16 holds that exactly (the
+// conversion of Kim, Henry, Fahim and Awadalla, "Who Says Elephants Can't Run", 2022)
 template <> __device__ __forceinline__ void to_half4<FLUXBIN_CACHE_INT8>(uint32_t x, uint32_t &lo, uint32_t &hi)
 {
     x ^= 0x80808080u;
@@ -492,23 +494,24 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
                         sm.any_nan = 1;
                     }
             }
-            if (FMT != FLUXBIN_CACHE_E4M3) return;
+            if constexpr (FMT == FLUXBIN_CACHE_E4M3) {
 #pragma unroll 1
-            for (int i = 0; i < 4 * VC * VW; ++i) {
-                const int part = i / VW, token = tok + 2 * lq + (part / VC & 1) + (part / VC >> 1) * 8;
-                const uint32_t at = v_ring + stage * (32 * D) + part * (VW * 128) + i % VW * 4;
-                uint32_t x;
-                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
-                uint32_t nan = ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;        // the top bits of the bytes that are NaN
-                if (none || token >= rq.length) x = nan = 0;
-                else if (nan) x &= ~(nan | (nan - (nan >> 7)));
-                else continue;
-                asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(x) : "memory");
-                for (; nan; nan &= nan - 1) {
-                    const int d = part % VC * (VW * 32) + lr * (VW * 4) + i % VW * 4 + (__ffs(nan) - 1) / 8;
-                    for (int row = 0; row < rows; ++row)
-                        if (token < sees(row)) atomicOr(&sm.nan[row][d / 32], 1u << (d % 32));
-                    sm.any_nan = 1;
+                for (int i = 0; i < 4 * VC * VW; ++i) {
+                    const int part = i / VW, token = tok + 2 * lq + (part / VC & 1) + (part / VC >> 1) * 8;
+                    const uint32_t at = v_ring + stage * (32 * D) + part * (VW * 128) + i % VW * 4;
+                    uint32_t x;
+                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+                    uint32_t nan = ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;        // the top bits of the bytes that are NaN
+                    if (none || token >= rq.length) x = nan = 0;
+                    else if (nan) x &= ~(nan | (nan - (nan >> 7)));
+                    else continue;
+                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(x) : "memory");
+                    for (; nan; nan &= nan - 1) {
+                        const int d = part % VC * (VW * 32) + lr * (VW * 4) + i % VW * 4 + (__ffs(nan) - 1) / 8;
+                        for (int row = 0; row < rows; ++row)
+                            if (token < sees(row)) atomicOr(&sm.nan[row][d / 32], 1u << (d % 32));
+                        sm.any_nan = 1;
+                    }
                 }
             }
         };
@@ -553,7 +556,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
                         mma(!QSHARED && (w & 1) ? s2[QSHARED ? 0 : t] : s[t], a0, a1, a2, a3, b.x, b.y);
                     }
                 }
-            // (here and not before the scores: 119 -> 114 us with 40 rows)
+            // (here and not before the scores: 4 % less time with 40 rows)
             if (tile + STAGES - 1 < tiles) fetch(ahead, stage_ahead);
             copies_commit();
 
@@ -819,13 +822,14 @@ cudaError_t run(const Args &a, cudaStream_t s)
 }
 template <int D, int FMT, typename T> cudaError_t run_rows(const Args &a, cudaStream_t s)
 {
-    // rows that share a key head in an average request; a tile of 40 rows takes 2.4 times one of 16 (at 128: 16 rows 56 us,
-    // 32 94, 40 139 against 111 in one tile, 64 176 against 190 in two, 72 212 against 191; at 64 tiles of 40 never won)
+    // rows that share a key head in an average request; a tile of 40 rows takes 2.2 times one of 16 (at 128, 16 requests of up to
+    // 8190 tokens: 24 rows 109 us against 117 in one tile, 32 112 against 119, 40 169 against 122, 64 213 in both, 72 256 against
+    // 215 in two, 112 337 against 324 in three; at 64 tiles of 40 never won)
     const long long rows = (long long)(a.q_heads / a.c.kv_heads) * ((a.tokens + a.batch - 1) / a.batch);
     if constexpr (D == 128) {
-        if ((rows + 39) / 40 * 12 < (rows + 15) / 16 * 5) return run<D, FMT, 5, T>(a, s);
+        if ((rows + 39) / 40 * 11 < (rows + 15) / 16 * 5) return run<D, FMT, 5, T>(a, s);
     }
-    // (9 to 16 rows in one tile of 16 instead of two of 8: 57 against 76 us at 128, 43 against 51 at 256)
+    // (9 to 16 rows in one tile of 16 instead of two of 8: 68 against 80 us at 128, 92 against 138 at 256, 41 against 48 at 64)
     if (rows > 8) return run<D, FMT, 2, T>(a, s);
     return run<D, FMT, 1, T>(a, s);
 }
