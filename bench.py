@@ -18,7 +18,8 @@ value = algorithmic bytes moved per second over all GPUs (GB/s); us_per_layer an
 carry the latency side of the metric.  With --gpus N the N ranks run independent replicas (the
 path has no exchange step): weak scaling, no collective on the data path.
 
-Beside the headline the line carries (rank 0, one GPU; --sections picks them):
+Beside the headline (rank 0, one GPU; --sections picks them; cpu_baseline in the line itself, the others, which are long, as
+one JSON object on stderr, so that the line stays one that is read whole):
   group_mode  the same stack with one launch per dependency group
   sustained   the headline launch replayed for at least two seconds under the clock sampler
   configs     the smaller workloads (one layer, hybrid layer, 7B set, 13B set) in linear / group / stack mode
@@ -53,6 +54,20 @@ METRIC = "decode_linear_stack_effective_hbm_gbps_batch1"
 UNIT = "GB/s"
 L2_BYTES = 126e6
 ALL_SECTIONS = ["group_mode", "sustained", "configs", "variants", "mu_sweep", "rc_decomp", "context", "cpu_baseline"]
+
+
+# what goes to stderr: a line of more than about 3000 characters is cut where output is kept by its end
+LONG = ("group_mode", "configs", "variants", "mu_sweep", "rc_decomp", "context_dense_fp16_gemv", "lookup_ceiling")
+
+
+def split_line(line):
+    """(the headline's line, the sections that go beside it)"""
+    sections = {k: line[k] for k in LONG if k in line}
+    short = {k: v for k, v in line.items() if k not in sections}
+    if "sustained" in short["roofline"]:
+        short["roofline"] = dict(short["roofline"])
+        sections["sustained"] = short["roofline"].pop("sustained")
+    return short, sections
 
 
 def algorithmic_bytes(M, N, Kb, Ks, g, n_sal, B):
@@ -887,6 +902,8 @@ def main():
             line["cpu_baseline"] = {"value": gbps, "unit": UNIT, "cores": cores, "kind": "oracle", "sample": sample,
                                     "seconds": round(tsec, 2), "gpu_vs_oracle_on_sample": agreement}
         line["sections_s"] = round(time.perf_counter() - t_sections, 1)
+        line, beside = split_line(line)
+        print(json.dumps({"sections": beside}), file=sys.stderr, flush=True)
         print(json.dumps(line), flush=True)
     if world > 1:
         dist.barrier()
