@@ -147,6 +147,9 @@ template <> __device__ __forceinline__ void to_bfloat2x4<FLUXBIN_CACHE_E4M3>(uin
     }
 }
 
+// the top bits of the bytes that are e4m3 NaN
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -496,21 +499,26 @@ __global__ void __launch_bounds__(Shape<D, NT>::warps * 32, Shape<D, NT>::ctas) 
             }
             if constexpr (FMT == FLUXBIN_CACHE_E4M3) {
 #pragma unroll 1
-                for (int i = 0; i < 4 * VC * VW; ++i) {
-                    const int part = i / VW, token = tok + 2 * lq + (part / VC & 1) + (part / VC >> 1) * 8;
-                    const uint32_t at = v_ring + stage * (32 * D) + part * (VW * 128) + i % VW * 4;
-                    uint32_t x;
-                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
-                    uint32_t nan = ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;        // the top bits of the bytes that are NaN
-                    if (none || token >= rq.length) x = nan = 0;
-                    else if (nan) x &= ~(nan | (nan - (nan >> 7)));
-                    else continue;
-                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(x) : "memory");
-                    for (; nan; nan &= nan - 1) {
-                        const int d = part % VC * (VW * 32) + lr * (VW * 4) + i % VW * 4 + (__ffs(nan) - 1) / 8;
-                        for (int row = 0; row < rows; ++row)
-                            if (token < sees(row)) atomicOr(&sm.nan[row][d / 32], 1u << (d % 32));
-                        sm.any_nan = 1;
+                for (int part = 0; part < 4 * VC; ++part) {
+                    const int token = tok + 2 * lq + (part / VC & 1) + (part / VC >> 1) * 8;
+                    const uint32_t at = v_ring + stage * (32 * D) + part * (VW * 128);
+                    Words<VW> x = take<VW>(at);
+                    uint32_t any = 0;
+#pragma unroll
+                    for (int w = 0; w < VW; ++w) any |= nan_bytes(x.w[w]);
+                    if (none || token >= rq.length) x = Words<VW>{};
+                    else if (any == 0) continue;
+#pragma unroll
+                    for (int w = 0; w < VW; ++w) {
+                        uint32_t nan = nan_bytes(x.w[w]);
+                        x.w[w] &= ~(nan | (nan - (nan >> 7)));
+                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(at + w * 4), "r"(x.w[w]) : "memory");
+                        for (; nan; nan &= nan - 1) {
+                            const int d = part % VC * (VW * 32) + lr * (VW * 4) + w * 4 + (__ffs(nan) - 1) / 8;
+                            for (int row = 0; row < rows; ++row)
+                                if (token < sees(row)) atomicOr(&sm.nan[row][d / 32], 1u << (d % 32));
+                            sm.any_nan = 1;
+                        }
                     }
                 }
             }
