@@ -370,8 +370,10 @@ class AttentionBlock:
         return b
 
     def forward(self, b: SimpleNamespace, tables: BlockTables, step: SimpleNamespace, stream=None) -> torch.Tensor:
-        """y = o(attention(x)) for the new tokens of `step` (BlockTables.advance) in b.x; the result is b.y.  Three launches
-        besides the output projection, nothing allocated: a decode step can be captured into a graph."""
+        """y = o(attention(x)) for the new tokens of `step` (BlockTables.advance) in b.x; the result is b.y (of tokens past the
+        step's own: o(0)).  A decode step is three launches besides the output projection (the append of a prompt turns its
+        queries in one of its own, and projections of many tokens take several); nothing is allocated, so a step can be captured
+        into a graph."""
         n, D = b.x.shape[0], self.cache.head_dim
         b.plan.run(stream)
         q, a = b.q.view(n, self.q_heads, D), b.a.view(n, self.q_heads, D)
