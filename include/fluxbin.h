@@ -514,6 +514,44 @@ fluxbin_status_t fluxbin_rotary(const fluxbin_rotary_t *rotary, int32_t dtype, i
                                 void *d_k_out, int64_t ko_token, int64_t ko_head, void *cuda_stream);
 
 /*
+ * Norms of query and key heads with the rotary's turn in the same pass:  y = turn_p(w * x * r),  r = (mean(x^2) + eps)^(-1/2)
+ * over the head_dim elements of a head; one gain w for all query heads and one for all key heads.  Everything between x and y
+ * is fp32, y is rounded once.
+ *   d_q_weight, d_k_weight   DEVICE [head_dim] of weight_dtype, or NULL: 1
+ *   eps                      > 0 and finite
+ * The rest as fluxbin_rotary (k may be NULL, outputs may be the inputs themselves).  Errors: as fluxbin_rotary.
+ */
+fluxbin_status_t fluxbin_norm_rotary(const fluxbin_rotary_t *rotary, float eps, int32_t dtype, int32_t weight_dtype, int32_t tokens,
+                                     const int32_t *d_positions,
+                                     const void *d_q, int32_t q_heads, int64_t q_token, int64_t q_head, const void *d_q_weight,
+                                     void *d_q_out, int64_t qo_token, int64_t qo_head,
+                                     const void *d_k, int32_t k_heads, int64_t k_token, int64_t k_head, const void *d_k_weight,
+                                     void *d_k_out, int64_t ko_token, int64_t ko_head, void *cuda_stream);
+
+/*
+ * The gradients of fluxbin_norm_rotary from its inputs x and those of its outputs, with e = turn_p^-1(gradient of y) (times the
+ * rotary's magnitude, as the turn):
+ *   of x:  r (w e - x r mean(w e x r))        of w:  sum over tokens and heads of e x r
+ *   d_q, d_k                        the inputs x; either may be NULL (a side without a gradient), its other arguments are then not looked at
+ *   d_q_grad, d_k_grad              gradients of the outputs, of dtype (heads may be expanded: strides of 0)
+ *   d_q_dx, d_k_dx                  out, or NULL: not wanted.  May not overlap the inputs.
+ *   d_q_dweight, d_k_dweight        out, DEVICE [head_dim] of weight_dtype, or NULL: not wanted.  With tokens == 0 they become 0.
+ *   d_workspace                     fluxbin_norm_rotary_backward_workspace_size bytes, 16-byte aligned, any contents; wanted only
+ *                                   with a gradient of a weight.  Calls that overlap need one each.
+ * Sums are fp32 in a fixed order: results do not change from run to run.  Errors: as fluxbin_rotary, BUFFER_TOO_SMALL.
+ */
+size_t fluxbin_norm_rotary_backward_workspace_size(int32_t head_dim);
+fluxbin_status_t fluxbin_norm_rotary_backward(const fluxbin_rotary_t *rotary, float eps, int32_t dtype, int32_t weight_dtype, int32_t tokens,
+                                              const int32_t *d_positions,
+                                              const void *d_q, int32_t q_heads, int64_t q_token, int64_t q_head, const void *d_q_weight,
+                                              const void *d_q_grad, int64_t qg_token, int64_t qg_head,
+                                              void *d_q_dx, int64_t qd_token, int64_t qd_head, void *d_q_dweight,
+                                              const void *d_k, int32_t k_heads, int64_t k_token, int64_t k_head, const void *d_k_weight,
+                                              const void *d_k_grad, int64_t kg_token, int64_t kg_head,
+                                              void *d_k_dx, int64_t kd_token, int64_t kd_head, void *d_k_dweight,
+                                              void *d_workspace, size_t ws_bytes, void *cuda_stream);
+
+/*
  * A cache of keys and values in 8 bits, in blocks of block_tokens tokens, with one fp32 scale for each block and key
  * head: an entry stands for (its 8-bit value) * (its block's and head's scale).
  *
@@ -634,8 +672,72 @@ fluxbin_status_t fluxbin_kv_advance(int32_t batch, int32_t tokens, int32_t block
                                     void *cuda_stream);
 
 /*
+ * Trees of drafted tokens: each new token of a request follows another one of them (its parent) or the request's cached tokens,
+ * and sees the cached tokens, its ancestors and itself.  From the parents to what the step's calls want:
+ *
+ *   d_query_start   DEVICE int32 [batch + 1], as fluxbin_kv_attend: the new tokens of each request
+ *   d_lengths       DEVICE int32 [batch]: cached tokens of each request, the new ones included
+ *   d_parents       DEVICE int32 [tokens]: the place of a token's parent among its request's new tokens; none if it is not an
+ *                   earlier one (-1)
+ *   nodes           the most new tokens of a request that count, 1 .. 1024; what comes after them has an empty mask
+ *   d_mask          DEVICE int32 [tokens][ceil(nodes / 32)], out: bit j % 32 of word j / 32 is set if the token sees its request's
+ *                   j-th new token: itself and its ancestors.  Tokens that are no request's see nothing.
+ *   d_positions     DEVICE int32 [tokens], out: cached tokens before the step plus the number of the token's ancestors; 0 for
+ *                   tokens that are no request's
+ * Errors: NULL, RANGE, ALIGNMENT, CUDA.
+ */
+fluxbin_status_t fluxbin_draft_tree(int32_t batch, int32_t tokens, int32_t nodes, const int32_t *d_query_start, const int32_t *d_lengths,
+                                    const int32_t *d_parents, int32_t *d_mask, int32_t *d_positions, void *cuda_stream);
+
+/*
+ * fluxbin_kv_attend where a row sees the cached tokens before the step's new ones and, of those, the ones in its mask:
+ *   d_tree        DEVICE int32 [tokens][tree_stride]: bit j % 32 of word j / 32 of a token's first tree_words words says whether
+ *                 it sees its request's j-th new token (of its count in d_query_start; later ones and those past the words are
+ *                 not seen).  fluxbin_draft_tree makes them; any other masks will do.
+ *   d_workspace   fluxbin_kv_attend_tree_workspace_size bytes, zeroed once with fluxbin_workspace_init; it serves
+ *                 fluxbin_kv_attend too, and calls that share one must be ordered on a stream.
+ * All else as fluxbin_kv_attend.  Errors: as there.
+ */
+size_t fluxbin_kv_attend_tree_workspace_size(int32_t batch, int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim);
+fluxbin_status_t fluxbin_kv_attend_tree(const fluxbin_kv_cache_t *cache, int32_t dtype, int32_t batch, int32_t tokens,
+                                        const void *d_q, int32_t q_heads, int64_t q_token, int64_t q_head,
+                                        const int32_t *d_query_start, const int32_t *d_lengths,
+                                        const int32_t *d_tree, int64_t tree_stride, int32_t tree_words,
+                                        const int32_t *d_block_table, int64_t block_table_stride, int32_t block_table_width,
+                                        float scale, void *d_out, int64_t out_token, int64_t out_head, float *d_lse,
+                                        void *d_workspace, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * The path of each request's tree that the model itself would have answered, token after token (greedy): its first new token --
+ * the last one that was known before the step -- then, as long as there is one, the first new token whose parent is the last of
+ * the path and which is what the model answered there.
+ *   d_drafted   DEVICE int32 [tokens]: the new tokens
+ *   d_answers   DEVICE int32 [tokens]: the token that the model answered at each of them
+ *   d_path      DEVICE int32 [tokens], out: places among the request's new tokens in the path's order, from d_query_start[r] on,
+ *               then -1; -1 for tokens that are no request's
+ *   d_count, d_answer, d_surplus   DEVICE int32 [batch], out: tokens of the path; the answer at its end, which comes next (-1
+ *               without new tokens); the path's tokens less the new ones, which is what fluxbin_kv_advance is to drop
+ * Only the first `nodes` new tokens of a request are looked at.  The rest as fluxbin_draft_tree.  Errors: as there.
+ */
+fluxbin_status_t fluxbin_draft_accept(int32_t batch, int32_t tokens, int32_t nodes, const int32_t *d_query_start, const int32_t *d_parents,
+                                      const int32_t *d_drafted, const int32_t *d_answers, int32_t *d_path, int32_t *d_count,
+                                      int32_t *d_answer, int32_t *d_surplus, void *cuda_stream);
+
+/*
+ * Move the entries of each request's path to the first slots of its new tokens: what d_path[query_start[r] + j] stands for is
+ * stored at slot d_slots[query_start[r] + j], as fluxbin_kv_append stores new keys and values (tokens of the path that are where
+ * they belong already are left as they are, with the scale of their block, unless a moved entry makes that grow).
+ *   d_slots   DEVICE int32 [tokens]: the slots the new tokens were appended at, as fluxbin_kv_advance gave them.  A token of a slot
+ *             outside the cache is not moved; one whose source is outside becomes 0.
+ *   d_path    DEVICE int32 [tokens]: ascending, entry j not below j; the first one that is not ends the path (fluxbin_draft_accept)
+ * Requests must not share blocks of new tokens.  Errors: as fluxbin_kv_append.
+ */
+fluxbin_status_t fluxbin_kv_keep(const fluxbin_kv_cache_t *cache, int32_t batch, int32_t tokens, const int32_t *d_query_start,
+                                 const int32_t *d_slots, const int32_t *d_path, void *cuda_stream);
+
+/*
  * The calls above with their arguments, in order, as an array of 64-bit words (integers and pointers as they are, `scale`
- * as a double): for bindings that pay for every argument they convert -- a decode step makes these calls in every layer,
+ * and `eps` as doubles): for bindings that pay for every argument they convert -- a decode step makes these calls in every layer,
  * and converting 20 arguments takes ctypes longer than the whole call takes without.  Checks, results and errors are
  * those of the call; UNSUPPORTED for an unknown one.
  */
@@ -644,6 +746,12 @@ fluxbin_status_t fluxbin_kv_advance(int32_t batch, int32_t tokens, int32_t block
 #define FLUXBIN_CALL_KV_READ 2
 #define FLUXBIN_CALL_KV_ATTEND 3
 #define FLUXBIN_CALL_KV_ADVANCE 4
+#define FLUXBIN_CALL_NORM_ROTARY 16
+#define FLUXBIN_CALL_NORM_ROTARY_BACKWARD 17
+#define FLUXBIN_CALL_DRAFT_TREE 18
+#define FLUXBIN_CALL_DRAFT_ACCEPT 19
+#define FLUXBIN_CALL_KV_ATTEND_TREE 20
+#define FLUXBIN_CALL_KV_KEEP 21
 fluxbin_status_t fluxbin_call_words(int32_t which, const int64_t *h_words);
 
 #ifdef __cplusplus

@@ -13,7 +13,18 @@ over it and the block tables both go by.  torch owns the memory and the stream, 
 elsewhere still uses it, and is recorded on the current stream too, so it may be dropped there.  The tensors given to the call
 have to be ready on `stream` and are the caller's to keep until it is through, as with any torch call on another stream.
 
-Rotary.apply carries gradients.  The other calls are those of answering: their results have none.
+Where query and key heads are normed first, NormedRotary(rope, q_weight, k_weight) takes rope's place; the cache then gets keys
+that are turned already.  A step that checks a tree of drafted tokens at once:
+
+    tree = DraftTree(parents, step.query_start, step.lengths, nodes=64)   # masks and positions, once for all layers
+    q, k = normed.apply(q, k, tree.positions)
+    cache.append(k, v, step.slots)
+    out = cache.attend(q, tables.table, step.lengths, ws, query_start=step.query_start, tree=tree.mask)
+    kept = tree.accept(drafted, answers)                                  # the path that the model itself would have answered
+    cache.keep(step.slots, step.query_start, kept.path)                   # its entries move to the step's first slots, in every layer
+    step = tables.advance(step.lengths, kept.surplus, step.num_free, 0)   # and the others are dropped
+
+Rotary.apply and NormedRotary.apply carry gradients.  The other calls are those of answering: their results have none.
 """
 from __future__ import annotations
 
@@ -162,6 +173,107 @@ class Rotary:
         return q_out, k_out
 
 
+class _NormedAndTurned(torch.autograd.Function):
+    """NormedRotary.apply for heads or gains that want a gradient."""
+
+    @staticmethod
+    def forward(ctx, normed, q, k, q_weight, k_weight, positions, stream):
+        ctx.normed, ctx.stream = normed, stream
+        ctx.save_for_backward(q, k, q_weight, k_weight, positions)
+        ctx.set_materialize_grads(False)
+        return normed._apply(q, k, q_weight, k_weight, positions, None, None, stream)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, q_grad, k_grad=None):
+        return (None, *ctx.normed._backward(*ctx.saved_tensors, q_grad, k_grad, *ctx.needs_input_grad[1:5]), None, None)
+
+
+class NormedRotary:
+    """Norms of query and key heads and rotary positions in one pass (fluxbin_norm_rotary): the root mean square of a head's
+    elements is taken out of them, a gain for each element comes in, then the head is turned by `rotary`.
+
+    `q_weight`, `k_weight`: [head_dim] gains of one type (fp16, bf16 or fp32), None for 1; parameters may require a gradient."""
+
+    def __init__(self, rotary: Rotary, q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, eps: float = 1e-6):
+        if not 0.0 < eps < 3e38:
+            raise ValueError("eps: a positive number is wanted")
+        for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            if w is not None and (w.dtype not in _TYPES or w.shape != (rotary.head_dim,) or not w.is_contiguous()):
+                raise ValueError(f"{what}: a contiguous tensor of {rotary.head_dim} gains in fp16, bf16 or fp32 is wanted")
+        if q_weight is not None and k_weight is not None and q_weight.dtype is not k_weight.dtype:
+            raise TypeError("q_weight, k_weight: one type is wanted")
+        self.rotary, self.q_weight, self.k_weight, self.eps = rotary, q_weight, k_weight, float(eps)
+
+    def apply(self, q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor, q_out: torch.Tensor | None = None,
+              k_out: torch.Tensor | None = None, stream=None):
+        """q, k [tokens][heads][head_dim] normed and turned to positions [tokens] (int32); outputs may be the inputs.  Returns
+        (q_out, k_out), k_out None without k.  New outputs carry gradients (of the heads and of the gains, the first ones; they are
+        formed on the stream that the gradients come on); outputs that were given are written without."""
+        if q_out is None and k_out is None and torch.is_grad_enabled() and any(x is not None and x.requires_grad for x in (q, k, self.q_weight, self.k_weight)):
+            return _NormedAndTurned.apply(self, q, k, self.q_weight, self.k_weight, positions, stream)
+        return self._apply(q, k, self.q_weight, self.k_weight, positions, q_out, k_out, stream)
+
+    def _weights(self, q_weight, k_weight):
+        """(type, addresses)"""
+        for w in (q_weight, k_weight):
+            if w is not None and w.get_device() != _device():
+                raise ValueError("the gains have to lie on the current CUDA device")
+        given = q_weight if q_weight is not None else k_weight
+        return (fluxbin.TYPE_FP32 if given is None else _TYPES[given.dtype], *(0 if w is None else w.data_ptr() for w in (q_weight, k_weight)))
+
+    def _check(self, q):
+        if q.dtype not in _TYPES:
+            raise TypeError("q: fp16, bf16 or fp32 is wanted")
+        if self.rotary.turns.get_device() != _device():
+            raise ValueError("the frequencies have to lie on the current CUDA device")
+
+    def _apply(self, q, k, q_weight, k_weight, positions, q_out, k_out, stream):
+        self._check(q)
+        n, dt, D = q.shape[0], q.dtype, self.rotary.head_dim
+        wt, qw, kw = self._weights(q_weight, k_weight)
+        qp, qh, qt, qs = _heads(q, n, D, dt, "q")
+        q_out, op, ot, os_ = _output(q_out, q, qh, "q_out", stream)
+        kp = kh = kt = ks = kop = kot = kos = 0
+        if k is None:
+            k_out = None
+        else:
+            kp, kh, kt, ks = _heads(k, n, D, dt, "k")
+            k_out, kop, kot, kos = _output(k_out, k, kh, "k_out", stream)
+        fluxbin.norm_rotary_call(self.rotary._ref, self.eps, _TYPES[dt], wt, n, _int32(positions, n, "positions"), qp, qh, qt, qs, qw, op, ot, os_,
+                                 kp, kh, kt, ks, kw, kop, kot, kos, _stream(stream))
+        return q_out, k_out
+
+    def _backward(self, q, k, q_weight, k_weight, positions, q_grad, k_grad, *wanted):
+        """The gradients of q, k and the gains, None where none is wanted or comes."""
+        self._check(q)
+        n, dt, D = q.shape[0], q.dtype, self.rotary.head_dim
+        wt, *wp = self._weights(q_weight, k_weight)
+        words, results, ws, held = [], [], None, []       # (what the call reads is held until it is queued)
+        for x, g, w, weight, want, want_w, what in ((q, q_grad, wp[0], q_weight, wanted[0], wanted[2], "q"), (k, k_grad, wp[1], k_weight, wanted[1], wanted[3], "k")):
+            if x is None or g is None or n == 0 or not (want or want_w):       # (tensors of no elements have no address)
+                results += [torch.empty_like(x) if want and n == 0 else None, torch.zeros_like(weight) if want_w and x is not None else None]
+                words += [0] * 12
+                continue
+            if g.stride(2) != 1 and D > 1:
+                g = g.contiguous()
+            held.append(g)
+            xp, xh, xt, xs = _heads(x, n, D, dt, what)
+            gp, gh, gt, gs = _heads(g, n, D, dt, what + "'s gradient")
+            if gh != xh:
+                raise ValueError(f"{what}'s gradient: {xh} heads are wanted")
+            dx = torch.empty_like(x, memory_format=torch.contiguous_format) if want else None
+            dw = torch.empty_like(weight) if want_w else None
+            if want_w and ws is None:
+                ws = torch.empty(fluxbin.norm_rotary_backward_workspace_size(D), dtype=torch.uint8, device=x.device)
+            results += [dx, dw]
+            words += [xp, xh, xt, xs, w, gp, gt, gs, 0 if dx is None else dx.data_ptr(), xh * D, D, 0 if dw is None else dw.data_ptr()]
+        if held:
+            fluxbin.norm_rotary_backward_call(self.rotary._ref, self.eps, _TYPES[dt], wt, n, _int32(positions, n, "positions"), *words,
+                                              0 if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _stream(None))
+        return results[0], results[2], results[1], results[3]
+
+
 class KVCache:
     """Keys and values in 8 bits, in blocks of tokens, one scale for each block and key head (fluxbin_kv_cache_t).
 
@@ -255,19 +367,31 @@ class KVCache:
         fluxbin.kv_read_call(self._ref, _TYPES[dtype], n, _int32(slots, n, "slots"), k.data_ptr(), v.data_ptr(), _stream(stream))
         return k, v
 
-    def workspace(self, batch: int, tokens: int, q_heads: int) -> Workspace:
-        """The workspace of attend() for up to `batch` requests with `tokens` new tokens in all."""
-        n = fluxbin.kv_attend_workspace_size(batch, tokens, q_heads, self.kv_heads, self.head_dim)
+    def keep(self, slots: torch.Tensor, query_start: torch.Tensor, path: torch.Tensor, stream=None) -> None:
+        """fluxbin_kv_keep: the entries of each request's `path` (int32 [tokens], DraftTree.accept) move to the first slots of its
+        new tokens.  `slots` int32 [tokens] and `query_start` int32 [batch + 1] are those the tokens were appended with."""
+        if self.k.get_device() != _device():
+            raise ValueError("the cache has to lie on the current CUDA device")
+        n, B = slots.shape[0], query_start.shape[0] - 1
+        fluxbin.kv_keep_call(self._ref, B, n, _int32(query_start, B + 1, "query_start"), _int32(slots, n, "slots"), _int32(path, n, "path"), _stream(stream))
+
+    def workspace(self, batch: int, tokens: int, q_heads: int, tree: bool = False) -> Workspace:
+        """The workspace of attend() for up to `batch` requests with `tokens` new tokens in all, with `tree` also of trees of them."""
+        size = fluxbin.kv_attend_tree_workspace_size if tree else fluxbin.kv_attend_workspace_size
+        n = size(batch, tokens, q_heads, self.kv_heads, self.head_dim)
         if n == 0:
             raise ValueError("workspace: batch >= 1, tokens >= 0 and a multiple of kv_heads for q_heads are wanted")
         return Workspace(n, self.device)
 
     def attend(self, q: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, ws: Workspace, query_start: torch.Tensor | None = None,
-               scale: float | None = None, out: torch.Tensor | None = None, with_lse: bool = False, stream=None):
+               scale: float | None = None, out: torch.Tensor | None = None, with_lse: bool = False, stream=None,
+               tree: torch.Tensor | None = None):
         """fluxbin_kv_attend: q [tokens][q_heads][head_dim] (fp16 or bf16) over the cached tokens of its requests.
 
         `table` int32 [batch][max_blocks] (its rows may be one row expanded over the batch), `lengths` int32 [batch] (the new tokens included), `query_start` int32
-        [batch + 1] or None for one token a request, `scale` head_dim ** -0.5 if not given.  Returns out [tokens][q_heads]
+        [batch + 1] or None for one token a request, `scale` head_dim ** -0.5 if not given.  `tree` int32 [tokens][words]: which
+        of its request's new tokens each one sees (fluxbin_kv_attend_tree; DraftTree.mask), those up to itself if not given; the
+        workspace is then one for trees.  Returns out [tokens][q_heads]
         [head_dim], with `with_lse` also the natural log of each row's sum, fp32 [tokens][q_heads]."""
         n, dt = q.shape[0], q.dtype
         if dt is not torch.float16 and dt is not torch.bfloat16:
@@ -280,12 +404,16 @@ class KVCache:
         if ws.tensor.get_device() != _device():
             raise ValueError("the workspace has to lie on the current CUDA device")
         B, width = table.shape
+        call, masks = fluxbin.kv_attend_call, ()
+        if tree is not None:
+            if tree.dtype is not torch.int32 or tree.dim() != 2 or tree.shape[0] != n or tree.get_device() != _device() or (tree.shape[1] > 1 and tree.stride(1) != 1):
+                raise ValueError("tree: an int32 tensor [tokens][words] with contiguous rows on the current CUDA device is wanted")
+            call, masks = fluxbin.kv_attend_tree_call, (tree.data_ptr(), tree.stride(0), tree.shape[1])
         out, op, ot, os_ = _output(out, q, qh, "out", stream)
         lse = self._new((n, qh), torch.float32, stream) if with_lse else None
-        fluxbin.kv_attend_call(self._ref, _TYPES[dt], B, n, qp, qh, qt, qs, 0 if query_start is None else _int32(query_start, B + 1, "query_start"),
-                               _int32(lengths, B, "lengths"), table.data_ptr(), _row_stride(table), width,
-                               self._scale if scale is None else scale, op, ot, os_, 0 if lse is None else lse.data_ptr(), ws.tensor.data_ptr(),
-                               ws.nbytes, _stream(stream))
+        call(self._ref, _TYPES[dt], B, n, qp, qh, qt, qs, 0 if query_start is None else _int32(query_start, B + 1, "query_start"),
+             _int32(lengths, B, "lengths"), *masks, table.data_ptr(), _row_stride(table), width, self._scale if scale is None else scale,
+             op, ot, os_, 0 if lse is None else lse.data_ptr(), ws.tensor.data_ptr(), ws.nbytes, _stream(stream))
         return (out, lse) if with_lse else out
 
 
@@ -349,35 +477,74 @@ class BlockTables:
         return step
 
 
+class DraftTree:
+    """The drafted tokens of a step, each behind another one of its request's (its parent) or behind the request's cached tokens
+    (fluxbin_draft_tree).
+
+    `parents` int32 [tokens]: the place of a token's parent among its request's new tokens, -1 for none; `query_start` int32
+    [batch + 1] and `lengths` int32 [batch] (the new tokens included) as for KVCache.attend; `nodes` the most new tokens of a
+    request that count, up to 1024.  Then `mask` int32 [tokens][ceil(nodes / 32)] says which of its request's new tokens each one sees,
+    and `positions` int32 [tokens] where it stands."""
+
+    def __init__(self, parents: torch.Tensor, query_start: torch.Tensor, lengths: torch.Tensor, nodes: int, stream=None):
+        n, B = parents.shape[0], lengths.shape[0]
+        if not 1 <= nodes <= 1024:
+            raise ValueError("nodes: 1 to 1024 are wanted")
+        pointers = _int32(query_start, B + 1, "query_start"), _int32(lengths, B, "lengths"), _int32(parents, n, "parents")
+        self.parents, self.query_start, self.nodes = parents, query_start, nodes
+        words = -(-nodes // 32)
+        both = _made(stream, lambda: torch.empty(n * (words + 1), dtype=torch.int32, device=parents.device))
+        self.mask, self.positions = both[:n * words].view(n, words), both[n * words:]
+        fluxbin.draft_tree_call(B, n, nodes, *pointers, self.mask.data_ptr(), self.positions.data_ptr(), _stream(stream))
+
+    def accept(self, drafted: torch.Tensor, answers: torch.Tensor, stream=None) -> SimpleNamespace:
+        """fluxbin_draft_accept: the path of each request's tree that the model itself would have answered.  `drafted` int32
+        [tokens]: the new tokens; `answers` int32 [tokens]: what the model answered at each.  Returns `path` int32 [tokens] (places
+        among the request's new tokens, then -1: for KVCache.keep), and int32 [batch] `count`, tokens of the path, `answer`, what
+        comes after it, `surplus`, what is to be dropped (as BlockTables.advance takes it)."""
+        n, B = self.parents.shape[0], self.query_start.shape[0] - 1
+        inputs = (_int32(self.query_start, B + 1, "query_start"), _int32(self.parents, n, "parents"), _int32(drafted, n, "drafted"), _int32(answers, n, "answers"))
+        path, *rest = _made(stream, lambda: torch.empty(n + 3 * B, dtype=torch.int32, device=self.parents.device)).split((n, B, B, B))
+        fluxbin.draft_accept_call(B, n, self.nodes, *inputs, path.data_ptr(), *(x.data_ptr() for x in rest), _stream(stream))
+        return SimpleNamespace(path=path, **dict(zip(("count", "answer", "surplus"), rest)))
+
+
 class AttentionBlock:
     """The attention block of a decoder layer on packed linears: q/k/v projections, positions, cache, attention, output
-    projection.  `q`, `k`, `v`, `o` are FluxBinLinear layers; the cache and the block tables may serve a whole batch of requests."""
+    projection.  `q`, `k`, `v`, `o` are FluxBinLinear layers; the cache and the block tables may serve a whole batch of requests.
+    A NormedRotary in the place of `rotary` norms the heads too."""
 
-    def __init__(self, q, k, v, o, cache: KVCache, rotary: Rotary):
+    def __init__(self, q, k, v, o, cache: KVCache, rotary: Rotary | NormedRotary):
         D = cache.head_dim
         if k.M != cache.kv_heads * D or v.M != k.M or q.M % k.M or o.N != q.M or not q.N == k.N == v.N == o.M:
             raise ValueError("the layers do not fit the cache's heads and each other")
         self.q, self.k, self.v, self.o, self.cache, self.rotary, self.q_heads = q, k, v, o, cache, rotary, q.M // D
 
-    def buffers(self, batch: int, tokens: int) -> SimpleNamespace:
-        """What forward() works in for up to `tokens` new tokens of `batch` requests, and its input x [tokens][hidden]
-        and output y: q, k and v run as one plan, so the buffers are theirs."""
+    def buffers(self, batch: int, tokens: int, tree: bool = False) -> SimpleNamespace:
+        """What forward() works in for up to `tokens` new tokens of `batch` requests (`tree`: also for trees of them), and its input x
+        [tokens][hidden] and output y: q, k and v run as one plan, so the buffers are theirs."""
         from .layer import FluxBinPlan
         new = lambda n: torch.empty((tokens, n), dtype=torch.float16, device=self.cache.device)  # noqa: E731
         b = SimpleNamespace(x=new(self.q.N), q=new(self.q.M), k=new(self.k.M), v=new(self.v.M), a=new(self.q.M), y=new(self.o.M))
         b.plan = FluxBinPlan([(self.q, b.x, b.q), (self.k, b.x, b.k), (self.v, b.x, b.v)], device=self.cache.device)
-        b.linear_ws, b.ws = self.o.workspace(tokens), self.cache.workspace(batch, tokens, self.q_heads)
+        b.linear_ws, b.ws = self.o.workspace(tokens), self.cache.workspace(batch, tokens, self.q_heads, tree)
         return b
 
-    def forward(self, b: SimpleNamespace, tables: BlockTables, step: SimpleNamespace, stream=None) -> torch.Tensor:
+    def forward(self, b: SimpleNamespace, tables: BlockTables, step: SimpleNamespace, stream=None, tree: DraftTree | None = None) -> torch.Tensor:
         """y = o(attention(x)) for the new tokens of `step` (BlockTables.advance) in b.x; the result is b.y (of tokens past the
-        step's own: o(0)).  A decode step is three launches besides the output projection (the append of a prompt turns its
-        queries in one of its own, and projections of many tokens take several); nothing is allocated, so a step can be captured
-        into a graph."""
+        step's own: o(0)).  With `tree` they stand and see as it says, and follow each other without.  A decode step is three
+        launches besides the output projection (the append of a prompt turns its queries in one of its own, normed heads take one
+        more, and projections of many tokens take several); nothing is allocated, so a step can be captured into a graph."""
         n, D = b.x.shape[0], self.cache.head_dim
         b.plan.run(stream)
         q, a = b.q.view(n, self.q_heads, D), b.a.view(n, self.q_heads, D)
         k, v = b.k.view(n, -1, D), b.v.view(n, -1, D)
-        self.cache.append(k, v, step.slots, rotary=self.rotary, positions=step.positions, q=q, q_out=q, stream=stream)
-        self.cache.attend(q, tables.table, step.lengths, b.ws, query_start=step.query_start, out=a, stream=stream)
+        positions = step.positions if tree is None else tree.positions
+        if isinstance(self.rotary, NormedRotary):
+            self.rotary.apply(q, k, positions, q_out=q, k_out=k, stream=stream)
+            self.cache.append(k, v, step.slots, stream=stream)
+        else:
+            self.cache.append(k, v, step.slots, rotary=self.rotary, positions=positions, q=q, q_out=q, stream=stream)
+        self.cache.attend(q, tables.table, step.lengths, b.ws, query_start=step.query_start, out=a, stream=stream,
+                          tree=None if tree is None else tree.mask)
         return self.o.forward(b.a, b.linear_ws, out=b.y, stream=stream)

@@ -1,0 +1,149 @@
+// Moving the entries of accepted paths to the first slots of their step's tokens (fluxbin_kv_keep).
+//
+// A warp for each request, key head and side.  The path ascends and no entry of it moves up, so going along it in order never
+// writes an entry that is still to be read, and what is read for a block lies in that block or behind it; the scale of a block
+// is changed only after the last entry that goes there has been read.  A block's entries are read twice: for the largest
+// magnitude, then to be stored.  Bound by a chain of dependent accesses (start, path, slots, entries, scale, entries).
+#include "fluxbin_cache.cuh"
+
+using namespace fbd;
+
+namespace {
+
+constexpr int kWarps = 4;
+
+struct Args {
+    fluxbin_kv_cache_t c;
+    int batch, tokens;
+    const int *query_start, *slots, *path;
+};
+
+template <int FMT> __device__ __forceinline__ void values16(const uint4 &x, float scale, float (&v)[16])
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __fmul_rn(Entry<FMT>::load((unsigned char)(w[i / 4] >> (i % 4 * 8))), scale);
+}
+template <int FMT> __device__ __forceinline__ uint4 entries16(const float (&v)[16], float factor)
+{
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w[i / 4] |= (uint32_t)Entry<FMT>::store(__fmul_rn(v[i], factor)) << (i % 4 * 8);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <int FMT, int D>
+__global__ void __launch_bounds__(kWarps * 32) keep_kernel(const __grid_constant__ Args a)
+{
+    constexpr int LANES = D / 16, AT_ONCE = 32 / LANES;          // of a token, tokens side by side
+    const int lane = threadIdx.x & 31, bs = a.c.block_tokens, limit = a.c.num_blocks * bs, H = a.c.kv_heads;
+    const long long task = (long long)blockIdx.x * kWarps + threadIdx.x / 32;
+    let_successor_start();
+    wait_for_predecessor();
+    if (task >= (long long)a.batch * H * 2) return;
+    const int r = (int)(task / (2 * H)), h = (int)(task / 2 % H), side = (int)(task & 1);
+    const int first = min(max(a.query_start[r], 0), a.tokens), n = max(min(max(a.query_start[r + 1], 0), a.tokens) - first, 0);
+    const int *path = a.path + first, *slots = a.slots + first;
+    unsigned char *cells = (unsigned char *)(side ? a.c.d_v : a.c.d_k) + h * a.c.head_stride;
+    float *scales = (side ? a.c.d_v_scale : a.c.d_k_scale) + h;
+
+    // ---- the tokens that move: from the first that is not where it belongs to the end of the path
+    int begin = n, end = n;
+    for (int i = 0; i < n; i += 32) {
+        const int j = i + lane, p = j < n ? path[j] : -1, before = j > 0 && j < n ? path[j - 1] : -1;
+        const unsigned over = __ballot_sync(0xffffffffu, p < j || p >= n || (j > 0 && p <= before)), moved = __ballot_sync(0xffffffffu, p != j);
+        if (begin == n && moved) begin = min(i + __ffs(moved) - 1, n);
+        if (over) {
+            end = min(i + __ffs(over) - 1, n);
+            break;
+        }
+    }
+    const int sub = lane / LANES, e0 = lane % LANES * 16;
+    const float top_inverse = 1.f / Entry<FMT>::kTop;
+    for (int j = begin; j < end;) {
+        const int s0 = slots[j];
+        if (s0 < 0 || s0 >= limit) {
+            ++j;
+            continue;
+        }
+        // ---- a run: tokens that go to consecutive slots of one block
+        const int block = s0 / bs, offset = s0 % bs;
+        int run = 1;
+        for (const int most = min(bs - offset, end - j); run < most;) {
+            const int i = run + lane;
+            const unsigned on = __ballot_sync(0xffffffffu, i < most && slots[j + min(i, most - 1)] == s0 + i);
+            const int more = on == 0xffffffffu ? 32 : __ffs(~on) - 1;
+            run += more;
+            if (more < 32) break;
+        }
+        unsigned char *to = cells + block * a.c.block_stride;
+        auto read = [&](int i, float (&v)[16]) {                 // what moves to the run's i-th place
+            const int from = slots[path[j + i]];
+            const bool live = from >= 0 && from < limit;
+            const int b = live ? from / bs : 0;
+            const uint4 x = *reinterpret_cast<const uint4 *>(cells + b * a.c.block_stride + (live ? from % bs : 0) * a.c.token_stride + e0);
+            const float scale = scales[(long long)b * H];
+            values16<FMT>(x, scale, v);
+            if (!live) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) v[k] = 0.f;
+            }
+        };
+        unsigned most = 0;
+        for (int i = sub; i < run; i += AT_ONCE) {
+            float v[16];
+            read(i, v);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) most = max(most, __float_as_uint(v[k]) & 0x7fffffffu);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+        float *scale = scales + (long long)block * H;
+        const float before = offset ? *scale : 0.f;
+        const Scale s = scale_of(before, __uint_as_float(most), top_inverse);
+        if (offset && !(s.now == before)) {
+            const float ratio = __fmul_rn(before, s.inverse);
+            for (int i = sub; i < offset; i += AT_ONCE) {
+                uint4 *p = reinterpret_cast<uint4 *>(to + i * a.c.token_stride + e0);
+                float v[16];
+                values16<FMT>(*p, 1.f, v);
+                *p = entries16<FMT>(v, ratio);
+            }
+        }
+        for (int i = 0; i < run; i += AT_ONCE) {
+            float v[16];
+            if (i + sub < run) read(i + sub, v);
+            __syncwarp();                        // read before anything is written there
+            if (i + sub < run) *reinterpret_cast<uint4 *>(to + (offset + i + sub) * a.c.token_stride + e0) = entries16<FMT>(v, s.inverse);
+            __syncwarp();
+        }
+        if (lane == 0) *scale = s.now;
+        __syncwarp();
+        j += run;
+    }
+}
+
+template <int FMT> cudaError_t run(const Args &a, cudaStream_t s)
+{
+    const long long tasks = (long long)a.batch * a.c.kv_heads * 2;
+    const dim3 grid((unsigned)((tasks + kWarps - 1) / kWarps));
+    if (a.c.head_dim == 64) return launch(keep_kernel<FMT, 64>, grid, kWarps * 32, 0, s, a);
+    if (a.c.head_dim == 128) return launch(keep_kernel<FMT, 128>, grid, kWarps * 32, 0, s, a);
+    return launch(keep_kernel<FMT, 256>, grid, kWarps * 32, 0, s, a);
+}
+
+} // namespace
+
+extern "C" fluxbin_status_t fluxbin_kv_keep(const fluxbin_kv_cache_t *cache, int32_t batch, int32_t tokens, const int32_t *d_query_start,
+                                            const int32_t *d_slots, const int32_t *d_path, void *cuda_stream)
+{
+    const fluxbin_status_t st = check_cache(cache);
+    if (st != FLUXBIN_OK) return st;
+    if (batch < 1 || tokens < 0 || (int64_t)batch * cache->kv_heads * 2 / kWarps >= INT32_MAX) return FLUXBIN_ERR_RANGE;
+    if (tokens == 0) return FLUXBIN_OK;
+    if (!d_query_start || !d_slots || !d_path) return FLUXBIN_ERR_NULL;
+    if (!aligned_to(d_query_start, 4) || !aligned_to(d_slots, 4) || !aligned_to(d_path, 4)) return FLUXBIN_ERR_ALIGNMENT;
+    const Args a = {*cache, batch, tokens, d_query_start, d_slots, d_path};
+    FBD_CUDA(cache->format == FLUXBIN_CACHE_INT8 ? run<FLUXBIN_CACHE_INT8>(a, (cudaStream_t)cuda_stream) : run<FLUXBIN_CACHE_E4M3>(a, (cudaStream_t)cuda_stream));
+    return FLUXBIN_OK;
+}

@@ -1,0 +1,37 @@
+// Attention of drafted tokens that see the cache and, of each other, what their masks say (fluxbin_kv_attend_tree).
+#include "fluxbin_kv_attend.cuh"
+
+extern "C" size_t fluxbin_kv_attend_tree_workspace_size(int32_t batch, int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim)
+{
+    return fluxbin_kv_attend_workspace_size(batch, tokens, q_heads, kv_heads, head_dim);
+}
+
+extern "C" fluxbin_status_t fluxbin_kv_attend_tree(const fluxbin_kv_cache_t *cache, int32_t dtype, int32_t batch, int32_t tokens,
+                                                   const void *d_q, int32_t q_heads, int64_t q_token, int64_t q_head,
+                                                   const int32_t *d_query_start, const int32_t *d_lengths,
+                                                   const int32_t *d_tree, int64_t tree_stride, int32_t tree_words,
+                                                   const int32_t *d_block_table, int64_t block_table_stride, int32_t block_table_width,
+                                                   float scale, void *d_out, int64_t out_token, int64_t out_head, float *d_lse,
+                                                   void *d_workspace, size_t ws_bytes, void *cuda_stream)
+{
+    const fluxbin_status_t st = check_cache(cache);
+    if (st != FLUXBIN_OK) return st;
+    if (dtype != FLUXBIN_TYPE_FP16 && dtype != FLUXBIN_TYPE_BF16) return FLUXBIN_ERR_UNSUPPORTED;
+    if (batch < 1 || tokens < 0 || q_heads < 1 || q_heads > 65535 || q_heads % cache->kv_heads != 0 || block_table_width < 1 ||
+        (block_table_stride != 0 && block_table_stride < block_table_width) || (!d_query_start && tokens != batch) || tree_words < 1 ||
+        tree_words > INT32_MAX / 32 || tree_stride < 0 || (int64_t)tokens * (q_heads / cache->kv_heads) > INT32_MAX) return FLUXBIN_ERR_RANGE;
+    if (tokens == 0) return FLUXBIN_OK;
+    if (!d_q || !d_out || !d_lengths || !d_block_table || !d_tree || !d_workspace) return FLUXBIN_ERR_NULL;
+    if (!aligned_to(d_q, 16) || !aligned_to(d_out, 16) || (tokens > 1 && (q_token % 8 || out_token % 8)) || (q_heads > 1 && (q_head % 8 || out_head % 8)) ||
+        !aligned_to(d_query_start, 4) || !aligned_to(d_lengths, 4) || !aligned_to(d_block_table, 4) || !aligned_to(d_tree, 4) || !aligned_to(d_lse, 4) ||
+        !aligned_to(d_workspace, 16)) return FLUXBIN_ERR_ALIGNMENT;
+    if (!heads_apart(tokens, q_heads, out_token, out_head, cache->head_dim)) return FLUXBIN_ERR_RANGE;
+    if (ws_bytes < fluxbin_kv_attend_tree_workspace_size(batch, tokens, q_heads, cache->kv_heads, cache->head_dim)) return FLUXBIN_ERR_BUFFER_TOO_SMALL;
+    const Args a = {*cache, batch, tokens, q_heads, block_table_width, d_q, q_token, q_head, d_query_start, d_lengths, d_block_table,
+                    block_table_stride, scale, d_out, out_token, out_head, d_lse,
+                    (unsigned *)d_workspace, (unsigned *)d_workspace + 1, (float *)((char *)d_workspace + kCounterBytes),
+                    (float *)((char *)d_workspace + kCounterBytes + kLseBytes), (const uint32_t *)d_tree, tree_stride, tree_words};
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    FBD_CUDA((dtype == FLUXBIN_TYPE_FP16 ? run_dim<__half, true>(a, s) : run_dim<__nv_bfloat16, true>(a, s)));
+    return FLUXBIN_OK;
+}

@@ -45,7 +45,9 @@ EXPORTS = ["fluxbin_packed_size", "fluxbin_validate", "fluxbin_pack_host", "flux
            "fluxbin_rc_decomp", "fluxbin_rc_decomp_workspace_size", "fluxbin_rc_decomp_passes",
            "fluxbin_rc_salient_collect", "fluxbin_pack_device", "fluxbin_pack_device_workspace_size", "fluxbin_rc_salient_residual",
            "fluxbin_rotary_frequencies", "fluxbin_rotary", "fluxbin_kv_validate", "fluxbin_kv_append", "fluxbin_kv_read",
-           "fluxbin_kv_attend_workspace_size", "fluxbin_kv_attend", "fluxbin_kv_advance", "fluxbin_call_words"]
+           "fluxbin_kv_attend_workspace_size", "fluxbin_kv_attend", "fluxbin_kv_advance", "fluxbin_norm_rotary",
+           "fluxbin_norm_rotary_backward", "fluxbin_norm_rotary_backward_workspace_size", "fluxbin_draft_tree", "fluxbin_draft_accept",
+           "fluxbin_kv_attend_tree", "fluxbin_kv_attend_tree_workspace_size", "fluxbin_kv_keep", "fluxbin_call_words"]
 
 TYPE_FP16, TYPE_FP32, TYPE_BF16 = 0, 1, 2
 CACHE_INT8, CACHE_E4M3 = 0, 1
@@ -149,6 +151,18 @@ def _lib():
         lib.fluxbin_kv_attend.argtypes = [vp, i32, i32, i32] + heads + [vp, vp, vp, i64, i32, f32, vp, i64, i64, vp, vp, sz, vp]
         lib.fluxbin_kv_advance.restype = ctypes.c_int
         lib.fluxbin_kv_advance.argtypes = [i32, i32, i32, vp, vp, vp, i64, i32, vp, i32] + [vp] * 8 + [vp]
+        out = [vp, i64, i64]
+        lib.fluxbin_norm_rotary.restype = ctypes.c_int
+        lib.fluxbin_norm_rotary.argtypes = [vp, f32, i32, i32, i32, vp] + (heads + [vp] + out) * 2 + [vp]
+        lib.fluxbin_norm_rotary_backward.restype = ctypes.c_int
+        lib.fluxbin_norm_rotary_backward.argtypes = [vp, f32, i32, i32, i32, vp] + (heads + [vp] + out + out + [vp]) * 2 + [vp, sz, vp]
+        lib.fluxbin_norm_rotary_backward_workspace_size.restype, lib.fluxbin_norm_rotary_backward_workspace_size.argtypes = sz, [i32]
+        lib.fluxbin_draft_tree.restype, lib.fluxbin_draft_tree.argtypes = ctypes.c_int, [i32] * 3 + [vp] * 6
+        lib.fluxbin_draft_accept.restype, lib.fluxbin_draft_accept.argtypes = ctypes.c_int, [i32] * 3 + [vp] * 9
+        lib.fluxbin_kv_attend_tree_workspace_size.restype, lib.fluxbin_kv_attend_tree_workspace_size.argtypes = sz, [i32] * 5
+        lib.fluxbin_kv_attend_tree.restype = ctypes.c_int
+        lib.fluxbin_kv_attend_tree.argtypes = [vp, i32, i32, i32] + heads + [vp, vp, vp, i64, i32, vp, i64, i32, f32, vp, i64, i64, vp, vp, sz, vp]
+        lib.fluxbin_kv_keep.restype, lib.fluxbin_kv_keep.argtypes = ctypes.c_int, [vp, i32, i32, vp, vp, vp, vp]
         lib.fluxbin_call_words.restype, lib.fluxbin_call_words.argtypes = ctypes.c_int, [i32, ctypes.c_char_p]
         _LIB = lib
     return _LIB
@@ -513,6 +527,39 @@ def kv_advance_status(*args) -> int:
     return _lib().fluxbin_kv_advance(*args)
 
 
+def norm_rotary_status(*args) -> int:
+    """fluxbin_norm_rotary with the arguments of the C call (the descriptor by ctypes.byref)."""
+    return _lib().fluxbin_norm_rotary(*args)
+
+
+def norm_rotary_backward_status(*args) -> int:
+    return _lib().fluxbin_norm_rotary_backward(*args)
+
+
+def norm_rotary_backward_workspace_size(head_dim: int) -> int:
+    return int(_lib().fluxbin_norm_rotary_backward_workspace_size(head_dim))
+
+
+def draft_tree_status(*args) -> int:
+    return _lib().fluxbin_draft_tree(*args)
+
+
+def draft_accept_status(*args) -> int:
+    return _lib().fluxbin_draft_accept(*args)
+
+
+def kv_attend_tree_status(*args) -> int:
+    return _lib().fluxbin_kv_attend_tree(*args)
+
+
+def kv_attend_tree_workspace_size(batch: int, tokens: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(_lib().fluxbin_kv_attend_tree_workspace_size(batch, tokens, q_heads, kv_heads, head_dim))
+
+
+def kv_keep_status(*args) -> int:
+    return _lib().fluxbin_kv_keep(*args)
+
+
 class Words:
     """One of the calls above through fluxbin_call_words: called with the C call's arguments (None is not an integer: 0)."""
 
@@ -527,9 +574,15 @@ class Words:
             raise FluxBinError(status, self.where)
 
 
-# (pointers as unsigned words, everything else signed; the scale of an attention as a double)
+# (pointers as unsigned words, everything else signed; the scale of an attention and the eps of a norm as doubles)
 rotary_call = Words(0, "=Q3qQQ3qQ2qQ3qQ2qQ", "fluxbin_rotary")
 kv_append_call = Words(1, "=Q2qQQ2qQ2qQQQ3qQ2qQ", "fluxbin_kv_append")
 kv_read_call = Words(2, "=Q2qQQQQ", "fluxbin_kv_read")
 kv_attend_call = Words(3, "=Q3qQ3qQQQ2qdQ2qQQQQ", "fluxbin_kv_attend")
 kv_advance_call = Words(4, "=3qQQQ2qQq9Q", "fluxbin_kv_advance")
+norm_rotary_call = Words(16, "=Qd3qQ" + "Q3qQQ2q" * 2 + "Q", "fluxbin_norm_rotary")
+norm_rotary_backward_call = Words(17, "=Qd3qQ" + "Q3qQQ2qQ2qQ" * 2 + "QQQ", "fluxbin_norm_rotary_backward")
+draft_tree_call = Words(18, "=3q6Q", "fluxbin_draft_tree")
+draft_accept_call = Words(19, "=3q9Q", "fluxbin_draft_accept")
+kv_attend_tree_call = Words(20, "=Q3qQ3qQQQ2qQ2qdQ2qQQQQ", "fluxbin_kv_attend_tree")
+kv_keep_call = Words(21, "=Q2qQQQQ", "fluxbin_kv_keep")
