@@ -34,6 +34,31 @@
 #include "fluxbin_cache.cuh"
 
 #include <atomic>
+#include <type_traits>
+
+namespace fbd {
+
+struct AttendArgs {
+    fluxbin_kv_cache_t c;
+    int batch, tokens, q_heads, width;
+    const void *q;
+    long long q_token, q_head;
+    const int *query_start, *lengths, *table;
+    long long table_stride;
+    float scale;
+    void *out;
+    long long out_token, out_head;
+    float *lse;
+    unsigned *drawn;                            // shares drawn so far
+    unsigned *arrived;                          // [kMaxShares], by the share in which a cut job begins
+    float *partial_lse;                         // [shares][2][rows], base 2
+    float *partial;                             // [shares][2][rows][D]
+    const uint32_t *tree;                       // TREE: bit j of a token's words: it sees its request's j-th new token
+    long long tree_stride;
+    int tree_words;
+};
+
+} // namespace fbd
 
 using namespace fbd;
 
@@ -66,25 +91,7 @@ constexpr int kMaxLength = INT32_MAX - 4095;    // rounded up to units it is sti
 constexpr float kNoRef = -3e38f;                // the reference before the first score: below every one, and finite
 constexpr int kMaxSms = 160, kMaxShares = kMaxSms * 3 * 2;
 
-struct Args {
-    fluxbin_kv_cache_t c;
-    int batch, tokens, q_heads, width;
-    const void *q;
-    long long q_token, q_head;
-    const int *query_start, *lengths, *table;
-    long long table_stride;
-    float scale;
-    void *out;
-    long long out_token, out_head;
-    float *lse;
-    unsigned *drawn;                            // shares drawn so far
-    unsigned *arrived;                          // [kMaxShares], by the share in which a cut job begins
-    float *partial_lse;                         // [shares][2][rows], base 2
-    float *partial;                             // [shares][2][rows][D]
-    const uint32_t *tree;                       // TREE: bit j of a token's words: it sees its request's j-th new token
-    long long tree_stride;
-    int tree_words;
-};
+using Args = AttendArgs;
 
 // ---- conversions of 8-bit entries ------------------------------------------------------------------------
 
@@ -854,11 +861,13 @@ template <int D, int FMT, typename T, bool TREE> cudaError_t run_rows(const Args
     // 8190 tokens: 24 rows 109 us against 117 in one tile, 32 112 against 119, 40 169 against 122, 64 213 in both, 72 256 against
     // 215 in two, 112 337 against 324 in three; at 64 tiles of 40 never won)
     const long long rows = (long long)(a.q_heads / a.c.kv_heads) * ((a.tokens + a.batch - 1) / a.batch);
-    if constexpr (D == 128) {
+    if constexpr (!TREE && D == 128) {
         if ((rows + 39) / 40 * 11 < (rows + 15) / 16 * 5) return run<D, FMT, 5, T, TREE>(a, s);
     }
     // (9 to 16 rows in one tile of 16 instead of two of 8: 68 against 80 us at 128, 92 against 138 at 256, 41 against 48 at 64)
-    if (rows > 8) return run<D, FMT, 2, T, TREE>(a, s);
+    if constexpr (!TREE) {                       // (many rows of trees are another kernel's)
+        if (rows > 8) return run<D, FMT, 2, T, TREE>(a, s);
+    }
     return run<D, FMT, 1, T, TREE>(a, s);
 }
 template <int D, typename T, bool TREE> cudaError_t run_format(const Args &a, cudaStream_t s)

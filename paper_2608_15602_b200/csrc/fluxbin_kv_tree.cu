@@ -1,9 +1,35 @@
 // Attention of drafted tokens that see the cache and, of each other, what their masks say (fluxbin_kv_attend_tree).
-#include "fluxbin_kv_attend.cuh"
+#include "fluxbin_kv_tree.cuh"
+
+namespace {
+
+// rows that share a key head in an average request: the kernel for few rows has tiles of 8
+constexpr long long kFewRows = 8;
+
+// A workspace of both kernels: the counters of the one for few rows, the partial results of either (of one call at a time), the
+// counters of this one -- behind all that the other writes, since each finds its own zeroed.
+size_t counters_at(int head_dim)
+{
+    const size_t few = kCounterBytes + kLseBytes * (1 + (size_t)head_dim), many = kCounterBytes + kTreeLseBytes * (1 + (size_t)head_dim);
+    return few > many ? few : many;
+}
+template <typename T> cudaError_t run_type(Args a, char *workspace, cudaStream_t s)
+{
+    const long long rows = (long long)(a.q_heads / a.c.kv_heads) * ((a.tokens + a.batch - 1) / a.batch);
+    if (rows <= kFewRows) return run_dim<T, true>(a, s);
+    a.arrived = (unsigned *)(workspace + counters_at(a.c.head_dim));
+    a.partial_lse = (float *)(workspace + kCounterBytes);
+    a.partial = (float *)(workspace + kCounterBytes + kTreeLseBytes);
+    const bool bf16 = !std::is_same<T, __half>::value;
+    return a.c.head_dim == 64 ? launch_tree_64(a, bf16, s) : a.c.head_dim == 128 ? launch_tree_128(a, bf16, s) : launch_tree_256(a, bf16, s);
+}
+
+} // namespace
 
 extern "C" size_t fluxbin_kv_attend_tree_workspace_size(int32_t batch, int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim)
 {
-    return fluxbin_kv_attend_workspace_size(batch, tokens, q_heads, kv_heads, head_dim);
+    if (fluxbin_kv_attend_workspace_size(batch, tokens, q_heads, kv_heads, head_dim) == 0) return 0;
+    return counters_at(head_dim) + kTreeCounterBytes;
 }
 
 extern "C" fluxbin_status_t fluxbin_kv_attend_tree(const fluxbin_kv_cache_t *cache, int32_t dtype, int32_t batch, int32_t tokens,
@@ -32,6 +58,6 @@ extern "C" fluxbin_status_t fluxbin_kv_attend_tree(const fluxbin_kv_cache_t *cac
                     (unsigned *)d_workspace, (unsigned *)d_workspace + 1, (float *)((char *)d_workspace + kCounterBytes),
                     (float *)((char *)d_workspace + kCounterBytes + kLseBytes), (const uint32_t *)d_tree, tree_stride, tree_words};
     cudaStream_t s = (cudaStream_t)cuda_stream;
-    FBD_CUDA((dtype == FLUXBIN_TYPE_FP16 ? run_dim<__half, true>(a, s) : run_dim<__nv_bfloat16, true>(a, s)));
+    FBD_CUDA((dtype == FLUXBIN_TYPE_FP16 ? run_type<__half>(a, (char *)d_workspace, s) : run_type<__nv_bfloat16>(a, (char *)d_workspace, s)));
     return FLUXBIN_OK;
 }

@@ -1,0 +1,864 @@
+// Attention over the 8-bit cache for many query rows of a key head: trees of drafted tokens (fluxbin_kv_attend_tree).
+//
+// A tile of 128 query rows (the query heads that share a key head, over a request's new tokens) goes over the cached tokens,
+// kTokens at a time:
+//     S = Q K^T  [rows x tokens],   P = exp2(S c - m),   O += P V  [rows x dim],   l += sum P
+// on the matrix unit that accumulates in its own memory: a row of Q, S, P and O is a lane of it, so a softmax thread has a row to
+// itself and needs no shuffle.  The unit takes operands of 16 bits:
+//   K      8-bit entries are exact in fp16; Q is fp16, or bf16 as fp16 times a power of two, and stays in the unit's memory
+//   V      exact in bf16 (int8 as parts 1 / 64)
+//   P      times its token's value scale: two bf16 numbers, written where S was, which lose 2^-16 of it and flush nothing
+//          short of fp32's range (see the kernel for few rows); so the second product is made twice
+// The cache's bytes come in by 16 a thread, a few tiles ahead in registers, and are converted into swizzled tiles in shared memory.
+//
+// Warps: four or eight for the softmax, eight that load and convert, one that issues the products.  At head dimension 64 and 128
+// the softmax is two groups of four warps that take the tiles in turn, each with accumulators of its own; what they have at the end
+// of a job is put together as parts of the line are (at 256 the accumulators of one group fill half of the unit's memory: one
+// group).  Scores and probabilities go through three places in turn, so that the scores of the next two tiles are under way
+// while a tile's probabilities are formed.
+//
+// Every wait has a limit; one that runs out (a fault of the machine) ends the waiting of the whole CTA, and its jobs' rows become NaN.
+#ifndef FLUXBIN_KV_TREE_CUH
+#define FLUXBIN_KV_TREE_CUH
+
+#include "fluxbin_kv_attend.cuh"
+
+namespace {
+
+constexpr int kRows = 128;                   // of a tile: the lanes of the matrix unit's memory
+constexpr int kTreeJobCost = 4;              // units that it costs to begin a job
+constexpr int kMetaRing = 32;                // tiles whose scales are kept
+constexpr float kValueLag = 1048576.f;       // 2^20: value scales may pass the largest one met so far by this much before O is rescaled
+constexpr unsigned long long kWaitLimit = 2000000000ull;         // ns
+
+template <int D> struct Tree {
+    static constexpr int kTokens = D == 256 ? 32 : 64;           // of a tile
+    static constexpr int kGroups = D == 256 ? 1 : 2;             // of four softmax warps
+    static constexpr int kStages = D == 64 ? 8 : 6;              // tiles in shared memory
+    static constexpr int kAhead = D == 64 ? 4 : 2;               // tiles in a converter's registers
+    static constexpr int kConverters = 8;                        // warps
+    static constexpr int kSoft = 128 * kGroups, kThreads = kSoft + kConverters * 32 + 32;
+    static constexpr int kSlab = kTokens * 128;                  // 64 elements of every token
+    static constexpr int kSide = D / 64 * kSlab, kStageBytes = 2 * kSide;
+    // columns of the unit's memory: the sums, the queries, three places for scores and then probabilities
+    static constexpr int kO = 0, kQ = kGroups * D, kS = kQ + D / 2, kPlaces = 3, kColumns = 512;
+    static_assert(kS + kPlaces * kTokens <= kColumns, "the unit's memory");
+    // With 17 warps 96 registers a thread are there, 52224 in all: 112 for the softmax, 80 for the converters
+    static constexpr bool kSplit = kGroups == 2;
+};
+
+struct Meta { float ks[4], vs[4]; int none; };   // of a tile's groups of 16 tokens: scales, which of them are in no block
+
+// ---- barriers, fences, the matrix unit -------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t shared_address(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void barrier_init(unsigned long long &b, unsigned count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(shared_address(&b)), "r"(count) : "memory"); }
+__device__ __forceinline__ void arrive(unsigned long long &b) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(shared_address(&b)) : "memory"); }
+__device__ __forceinline__ bool try_wait(uint32_t b, unsigned parity)
+{
+    unsigned ok;
+    asm volatile("{ .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n }" : "=r"(ok) : "r"(b), "r"(parity) : "memory");
+    return ok;
+}
+__device__ __forceinline__ unsigned long long now_ns()
+{
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+// false once a wait of this CTA has run out
+__device__ __forceinline__ bool wait_for(unsigned long long &barrier, unsigned parity, int &failed)
+{
+    const uint32_t b = shared_address(&barrier);
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+        if (try_wait(b, parity)) return true;
+    const unsigned long long begin = now_ns();
+    for (;;) {
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i)
+            if (try_wait(b, parity)) return true;
+        if (*(volatile int *)&failed) return false;
+        if (now_ns() - begin > kWaitLimit) {
+            *(volatile int *)&failed = 1;
+            return false;
+        }
+    }
+}
+// the same for a whole warp, which goes on together
+__device__ __forceinline__ bool wait_together(unsigned long long &barrier, unsigned parity, int &failed) { return __all_sync(0xffffffffu, wait_for(barrier, parity, failed)); }
+template <int ID, int THREADS> __device__ __forceinline__ void sync_some() { asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(THREADS) : "memory"); }
+
+__device__ __forceinline__ void unit_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void unit_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void unit_commit(unsigned long long &b)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_address(&b)) : "memory");
+}
+// C [128 x N] (+)= A B^T, A in the unit's memory, B in shared memory
+__device__ __forceinline__ void unit_mma(uint32_t c, uint32_t a, uint64_t b, uint32_t kind, bool add)
+{
+    asm volatile("{ .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n }" ::"r"(c), "r"(a), "l"(b), "r"(kind), "r"((int)add) : "memory");
+}
+template <int REGISTERS> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGISTERS)); }
+template <int REGISTERS> __device__ __forceinline__ void leave_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGISTERS)); }
+// What a product is told about its operands: fp32 sums; A and B of fp16 (0) or bf16 (1); whether B's rows lie along its columns; sizes
+__host__ __device__ constexpr uint32_t unit_kind(int type, bool b_turned, int n) { return 1u << 4 | (uint32_t)type << 7 | (uint32_t)type << 10 | (uint32_t)b_turned << 16 | (uint32_t)(n / 8) << 17 | (uint32_t)(kRows / 16) << 24; }
+// An operand in shared memory: rows of 128 bytes whose 16-byte pieces are swizzled by the row's number, eight rows every 1024 bytes; `slab`
+// is the stride between pieces of 64 elements along the rows (used where rows lie along the operand's columns)
+__device__ __forceinline__ uint64_t operand(uint32_t address, uint32_t slab)
+{
+    return (uint64_t)(address >> 4) | (uint64_t)(slab >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+
+template <int N> struct Columns { uint32_t w[N]; };
+__device__ __forceinline__ void load_columns(uint32_t from, uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, "
+                 "%26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+                   "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+                   "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(from) : "memory");
+}
+__device__ __forceinline__ void load_columns(uint32_t from, uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+                   "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(from) : "memory");
+}
+__device__ __forceinline__ void store_columns(uint32_t to, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(to), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+                 "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void store_columns(uint32_t to, const uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(to), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]),
+                 "r"(r[7]) : "memory");
+}
+__device__ __forceinline__ void loads_done() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void stores_done() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// ---- the line of work ------------------------------------------------------------------------------------
+// As in the kernel for few rows: jobs (request, head, tile of rows) of kTreeJobCost units and their pieces, a range for each CTA.
+// Every role walks its CTA's range by itself.
+
+struct Job {
+    int r, h, row0, rows, p0, p1, tiles;
+    long long begin;                             // of its units on the line
+    int span;
+};
+template <int D> struct Walk {
+    long long u, u_end, before;
+    int r;
+    Request rq;
+    Job j;
+    __device__ __forceinline__ long long units(const Args &a) const { return (long long)rq.row_tiles * a.c.kv_heads * (rq.pieces + kTreeJobCost); }
+    // the next job of a warp whose lanes all ask
+    __device__ __forceinline__ bool next(const Args &a, int lane)
+    {
+        Walk w = *this;
+        const bool any = w.step(a);
+        __syncwarp();
+        if (lane == 0) *this = w;
+        __syncwarp();
+        return any;
+    }
+    __device__ __forceinline__ bool step(const Args &a)
+    {
+        const int G = a.q_heads / a.c.kv_heads;
+        while (u < u_end) {
+            while (u >= before + units(a)) {
+                before += units(a);
+                rq = request_of<kRows, Tree<D>::kTokens>(a, ++r);
+            }
+            j.span = rq.pieces + kTreeJobCost;
+            const int job = (int)((u - before) / j.span);
+            j.begin = before + (long long)job * j.span;
+            j.p0 = max((int)(u - j.begin) - kTreeJobCost, 0);
+            j.p1 = (int)min(u_end - j.begin, (long long)j.span) - kTreeJobCost;
+            u = min(u_end, j.begin + j.span);
+            if (j.p1 <= j.p0) continue;
+            j.r = r;
+            j.h = job / rq.row_tiles;
+            j.row0 = job % rq.row_tiles * kRows;
+            j.rows = (int)min((long long)kRows, (long long)rq.count * G - j.row0);
+            j.tiles = max(min(j.p1, (rq.length + Tree<D>::kTokens - 1) / Tree<D>::kTokens) - j.p0, 0);
+            return true;
+        }
+        return false;
+    }
+};
+
+template <int D> struct TreeShared {
+    float factor[2][kRows];                      // by the parity of the job, as all that is
+    uint32_t nan[2][kRows][D / 32];
+    int any_nan[2];
+    float m[2][kRows], l[2][kRows], vref[2];     // of the two softmax groups
+    float join_max[kRows], join_inv[kRows], join_lse[kRows];
+    Meta meta[kMetaRing];
+    unsigned long long full[Tree<D>::kStages], free[Tree<D>::kStages];
+    unsigned long long q_full, q_free, s_full[3], p_full[3], pv_done[3], ended[2], drained;
+    long long place[Tree<D>::kConverters][2][32];                // of each converting warp: where 16 tokens lie, -1 for no block
+    long long scan[32], before;
+    int request, last, failed;
+    uint32_t columns;
+    Walk<D> walk[Tree<D>::kThreads / 32];        // of each warp: in registers only while it is looked at
+};
+
+// which of the tokens tok .. tok + 63 a row sees: those before the new ones, of those what its mask says, none past the length
+__device__ __forceinline__ unsigned long long seen_bits(const Args &a, const Request &rq, int row, int tok)
+{
+    const int base = rq.length - rq.count, lead = min(max(base - tok, 0), 64), valid = rq.length - tok;
+    unsigned long long bits = ~0ull;
+    if (lead < 64) {
+        const int j = max(tok - base, 0), w = j / 32, sh = j % 32;
+        const uint32_t *words = a.tree + (long long)(rq.first + row / (a.q_heads / a.c.kv_heads)) * a.tree_stride;
+        const unsigned long long w0 = w < a.tree_words ? words[w] : 0u, w1 = w + 1 < a.tree_words ? words[w + 1] : 0u, w2 = w + 2 < a.tree_words ? words[w + 2] : 0u;
+        unsigned long long window = (w0 | w1 << 32) >> sh;
+        if (sh) window |= w2 << (64 - sh);
+        bits = window << lead | ((1ull << lead) - 1);
+    }
+    return valid >= 64 ? bits : valid <= 0 ? 0 : bits & ((1ull << valid) - 1);
+}
+
+// ---- the converters --------------------------------------------------------------------------------------
+
+template <int FMT> __device__ __forceinline__ void key_chunks(const uint4 &x, uint4 &lo, uint4 &hi)
+{
+    to_half4<FMT>(x.x, lo.x, lo.y);
+    to_half4<FMT>(x.y, lo.z, lo.w);
+    to_half4<FMT>(x.z, hi.x, hi.y);
+    to_half4<FMT>(x.w, hi.z, hi.w);
+}
+template <int FMT> __device__ __forceinline__ void to_bfloat4(uint32_t x, uint32_t &lo, uint32_t &hi);
+// (as to_bfloat2x4, of four elements of one token)
+template <> __device__ __forceinline__ void to_bfloat4<FLUXBIN_CACHE_INT8>(uint32_t x, uint32_t &lo, uint32_t &hi)
+{
+    x ^= 0x80808080u;
+    const __nv_bfloat162 up = __bfloat162bfloat162(__ushort_as_bfloat16(0x7f00)), down = __bfloat162bfloat162(__ushort_as_bfloat16(0xc000));     // 2^127, -2
+    const uint32_t a = __byte_perm(x, 0, 0x4140), b = __byte_perm(x, 0, 0x4342);
+    const __nv_bfloat162 ra = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&a), up, down), rb = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&b), up, down);
+    lo = *reinterpret_cast<const uint32_t *>(&ra);
+    hi = *reinterpret_cast<const uint32_t *>(&rb);
+}
+template <> __device__ __forceinline__ void to_bfloat4<FLUXBIN_CACHE_E4M3>(uint32_t x, uint32_t &lo, uint32_t &hi)
+{
+    uint32_t h[2];
+    to_half4<FLUXBIN_CACHE_E4M3>(x, h[0], h[1]);
+    lo = bfloat2_of_half2(*reinterpret_cast<const __half2 *>(&h[0]));
+    hi = bfloat2_of_half2(*reinterpret_cast<const __half2 *>(&h[1]));
+}
+template <int FMT> __device__ __forceinline__ void value_chunks(const uint4 &x, uint4 &lo, uint4 &hi)
+{
+    to_bfloat4<FMT>(x.x, lo.x, lo.y);
+    to_bfloat4<FMT>(x.y, lo.z, lo.w);
+    to_bfloat4<FMT>(x.z, hi.x, hi.y);
+    to_bfloat4<FMT>(x.w, hi.z, hi.w);
+}
+__device__ __forceinline__ void put16(uint32_t to, const uint4 &v) { asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory"); }
+
+template <int D, int FMT, typename T>
+__device__ __forceinline__ void convert_role(const Args &a, TreeShared<D> &sm, uint32_t stages, Walk<D> &walk, int tid)
+{
+    using C = Tree<D>;
+    constexpr int PIECES = D / 16, PASS = C::kConverters * 32 / PIECES, N = C::kTokens / PASS, AHEAD = C::kAhead, GROUPS = C::kTokens / 16, BATCH = 32 / GROUPS;
+    static_assert(PASS % 16 == 0 && AHEAD + C::kStages + BATCH + 1 <= kMetaRing, "places and scales ahead");
+    const int lane = tid & 31, warp = tid >> 5, bs = a.c.block_tokens, H = a.c.kv_heads, G = a.q_heads / H;
+    const int piece = tid % PIECES, sub = tid / PIECES;          // its 16 elements of tokens sub, sub + PASS ...
+    const uint32_t slab = piece / 4 * C::kSlab, odd = piece / 4 & 1;             // (odd slabs write their chunks in the other order: all banks)
+    bool ok = true;
+    unsigned it = 0, jobs = 0;
+    const Job &j = walk.j;
+    const Request &rq = walk.rq;
+    while (walk.next(a, lane)) {
+        const int tiles = j.tiles;
+        if (tiles == 0) continue;
+        const unsigned parity = jobs & 1;
+        // ---- what the job before the last left is done with
+        if (jobs >= 2) ok = ok && wait_together(sm.ended[parity], (jobs / 2 - 1) & 1, sm.failed);
+        for (int i = tid; i < kRows * (D / 32); i += C::kConverters * 32) sm.nan[parity][i / (D / 32)][i % (D / 32)] = 0;
+        if (tid == 0) sm.any_nan[parity] = 0;
+        sync_some<1, C::kConverters * 32>();
+
+        // ---- places of the tokens, 16 at a time: 32 of them are looked up together, well ahead, and kept in shared memory
+        const int tok0 = j.p0 * C::kTokens, base = rq.length - rq.count;
+        auto block_of = [&](int group) {
+            const int tok = tok0 + group * 16;
+            if (group >= tiles * GROUPS || tok >= rq.length) return -1;
+            const int id = a.table[j.r * a.table_stride + tok / bs];
+            return id >= 0 && id < a.c.num_blocks ? id : -1;
+        };
+        struct Place { long long at; float ks, vs; };
+        auto place_of = [&](int id, int group) {
+            Place x = {-1, 0.f, 0.f};
+            if (id >= 0) {
+                x.at = id * a.c.block_stride + (tok0 + group * 16) % bs * a.c.token_stride;
+                if (warp == 0) {
+                    x.ks = a.c.d_k_scale[(long long)id * H + j.h];
+                    x.vs = a.c.d_v_scale[(long long)id * H + j.h];
+                }
+            }
+            return x;
+        };
+        auto keep_places = [&](const Place &x, int batch) {
+            sm.place[warp][batch & 1][lane] = x.at;
+            if (warp == 0) {
+                float vs = x.vs;
+                const int tok = tok0 + (batch * 32 + lane) * 16;
+                if (x.at >= 0 && !(vs < INFINITY) && tok + 16 > base) {
+                    // a scale that is no number, of tokens that not all rows see: 0, and noted for those that do
+                    for (int row = 0; row < j.rows; ++row)
+                        if (seen_bits(a, rq, j.row0 + row, tok) & 0xffff) {
+                            for (int d = 0; d < D / 32; ++d) atomicOr(&sm.nan[parity][row][d], 0xffffffffu);
+                            sm.any_nan[parity] = 1;
+                        }
+                    vs = 0.f;
+                }
+                Meta &m = sm.meta[(it + batch * BATCH + lane / GROUPS) % kMetaRing];
+                m.ks[lane % GROUPS] = x.ks;
+                m.vs[lane % GROUPS] = vs;
+                const unsigned none = __ballot_sync(0xffffffffu, x.at < 0);
+                if (lane % GROUPS == 0) m.none = (int)(none >> lane & ((1u << GROUPS) - 1));
+            }
+            __syncwarp();
+        };
+        keep_places(place_of(block_of(lane), lane), 0);
+        int id = -1;
+        Place ahead = {-1, 0.f, 0.f};
+        const long long mine = (long long)j.h * a.c.head_stride + sub % 16 * a.c.token_stride + piece * 16;
+        uint4 kr[AHEAD][N], vr[AHEAD][N];
+        auto load = [&](int tile, uint4 (&k)[N], uint4 (&v)[N]) {                // tiles in order
+            const int slot = tile % BATCH, batch = tile / BATCH;
+            if (slot == 0) id = block_of((batch + 1) * 32 + lane);
+            if (slot == BATCH / 2) ahead = place_of(id, (batch + 1) * 32 + lane);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const long long at = sm.place[warp][batch & 1][slot * GROUPS + (sub + i * PASS) / 16];
+                k[i] = v[i] = make_uint4(0, 0, 0, 0);
+                if (at >= 0) {
+                    k[i] = __ldcs(reinterpret_cast<const uint4 *>((const unsigned char *)a.c.d_k + (at + mine)));
+                    v[i] = __ldcs(reinterpret_cast<const uint4 *>((const unsigned char *)a.c.d_v + (at + mine)));
+                }
+            }
+            if (slot == BATCH - 1) keep_places(ahead, batch + 1);
+        };
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (i < tiles) load(i, kr[i], vr[i]);
+
+        // ---- the query rows, a lane for each: two warps share 32 rows, each writes half of their elements
+        if (jobs >= 1) ok = ok && wait_together(sm.q_free, (jobs - 1) & 1, sm.failed);
+        {
+            unit_after_sync();
+            const int row = (warp & 3) * 32 + lane, g = j.row0 + row, half = warp >> 2;
+            const bool live = row < j.rows;
+            const uint4 *x = reinterpret_cast<const uint4 *>((const T *)a.q + (long long)(rq.first + (live ? g / G : 0)) * a.q_token + (long long)(j.h * G + (live ? g % G : 0)) * a.q_head);
+            float f = a.scale * 1.4426950408889634f;
+            int e = 0;
+            if constexpr (!std::is_same<T, __half>::value) {
+                float largest = 0.f;
+#pragma unroll 4
+                for (int i = 0; i < D / 8; ++i) {
+                    const uint4 v = live ? x[i] : make_uint4(0, 0, 0, 0);
+                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) largest = fmaxf(largest, fmaxf(fabsf(__uint_as_float(w[k] << 16)), fabsf(__uint_as_float(w[k] & 0xffff0000u))));
+                }
+                e = exponent_of(largest);
+                f = ldexpf(f, e);
+            }
+            const uint32_t to = sm.columns + ((uint32_t)((warp & 3) * 32) << 16) + C::kQ + half * (D / 4);
+#pragma unroll 1
+            for (int i = 0; i < D / 16; i += 2) {
+                uint32_t w[8];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint4 v = live ? x[half * (D / 16) + i + k] : make_uint4(0, 0, 0, 0);
+                    w[4 * k] = v.x; w[4 * k + 1] = v.y; w[4 * k + 2] = v.z; w[4 * k + 3] = v.w;
+                }
+                if constexpr (!std::is_same<T, __half>::value) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) w[k] = half2_of_bf16(w[k], e);
+                }
+                store_columns(to + i * 4, w);
+            }
+            if (half == 0) sm.factor[parity][row] = f;
+            stores_done();
+            unit_before_sync();
+            __syncwarp();
+            if (lane == 0) arrive(sm.q_full);
+        }
+
+        // ---- tile after tile
+        for (int t0 = 0; t0 < tiles; t0 += AHEAD)
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const int t = t0 + i;
+                if (t >= tiles) break;
+                const unsigned n = it + t, stage = n % C::kStages;
+                if (n >= C::kStages) ok = ok && wait_together(sm.free[stage], (n / C::kStages - 1) & 1, sm.failed);
+                const uint32_t k_to = stages + stage * C::kStageBytes + slab, v_to = k_to + C::kSide;
+                const int tok = tok0 + t * C::kTokens;
+                if (FMT == FLUXBIN_CACHE_E4M3 && tok + C::kTokens > base) {
+                    // values that must not meet the probability 0 of a row that does not see them (see the kernel for few rows)
+#pragma unroll
+                    for (int k = 0; k < N; ++k) {
+                        const int token = tok + sub + k * PASS;
+                        uint32_t w[4] = {vr[i][k].x, vr[i][k].y, vr[i][k].z, vr[i][k].w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            uint32_t nan = nan_bytes(w[e]);
+                            if (token >= rq.length) w[e] = 0;
+                            else if (nan) {
+                                w[e] &= ~(nan | (nan - (nan >> 7)));
+                                for (; nan; nan &= nan - 1) {
+                                    const int d = piece * 16 + e * 4 + (__ffs(nan) - 1) / 8;
+                                    for (int row = 0; row < j.rows; ++row)
+                                        if (seen_bits(a, rq, j.row0 + row, token) & 1) atomicOr(&sm.nan[parity][row][d / 32], 1u << (d % 32));
+                                    sm.any_nan[parity] = 1;
+                                }
+                            }
+                        }
+                        vr[i][k] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const int token = sub + k * PASS;
+                    const uint32_t c0 = (piece % 4 * 2 + odd) ^ (token & 7), c1 = (piece % 4 * 2 + (odd ^ 1)) ^ (token & 7);
+                    uint4 lo, hi;
+                    key_chunks<FMT>(kr[i][k], lo, hi);
+                    put16(k_to + token * 128 + (c0 << 4), odd ? hi : lo);
+                    put16(k_to + token * 128 + (c1 << 4), odd ? lo : hi);
+                    value_chunks<FMT>(vr[i][k], lo, hi);
+                    put16(v_to + token * 128 + (c0 << 4), odd ? hi : lo);
+                    put16(v_to + token * 128 + (c1 << 4), odd ? lo : hi);
+                }
+                if (t + AHEAD < tiles) load(t + AHEAD, kr[i], vr[i]);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) arrive(sm.full[stage]);
+            }
+        it += tiles;
+        ++jobs;
+    }
+}
+
+// ---- the products ----------------------------------------------------------------------------------------
+
+template <int D>
+__device__ __forceinline__ void product_role(const Args &a, TreeShared<D> &sm, uint32_t stages, Walk<D> walk)
+{
+    using C = Tree<D>;
+    constexpr int LOOK = C::kPlaces - 1;         // tiles whose scores are asked for ahead
+    constexpr uint32_t kScores = unit_kind(0, false, C::kTokens), kValues = unit_kind(1, true, D);
+    const uint32_t unit = sm.columns;
+    unsigned it = 0, jobs = 0;
+    const Job &j = walk.j;
+    auto run = [&]() -> bool {
+        while (walk.step(a)) {
+            if (j.tiles == 0) continue;
+            if (!wait_for(sm.q_full, jobs & 1, sm.failed)) return false;
+            for (int step = 0; step < j.tiles + LOOK; ++step) {
+                if (step < j.tiles) {
+                    const unsigned n = it + step, stage = n % C::kStages, place = n % C::kPlaces;
+                    if (!wait_for(sm.full[stage], n / C::kStages & 1, sm.failed)) return false;
+                    if (n >= C::kPlaces && !wait_for(sm.pv_done[place], (n / C::kPlaces - 1) & 1, sm.failed)) return false;
+                    unit_after_sync();
+                    const uint64_t keys = operand(stages + stage * C::kStageBytes, 16);
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+                        unit_mma(unit + C::kS + place * C::kTokens, unit + C::kQ + k * 8, keys + ((k / 4 * C::kSlab + k % 4 * 32) >> 4), kScores, k > 0);
+                    unit_commit(sm.s_full[place]);
+                    if (step == j.tiles - 1) unit_commit(sm.q_free);
+                }
+                if (step >= LOOK) {
+                    const int t = step - LOOK;
+                    const unsigned n = it + t, stage = n % C::kStages, place = n % C::kPlaces;
+                    if (!wait_for(sm.p_full[place], n / C::kPlaces & 1, sm.failed)) return false;
+                    unit_after_sync();
+                    const uint64_t values = operand(stages + stage * C::kStageBytes + C::kSide, C::kSlab);
+                    const uint32_t o = unit + C::kO + n % C::kGroups * D, p = unit + C::kS + place * C::kTokens;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+#pragma unroll
+                        for (int k = 0; k < C::kTokens / 16; ++k)
+                            unit_mma(o, p + half * (C::kTokens / 2) + k * 8, values + (k * 2048 >> 4), kValues, t >= C::kGroups || half > 0 || k > 0);
+                    unit_commit(sm.pv_done[place]);
+                    unit_commit(sm.free[stage]);
+                }
+            }
+            it += j.tiles;
+            ++jobs;
+        }
+        return true;
+    };
+    if (!run()) {                                // what is under way has to end before the unit's memory is given back
+        unit_commit(sm.drained);
+        int own = 0;
+        wait_for(sm.drained, 0, own);
+    }
+}
+
+// ---- the softmax -----------------------------------------------------------------------------------------
+
+template <int D, int FMT, typename T>
+__device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, Walk<D> &walk, long long size, long long over, int tid)
+{
+    using C = Tree<D>;
+    constexpr int N = C::kTokens, GROUPS = C::kGroups;
+    const int lane = tid & 31, warp = tid >> 5, group = warp / 4, row = tid % 128, H = a.c.kv_heads, G = a.q_heads / H;
+    const uint32_t unit = sm.columns + ((uint32_t)(warp % 4 * 32) << 16);
+    const long long share = blockIdx.x;
+    bool ok = true;
+    unsigned it = 0, jobs = 0;
+    const Job &j = walk.j;
+    const Request &rq = walk.rq;
+    while (walk.next(a, lane)) {
+        const int tiles = j.tiles;
+        const unsigned parity = jobs & 1;
+        const bool live = warp % 4 * 32 < j.rows;                // (the rows of a warp are all past the end, or not)
+        const int base = rq.length - rq.count, my_row = min(row, j.rows - 1);
+        float ref = kNoRef, sum = 0.f, vref = 0.f, vref_inverse = 0.f, factor = 0.f;
+        const int t_first = (group - (int)it) & (GROUPS - 1);    // tiles go to the groups in turn, from job to job
+        for (int t = t_first; t < tiles; t += GROUPS) {
+            const unsigned n = it + t, place = n % C::kPlaces;
+            ok = ok && wait_together(sm.full[n % C::kStages], n / C::kStages & 1, sm.failed) && wait_together(sm.s_full[place], n / C::kPlaces & 1, sm.failed);
+            if (!ok) break;
+            if (t == t_first) factor = sm.factor[parity][row];
+            if (live) {
+                unit_after_sync();
+                const uint32_t at = unit + C::kS + place * N;
+                uint32_t s[N];
+#pragma unroll
+                for (int i = 0; i < N; i += 32) load_columns(at + i, reinterpret_cast<uint32_t (&)[32]>(s[i]));
+                const Meta &m = sm.meta[n % kMetaRing];
+                const int tok = (j.p0 + t) * N;
+                float c[N / 16], vf[N / 16], vmax = 0.f;
+#pragma unroll
+                for (int i = 0; i < N / 16; ++i) {
+                    c[i] = factor * m.ks[i];
+                    vf[i] = m.vs[i];
+                    if (vf[i] < INFINITY) vmax = fmaxf(vmax, vf[i]);
+                }
+                const bool edge = tok + N > base || m.none;
+                unsigned long long bits = ~0ull;
+                if (edge) {
+                    bits = seen_bits(a, rq, j.row0 + my_row, tok);
+#pragma unroll
+                    for (int i = 0; i < N / 16; ++i)
+                        if (m.none >> i & 1) bits &= ~(0xffffull << (i * 16));
+                }
+                // ---- the largest score against the lagging reference
+                loads_done();
+                float most = -INFINITY;
+                float *x = reinterpret_cast<float *>(s);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    x[i] *= c[i / 16];
+                    if (edge && !(bits >> i & 1)) x[i] = -INFINITY;
+                    most = fmaxf(most, x[i]);
+                }
+                float rescale = 1.f;
+                if (most > ref + 15.f) {
+                    const float now = most - 7.f;
+                    rescale = exp2_fast(ref - now);
+                    ref = now;
+                    sum *= rescale;
+                }
+                if (vmax >= 7.888609052210118e-31f && (vref == 0.f || vmax > vref * kValueLag)) {        // (the same for every row)
+                    rescale *= vref / vmax;
+                    vref = vmax;
+                    vref_inverse = kPart<FMT> / vmax;
+                }
+                if (t >= GROUPS && __any_sync(0xffffffffu, rescale != 1.f)) {
+                    const unsigned before = n - GROUPS;          // the last tile that went to the same sums
+                    ok = wait_together(sm.pv_done[before % C::kPlaces], before / C::kPlaces & 1, sm.failed);
+                    unit_after_sync();
+                    const uint32_t o = unit + C::kO + group * D;
+#pragma unroll 1
+                    for (int i = 0; i < D; i += 16) {
+                        uint32_t v[16];
+                        load_columns(o + i, v);
+                        loads_done();
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * rescale);
+                        store_columns(o + i, v);
+                    }
+                }
+                // ---- probabilities, 16 tokens at a time
+#pragma unroll
+                for (int i = 0; i < N / 16; ++i) {
+                    const float f = edge && !(vf[i] < INFINITY) ? 0.f : vf[i] * vref_inverse;
+                    uint32_t upper[8], rest[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const float p0 = exp2_fast(x[i * 16 + 2 * k] - ref), p1 = exp2_fast(x[i * 16 + 2 * k + 1] - ref);
+                        sum += p0 + p1;
+                        split_bfloat2(p0 * f, p1 * f, upper[k], rest[k]);
+                    }
+                    store_columns(at + i * 8, upper);
+                    store_columns(at + N / 2 + i * 8, rest);
+                }
+                stores_done();
+                unit_before_sync();
+            }
+            __syncwarp();
+            if (lane == 0) arrive(sm.p_full[place]);
+        }
+        // ---- the end of the job: sums of both groups
+        sm.m[group][row] = ref;
+        sm.l[group][row] = sum;
+        if (row == 0) sm.vref[group] = vref;
+        if (tiles > 0) {                       // (the products end in order)
+            const unsigned n = it + tiles - 1;
+            ok = ok && wait_together(sm.pv_done[n % C::kPlaces], n / C::kPlaces & 1, sm.failed);
+        }
+        sync_some<2, C::kSoft>();
+        unit_after_sync();
+        const bool whole = j.p0 == 0 && j.p1 == rq.pieces;
+        const long long slot = share * 2 + (j.p0 == 0);
+        float *part = a.partial + slot * kRows * D, *part_lse = a.partial_lse + slot * kRows;
+        auto write_out = [&](int r, int d, const float (&v)[4], float lse2) {
+            const int g = j.row0 + r, head = j.h * G + g % G;
+            const long long tok = rq.first + g / G;
+            T *op = (T *)a.out + tok * a.out_token + (long long)head * a.out_head + d;
+            __align__(8) T e[4] = {from_float<T>(v[0]), from_float<T>(v[1]), from_float<T>(v[2]), from_float<T>(v[3])};
+            *reinterpret_cast<uint2 *>(op) = *reinterpret_cast<const uint2 *>(e);
+            if (d == 0 && a.lse) a.lse[tok * a.q_heads + head] = lse2 * 0.6931471805599453f;
+        };
+        if (live) {
+            float m = -INFINITY, l = 0.f, f[GROUPS];
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) m = fmaxf(m, sm.m[g][row]);
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                const float lg = sm.l[g][row];
+                f[g] = lg == 0.f ? 0.f : exp2_fast(sm.m[g][row] - m);
+                l += f[g] * lg;
+            }
+            if (!ok) l = NAN;
+            const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m + log2f(l);
+            const bool any_nan = tiles > 0 && sm.any_nan[parity];
+#pragma unroll 1
+            for (int d0 = group * (D / GROUPS); d0 < (group + 1) * (D / GROUPS); d0 += 16) {
+                float v[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) v[k] = ok ? 0.f : NAN;
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g) {
+                    if (tiles <= ((g - (int)it) & (GROUPS - 1)) || !ok) continue;           // no tile was this group's
+                    uint32_t o[16];
+                    load_columns(unit + C::kO + g * D + d0, o);
+                    loads_done();
+                    const float fv = f[g] * sm.vref[g];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) v[k] += fv * (__uint_as_float(o[k]) * inv);
+                }
+                if (any_nan) {
+                    const uint32_t nan = sm.nan[parity][row][d0 / 32] >> (d0 % 32);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        if (nan >> k & 1) v[k] = NAN;
+                }
+                if (row < j.rows) {
+#pragma unroll
+                    for (int k = 0; k < 16; k += 4) {
+                        const float e[4] = {v[k], v[k + 1], v[k + 2], v[k + 3]};
+                        if (whole) write_out(row, d0 + k, e, lse2);
+                        else *reinterpret_cast<float4 *>(part + row * D + d0 + k) = make_float4(e[0], e[1], e[2], e[3]);
+                    }
+                    if (!whole && d0 == 0) part_lse[row] = lse2;
+                }
+            }
+            unit_before_sync();
+        }
+        if (!whole) {
+            // the CTAs that hold parts of this job, by the cut of the line
+            auto owner = [&](long long x) { return x < over * (size + 1) ? x / (size + 1) : over + (x - over * (size + 1)) / size; };
+            const int c0 = (int)owner(j.begin + kTreeJobCost), c1 = (int)owner(j.begin + j.span - 1);
+            __threadfence();
+            sync_some<2, C::kSoft>();
+            if (tid == 0) sm.last = atomicAdd(&a.arrived[c0], 1u) == (unsigned)(c1 - c0);
+            sync_some<2, C::kSoft>();
+            if (sm.last) {
+                __threadfence();
+                const int parts = c1 - c0 + 1;
+                auto slot_of = [&](int c) { return (long long)(c0 + c) * 2 + (c == 0); };
+                for (int r = warp; r < j.rows; r += C::kSoft / 32) {
+                    float m = -INFINITY, l = 0.f;
+                    for (int c = lane; c < parts; c += 32) {
+                        const float x = __ldcg(a.partial_lse + slot_of(c) * kRows + r), m_now = fmaxf(m, x);
+                        l = l * (m == -INFINITY ? 0.f : exp2_fast(m - m_now)) + (x == -INFINITY ? 0.f : exp2_fast(x - m_now));
+                        m = m_now;
+                    }
+                    float top = m;
+                    for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+                    l *= m == -INFINITY ? (l == l ? 0.f : 1.f) : exp2_fast(m - top);
+                    for (int x = 16; x; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+                    if (lane == 0) {
+                        sm.join_max[r] = top == -INFINITY ? 0.f : top;
+                        sm.join_inv[r] = l == 0.f ? 0.f : 1.f / l;
+                        sm.join_lse[r] = l == 0.f ? -INFINITY : top + log2f(l);
+                    }
+                }
+                sync_some<2, C::kSoft>();
+                for (int i = tid; i < j.rows * (D / 4); i += C::kSoft) {
+                    const int r = i / (D / 4), d = i % (D / 4) * 4;
+                    float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+                    for (int c = 0; c < parts; ++c) {
+                        const float f = exp2_fast(__ldcg(a.partial_lse + slot_of(c) * kRows + r) - sm.join_max[r]) * sm.join_inv[r];
+                        const float4 y = __ldcg(reinterpret_cast<const float4 *>(a.partial + (slot_of(c) * kRows + r) * D + d));
+                        v[0] += f * y.x; v[1] += f * y.y; v[2] += f * y.z; v[3] += f * y.w;
+                    }
+                    write_out(r, d, v, sm.join_lse[r]);
+                }
+                if (tid == 0) a.arrived[c0] = 0;
+            }
+        }
+        sync_some<2, C::kSoft>();                // both groups have read the sums, which the next job's products write
+        if (tiles > 0) {
+            if (tid == 0) arrive(sm.ended[parity]);
+            ++jobs;
+        }
+        it += tiles;
+    }
+}
+
+template <int D, int FMT, typename T>
+__global__ void __launch_bounds__(Tree<D>::kThreads, 1) tree_attend_kernel(const __grid_constant__ Args a)
+{
+    using C = Tree<D>;
+    extern __shared__ unsigned char smem_tree[];
+    const uint32_t tiles = (shared_address(smem_tree) + 1023) & ~1023u;
+    TreeShared<D> &sm = *reinterpret_cast<TreeShared<D> *>(smem_tree + (tiles - shared_address(smem_tree)) + C::kStages * C::kStageBytes);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+    let_successor_start();
+    wait_for_predecessor();
+    if (a.query_start) empty_rows<D, T>(a, tid, C::kThreads);
+
+    // ---- where this CTA's part begins: a sum over the requests, each thread over a run of them
+    const int per = (a.batch + C::kThreads - 1) / C::kThreads, r_lo = min(tid * per, a.batch), r_hi = min(r_lo + per, a.batch);
+    auto units = [&](int r) {
+        const Request q = request_of<kRows, C::kTokens>(a, r);
+        return (long long)q.row_tiles * a.c.kv_heads * (q.pieces + kTreeJobCost);
+    };
+    long long mine = 0;
+    for (int r = r_lo; r < r_hi; ++r) mine += units(r);
+    long long upto = mine;
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+    }
+    if (lane == 31) sm.scan[warp] = upto;
+    __syncthreads();
+    long long total = 0;
+    for (int w = 0; w < C::kThreads / 32; ++w) {
+        if (w < warp) upto += sm.scan[w];
+        total += sm.scan[w];
+    }
+    const long long active = min((long long)gridDim.x, total);
+    if (blockIdx.x >= active) return;            // (the whole CTA)
+    const long long size = total / active, over = total - size * active;
+    auto cut = [&](long long i) { return i * size + min(i, over); };
+    const long long u = cut(blockIdx.x), u_end = cut(blockIdx.x + 1);
+    if (u >= upto - mine && u < upto) {
+        long long before = upto - mine;
+        for (int r = r_lo; r < r_hi; ++r) {
+            const long long n = units(r);
+            if (u < before + n) { sm.request = r; sm.before = before; break; }
+            before += n;
+        }
+    }
+    if (tid == 0) {
+        for (int i = 0; i < C::kStages; ++i) {
+            barrier_init(sm.full[i], C::kConverters);
+            barrier_init(sm.free[i], 1);
+        }
+        barrier_init(sm.q_full, C::kConverters);
+        barrier_init(sm.q_free, 1);
+        barrier_init(sm.drained, 1);
+        for (int i = 0; i < C::kPlaces; ++i) {
+            barrier_init(sm.s_full[i], 1);
+            barrier_init(sm.p_full[i], 4);
+            barrier_init(sm.pv_done[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) barrier_init(sm.ended[i], 1);
+        sm.failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    constexpr int kIssuer = C::kThreads / 32 - 1;
+    if (warp == kIssuer) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(&sm.columns)), "n"(C::kColumns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    unit_before_sync();
+    __syncthreads();
+    unit_after_sync();
+    Walk<D> walk;
+    walk.u = u;
+    walk.u_end = u_end;
+    walk.before = sm.before;
+    walk.r = sm.request;
+    walk.rq = request_of<kRows, C::kTokens>(a, walk.r);
+    if (lane == 0) sm.walk[warp] = walk;
+    __syncwarp();
+    if (warp < C::kSoft / 32) {
+        if constexpr (C::kSplit) take_registers<112>();
+        softmax_role<D, FMT, T>(a, sm, sm.walk[warp], size, over, tid);
+    } else if (warp < kIssuer) {
+        if constexpr (C::kSplit) leave_registers<80>();
+        convert_role<D, FMT, T>(a, sm, tiles, sm.walk[warp], tid - C::kSoft);
+    } else {
+        if (lane == 0) product_role<D>(a, sm, tiles, walk);
+        __syncwarp();
+    }
+    unit_before_sync();
+    __syncthreads();
+    unit_after_sync();
+    if (warp == kIssuer) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sm.columns), "n"(C::kColumns) : "memory");
+}
+
+// CTAs of a launch, and what their partial results take: two parts each
+constexpr size_t kTreeCounterBytes = (kMaxSms * sizeof(unsigned) + 255) / 256 * 256, kTreePartRows = (size_t)kMaxSms * 2 * kRows, kTreeLseBytes = kTreePartRows * sizeof(float);
+
+template <int D, int FMT, typename T> cudaError_t run_tree(const Args &a, cudaStream_t s)
+{
+    const size_t smem = 1024 + Tree<D>::kStages * Tree<D>::kStageBytes + sizeof(TreeShared<D>);
+    static std::atomic<bool> opted[fb::kMaxDevices];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= fb::kMaxDevices) return cudaErrorInvalidDevice;
+    if (!opted[dev].load(std::memory_order_relaxed)) {
+        e = cudaFuncSetAttribute(tree_attend_kernel<D, FMT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+        opted[dev].store(true, std::memory_order_relaxed);
+    }
+    const int sms = num_sms();
+    if (sms == 0) return cudaErrorInvalidDevice;
+    return launch(tree_attend_kernel<D, FMT, T>, dim3((unsigned)(sms < kMaxSms ? sms : kMaxSms)), Tree<D>::kThreads, smem, s, a);
+}
+
+template <int D> cudaError_t run_tree_of(const Args &a, bool bf16, cudaStream_t s)
+{
+    if (bf16) return a.c.format == FLUXBIN_CACHE_INT8 ? run_tree<D, FLUXBIN_CACHE_INT8, __nv_bfloat16>(a, s) : run_tree<D, FLUXBIN_CACHE_E4M3, __nv_bfloat16>(a, s);
+    return a.c.format == FLUXBIN_CACHE_INT8 ? run_tree<D, FLUXBIN_CACHE_INT8, __half>(a, s) : run_tree<D, FLUXBIN_CACHE_E4M3, __half>(a, s);
+}
+
+} // namespace
+
+// by head dimension, in files of their own
+namespace fbd {
+cudaError_t launch_tree_64(const AttendArgs &a, bool bf16, cudaStream_t s);
+cudaError_t launch_tree_128(const AttendArgs &a, bool bf16, cudaStream_t s);
+cudaError_t launch_tree_256(const AttendArgs &a, bool bf16, cudaStream_t s);
+} // namespace fbd
+
+#endif
