@@ -9,7 +9,9 @@
 //   V      exact in bf16 (int8 as parts 1 / 64)
 //   P      times its token's value scale: two bf16 numbers, written where S was, which lose 2^-16 of it and flush nothing
 //          short of fp32's range (see the kernel for few rows); so the second product is made twice
-// The cache's bytes come in by 16 a thread, a few tiles ahead in registers, and are converted into swizzled tiles in shared memory.
+// The cache's bytes come in by asynchronous copies, 16 a thread, into places of shared memory that only this thread reads again, a few
+// tiles ahead; the same thread converts them into swizzled tiles.  (A tile or two in registers instead: 174 us against 120 with 128
+// rows on 16 requests of 8190 tokens, and a warp that waits for the older one's bytes waits for the younger one's too.)
 //
 // Warps: four or eight for the softmax, eight that load and convert, one that issues the products.  At head dimension 64 and 128
 // the softmax is two groups of four warps that take the tiles in turn, each with accumulators of its own; what they have at the end
@@ -34,20 +36,22 @@ constexpr unsigned long long kWaitLimit = 2000000000ull;         // ns
 template <int D> struct Tree {
     static constexpr int kTokens = D == 256 ? 32 : 64;           // of a tile
     static constexpr int kGroups = D == 256 ? 1 : 2;             // of four softmax warps
-    static constexpr int kStages = D == 64 ? 8 : 6;              // tiles in shared memory
-    static constexpr int kAhead = D == 64 ? 4 : 2;               // tiles in a converter's registers
+    static constexpr int kStages = D == 64 ? 6 : 4;              // tiles in shared memory
+    static constexpr int kRing = D == 64 ? 6 : 4;                // tiles on their way there
     static constexpr int kConverters = 8;                        // warps
     static constexpr int kSoft = 128 * kGroups, kThreads = kSoft + kConverters * 32 + 32;
     static constexpr int kSlab = kTokens * 128;                  // 64 elements of every token
-    static constexpr int kSide = D / 64 * kSlab, kStageBytes = 2 * kSide;
+    static constexpr int kSide = D / 64 * kSlab, kStageBytes = 2 * kSide, kRingBytes = 2 * kTokens * D;
     // columns of the unit's memory: the sums, the queries, three places for scores and then probabilities
     static constexpr int kO = 0, kQ = kGroups * D, kS = kQ + D / 2, kPlaces = 3, kColumns = 512;
     static_assert(kS + kPlaces * kTokens <= kColumns, "the unit's memory");
-    // With 17 warps 96 registers a thread are there, 52224 in all: 112 for the softmax, 80 for the converters
+    // With 17 warps 96 registers a thread are there, 52224 in all: 120 for the softmax, 72 for the converters
     static constexpr bool kSplit = kGroups == 2;
 };
 
-struct Meta { float ks[4], vs[4]; int none; };   // of a tile's groups of 16 tokens: scales, which of them are in no block
+// What the softmax wants to know about a tile: key scales of its groups of 16 tokens, value scales as factors of the probabilities
+// (over `vref`, the reference that the sums are in), which groups are in no block and whether rows may differ in what they see
+struct __align__(16) Meta { float ks[4], f[4], vref; int none, edge; };
 
 // ---- barriers, fences, the matrix unit -------------------------------------------------------------------
 
@@ -58,6 +62,12 @@ __device__ __forceinline__ bool try_wait(uint32_t b, unsigned parity)
 {
     unsigned ok;
     asm volatile("{ .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n }" : "=r"(ok) : "r"(b), "r"(parity) : "memory");
+    return ok;
+}
+__device__ __forceinline__ bool is_through(unsigned long long &barrier, unsigned parity)
+{
+    unsigned ok;
+    asm volatile("{ .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n }" : "=r"(ok) : "r"(shared_address(&barrier)), "r"(parity) : "memory");
     return ok;
 }
 __device__ __forceinline__ unsigned long long now_ns()
@@ -99,6 +109,13 @@ __device__ __forceinline__ void unit_commit(unsigned long long &b)
 __device__ __forceinline__ void unit_mma(uint32_t c, uint32_t a, uint64_t b, uint32_t kind, bool add)
 {
     asm volatile("{ .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n }" ::"r"(c), "r"(a), "l"(b), "r"(kind), "r"((int)add) : "memory");
+}
+// one lane of a warp, always the same
+__device__ __forceinline__ bool elected()
+{
+    unsigned one;
+    asm volatile("{ .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n }" : "=r"(one));
+    return one;
 }
 template <int REGISTERS> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGISTERS)); }
 template <int REGISTERS> __device__ __forceinline__ void leave_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGISTERS)); }
@@ -201,7 +218,8 @@ template <int D> struct TreeShared {
     Meta meta[kMetaRing];
     unsigned long long full[Tree<D>::kStages], free[Tree<D>::kStages];
     unsigned long long q_full, q_free, s_full[3], p_full[3], pv_done[3], ended[2], drained;
-    long long place[Tree<D>::kConverters][2][32];                // of each converting warp: where 16 tokens lie, -1 for no block
+    long long place[Tree<D>::kConverters][2][32];                // of each converting warp: where 16 tokens lie
+    uint32_t none[Tree<D>::kConverters][2];                      // which of them are in no block (and read the cache's first one instead)
     long long scan[32], before;
     int request, last, failed;
     uint32_t columns;
@@ -226,12 +244,12 @@ __device__ __forceinline__ unsigned long long seen_bits(const Args &a, const Req
 
 // ---- the converters --------------------------------------------------------------------------------------
 
-template <int FMT> __device__ __forceinline__ void key_chunks(const uint4 &x, uint4 &lo, uint4 &hi)
+template <int FMT> __device__ __forceinline__ uint4 key_chunk(uint32_t x, uint32_t y)
 {
-    to_half4<FMT>(x.x, lo.x, lo.y);
-    to_half4<FMT>(x.y, lo.z, lo.w);
-    to_half4<FMT>(x.z, hi.x, hi.y);
-    to_half4<FMT>(x.w, hi.z, hi.w);
+    uint4 v;
+    to_half4<FMT>(x, v.x, v.y);
+    to_half4<FMT>(y, v.z, v.w);
+    return v;
 }
 template <int FMT> __device__ __forceinline__ void to_bfloat4(uint32_t x, uint32_t &lo, uint32_t &hi);
 // (as to_bfloat2x4, of four elements of one token)
@@ -251,12 +269,12 @@ template <> __device__ __forceinline__ void to_bfloat4<FLUXBIN_CACHE_E4M3>(uint3
     lo = bfloat2_of_half2(*reinterpret_cast<const __half2 *>(&h[0]));
     hi = bfloat2_of_half2(*reinterpret_cast<const __half2 *>(&h[1]));
 }
-template <int FMT> __device__ __forceinline__ void value_chunks(const uint4 &x, uint4 &lo, uint4 &hi)
+template <int FMT> __device__ __forceinline__ uint4 value_chunk(uint32_t x, uint32_t y)
 {
-    to_bfloat4<FMT>(x.x, lo.x, lo.y);
-    to_bfloat4<FMT>(x.y, lo.z, lo.w);
-    to_bfloat4<FMT>(x.z, hi.x, hi.y);
-    to_bfloat4<FMT>(x.w, hi.z, hi.w);
+    uint4 v;
+    to_bfloat4<FMT>(x, v.x, v.y);
+    to_bfloat4<FMT>(y, v.z, v.w);
+    return v;
 }
 __device__ __forceinline__ void put16(uint32_t to, const uint4 &v) { asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory"); }
 
@@ -264,11 +282,15 @@ template <int D, int FMT, typename T>
 __device__ __forceinline__ void convert_role(const Args &a, TreeShared<D> &sm, uint32_t stages, Walk<D> &walk, int tid)
 {
     using C = Tree<D>;
-    constexpr int PIECES = D / 16, PASS = C::kConverters * 32 / PIECES, N = C::kTokens / PASS, AHEAD = C::kAhead, GROUPS = C::kTokens / 16, BATCH = 32 / GROUPS;
-    static_assert(PASS % 16 == 0 && AHEAD + C::kStages + BATCH + 1 <= kMetaRing, "places and scales ahead");
+    constexpr int PIECES = D / 16, THREADS = C::kConverters * 32, PASS = THREADS / PIECES, N = C::kTokens / PASS, GROUPS = C::kTokens / 16, BATCH = 32 / GROUPS, RING = C::kRing;
+    static_assert(PASS % 16 == 0 && C::kStages + RING + BATCH + 1 <= kMetaRing && RING <= BATCH, "places and scales ahead");
     const int lane = tid & 31, warp = tid >> 5, bs = a.c.block_tokens, H = a.c.kv_heads, G = a.q_heads / H;
-    const int piece = tid % PIECES, sub = tid / PIECES;          // its 16 elements of tokens sub, sub + PASS ...
-    const uint32_t slab = piece / 4 * C::kSlab, odd = piece / 4 & 1;             // (odd slabs write their chunks in the other order: all banks)
+    // a thread's 16 elements of tokens sub, sub + PASS ...; eight neighbouring lanes hold four pieces of two neighbouring tokens: their
+    // chunks go to all banks
+    const int piece = lane % 4 + lane / (128 / PIECES) * 4, sub = warp * (32 / PIECES) + lane / 4 % (32 / PIECES);
+    const uint32_t to0 = piece / 4 * C::kSlab + sub * 128 + (((uint32_t)(piece % 4 * 2) ^ (sub & 7)) << 4);
+    const uint32_t ring = stages + C::kStages * C::kStageBytes + tid * 16;
+    unsigned stage = 0, stage_phase = 1;         // (the first time round a stage is free)
     bool ok = true;
     unsigned it = 0, jobs = 0;
     const Job &j = walk.j;
@@ -283,7 +305,7 @@ __device__ __forceinline__ void convert_role(const Args &a, TreeShared<D> &sm, u
         if (tid == 0) sm.any_nan[parity] = 0;
         sync_some<1, C::kConverters * 32>();
 
-        // ---- places of the tokens, 16 at a time: 32 of them are looked up together, well ahead, and kept in shared memory
+        // ---- places of the tokens, 16 at a time: 32 of them (a batch) are looked up together, well ahead, and kept in shared memory
         const int tok0 = j.p0 * C::kTokens, base = rq.length - rq.count;
         auto block_of = [&](int group) {
             const int tok = tok0 + group * 16;
@@ -303,12 +325,16 @@ __device__ __forceinline__ void convert_role(const Args &a, TreeShared<D> &sm, u
             }
             return x;
         };
+        float vref = 0.f;                        // (warp 0)
         auto keep_places = [&](const Place &x, int batch) {
-            sm.place[warp][batch & 1][lane] = x.at;
+            const unsigned none = __ballot_sync(0xffffffffu, x.at < 0);
+            sm.place[warp][batch & 1][lane] = max(x.at, 0ll);
+            if (lane == 0) sm.none[warp][batch & 1] = none;
             if (warp == 0) {
+                const int tok = tok0 + (batch * 32 + lane) * 16, mine = lane / GROUPS;
+                const int none_here = (int)(none >> (mine * GROUPS) & ((1u << GROUPS) - 1)), edge = tok0 + (batch * BATCH + mine + 1) * C::kTokens > base || none_here;
                 float vs = x.vs;
-                const int tok = tok0 + (batch * 32 + lane) * 16;
-                if (x.at >= 0 && !(vs < INFINITY) && tok + 16 > base) {
+                if (x.at >= 0 && !(vs < INFINITY) && edge) {
                     // a scale that is no number, of tokens that not all rows see: 0, and noted for those that do
                     for (int row = 0; row < j.rows; ++row)
                         if (seen_bits(a, rq, j.row0 + row, tok) & 0xffff) {
@@ -317,11 +343,23 @@ __device__ __forceinline__ void convert_role(const Args &a, TreeShared<D> &sm, u
                         }
                     vs = 0.f;
                 }
-                Meta &m = sm.meta[(it + batch * BATCH + lane / GROUPS) % kMetaRing];
+                // the reference is raised where the largest scale of a tile passes it by more than the sums' range is good for
+                float most = vs < INFINITY ? vs : 0.f, own = 0.f;
+#pragma unroll
+                for (int o = GROUPS / 2; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+                for (int t = 0; t < BATCH; ++t) {
+                    const float m = __shfl_sync(0xffffffffu, most, t * GROUPS);
+                    if (m >= 7.888609052210118e-31f && (vref == 0.f || m > vref * kValueLag)) vref = m;
+                    if (t == mine) own = vref;
+                }
+                Meta &m = sm.meta[(it + batch * BATCH + mine) % kMetaRing];
                 m.ks[lane % GROUPS] = x.ks;
-                m.vs[lane % GROUPS] = vs;
-                const unsigned none = __ballot_sync(0xffffffffu, x.at < 0);
-                if (lane % GROUPS == 0) m.none = (int)(none >> lane & ((1u << GROUPS) - 1));
+                m.f[lane % GROUPS] = vs * (own == 0.f ? 0.f : kPart<FMT> / own);
+                if (lane % GROUPS == 0) {
+                    m.vref = own;
+                    m.none = none_here;
+                    m.edge = edge;
+                }
             }
             __syncwarp();
         };
@@ -329,25 +367,29 @@ __device__ __forceinline__ void convert_role(const Args &a, TreeShared<D> &sm, u
         int id = -1;
         Place ahead = {-1, 0.f, 0.f};
         const long long mine = (long long)j.h * a.c.head_stride + sub % 16 * a.c.token_stride + piece * 16;
-        uint4 kr[AHEAD][N], vr[AHEAD][N];
-        auto load = [&](int tile, uint4 (&k)[N], uint4 (&v)[N]) {                // tiles in order
-            const int slot = tile % BATCH, batch = tile / BATCH;
-            if (slot == 0) id = block_of((batch + 1) * 32 + lane);
-            if (slot == BATCH / 2) ahead = place_of(id, (batch + 1) * 32 + lane);
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const long long at = sm.place[warp][batch & 1][slot * GROUPS + (sub + i * PASS) / 16];
-                k[i] = v[i] = make_uint4(0, 0, 0, 0);
-                if (at >= 0) {
-                    k[i] = __ldcs(reinterpret_cast<const uint4 *>((const unsigned char *)a.c.d_k + (at + mine)));
-                    v[i] = __ldcs(reinterpret_cast<const uint4 *>((const unsigned char *)a.c.d_v + (at + mine)));
+        const unsigned char *k_mine = (const unsigned char *)a.c.d_k + mine, *v_mine = (const unsigned char *)a.c.d_v + mine;
+        uint32_t ring_in = ring, ring_out = ring;
+        auto load = [&](int t) {                 // in order
+            if (t < tiles) {
+                const int slot = t % BATCH, batch = t / BATCH;
+                if (slot % (BATCH / 2) == 0) {
+                    if (slot == 0) id = block_of((batch + 1) * 32 + lane);
+                    else ahead = place_of(id, (batch + 1) * 32 + lane);
                 }
-            }
-            if (slot == BATCH - 1) keep_places(ahead, batch + 1);
-        };
+                const long long *place = &sm.place[warp][batch & 1][slot * GROUPS + sub / 16];
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-            if (i < tiles) load(i, kr[i], vr[i]);
+                for (int i = 0; i < N; ++i) {
+                    const long long at = place[i * PASS / 16];
+                    copy_ahead<16>(ring_in + i * (THREADS * 16), k_mine + at);
+                    copy_ahead<16>(ring_in + (N + i) * (THREADS * 16), v_mine + at);
+                }
+                if (slot == BATCH - 1) keep_places(ahead, batch + 1);
+            }
+            copies_commit();
+            ring_in = ring_in + C::kRingBytes == ring + RING * C::kRingBytes ? ring : ring_in + C::kRingBytes;
+        };
+#pragma unroll 1
+        for (int t = 0; t < RING - 1; ++t) load(t);
 
         // ---- the query rows, a lane for each: two warps share 32 rows, each writes half of their elements
         if (jobs >= 1) ok = ok && wait_together(sm.q_free, (jobs - 1) & 1, sm.failed);
@@ -393,27 +435,32 @@ __device__ __forceinline__ void convert_role(const Args &a, TreeShared<D> &sm, u
         }
 
         // ---- tile after tile
-        for (int t0 = 0; t0 < tiles; t0 += AHEAD)
+#pragma unroll 1
+        for (int t = 0; t < tiles; ++t) {
+            copies_wait<RING - 2>();
+            Words<4> k[N], v[N];
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) {
-                const int t = t0 + i;
-                if (t >= tiles) break;
-                const unsigned n = it + t, stage = n % C::kStages;
-                if (n >= C::kStages) ok = ok && wait_together(sm.free[stage], (n / C::kStages - 1) & 1, sm.failed);
-                const uint32_t k_to = stages + stage * C::kStageBytes + slab, v_to = k_to + C::kSide;
+            for (int i = 0; i < N; ++i) {
+                k[i] = take<4>(ring_out + i * (THREADS * 16));
+                v[i] = take<4>(ring_out + (N + i) * (THREADS * 16));
+            }
+            ring_out = ring_out + C::kRingBytes == ring + RING * C::kRingBytes ? ring : ring_out + C::kRingBytes;
+            load(t + RING - 1);
+            if constexpr (FMT == FLUXBIN_CACHE_E4M3) {
+                // values that must not meet the probability 0 of a row that does not see them (see the kernel for few rows)
                 const int tok = tok0 + t * C::kTokens;
-                if (FMT == FLUXBIN_CACHE_E4M3 && tok + C::kTokens > base) {
-                    // values that must not meet the probability 0 of a row that does not see them (see the kernel for few rows)
+                const uint32_t none = sm.none[warp][t / BATCH & 1] >> (t % BATCH * GROUPS) & ((1u << GROUPS) - 1);
+                if (tok + C::kTokens > base || none) {
 #pragma unroll
-                    for (int k = 0; k < N; ++k) {
-                        const int token = tok + sub + k * PASS;
-                        uint32_t w[4] = {vr[i][k].x, vr[i][k].y, vr[i][k].z, vr[i][k].w};
+                    for (int i = 0; i < N; ++i) {
+                        const int token = tok + sub + i * PASS;
+                        const bool out = (none >> ((sub + i * PASS) / 16) & 1) || token >= rq.length;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            uint32_t nan = nan_bytes(w[e]);
-                            if (token >= rq.length) w[e] = 0;
+                            uint32_t nan = nan_bytes(v[i].w[e]);
+                            if (out) v[i].w[e] = 0;
                             else if (nan) {
-                                w[e] &= ~(nan | (nan - (nan >> 7)));
+                                v[i].w[e] &= ~(nan | (nan - (nan >> 7)));
                                 for (; nan; nan &= nan - 1) {
                                     const int d = piece * 16 + e * 4 + (__ffs(nan) - 1) / 8;
                                     for (int row = 0; row < j.rows; ++row)
@@ -422,26 +469,24 @@ __device__ __forceinline__ void convert_role(const Args &a, TreeShared<D> &sm, u
                                 }
                             }
                         }
-                        vr[i][k] = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                 }
-#pragma unroll
-                for (int k = 0; k < N; ++k) {
-                    const int token = sub + k * PASS;
-                    const uint32_t c0 = (piece % 4 * 2 + odd) ^ (token & 7), c1 = (piece % 4 * 2 + (odd ^ 1)) ^ (token & 7);
-                    uint4 lo, hi;
-                    key_chunks<FMT>(kr[i][k], lo, hi);
-                    put16(k_to + token * 128 + (c0 << 4), odd ? hi : lo);
-                    put16(k_to + token * 128 + (c1 << 4), odd ? lo : hi);
-                    value_chunks<FMT>(vr[i][k], lo, hi);
-                    put16(v_to + token * 128 + (c0 << 4), odd ? hi : lo);
-                    put16(v_to + token * 128 + (c1 << 4), odd ? lo : hi);
-                }
-                if (t + AHEAD < tiles) load(t + AHEAD, kr[i], vr[i]);
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) arrive(sm.full[stage]);
             }
+            ok = ok && wait_together(sm.free[stage], stage_phase, sm.failed);
+            const uint32_t to = stages + stage * C::kStageBytes + to0;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                put16(to + i * (PASS * 128), key_chunk<FMT>(k[i].w[0], k[i].w[1]));
+                put16((to ^ 16) + i * (PASS * 128), key_chunk<FMT>(k[i].w[2], k[i].w[3]));
+                put16(to + C::kSide + i * (PASS * 128), value_chunk<FMT>(v[i].w[0], v[i].w[1]));
+                put16((to ^ 16) + C::kSide + i * (PASS * 128), value_chunk<FMT>(v[i].w[2], v[i].w[3]));
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) arrive(sm.full[stage]);
+            if (++stage == C::kStages) { stage = 0; stage_phase ^= 1; }
+        }
+        copies_wait<0>();
         it += tiles;
         ++jobs;
     }
@@ -449,58 +494,118 @@ __device__ __forceinline__ void convert_role(const Args &a, TreeShared<D> &sm, u
 
 // ---- the products ----------------------------------------------------------------------------------------
 
+// The stage, the place and the group of a tile, and how often stage and place have been gone through
+template <int D> struct Turn {
+    int stage = 0, place = 0, group = 0;
+    unsigned stage_phase = 0, place_phase = 0;
+    __device__ __forceinline__ void next()
+    {
+        if (++stage == Tree<D>::kStages) { stage = 0; stage_phase ^= 1; }
+        if (++place == Tree<D>::kPlaces) { place = 0; place_phase ^= 1; }
+        if (Tree<D>::kGroups == 2) group ^= 1;
+    }
+};
+
+// The whole warp goes along, so that what it works out is the same for all lanes and stays in the registers that the unit's
+// instructions take; one lane issues them.  The next tile's scores are asked for as soon as there is a place, a tile's values
+// multiplied as soon as its probabilities are there, whichever comes first.  (One after the other: 180 us against 150 with 128 rows
+// on 16 requests of 8190 tokens.)
 template <int D>
-__device__ __forceinline__ void product_role(const Args &a, TreeShared<D> &sm, uint32_t stages, Walk<D> walk)
+__device__ __forceinline__ void product_role(const Args &a, TreeShared<D> &sm, uint32_t stages, Walk<D> &walk, int lane)
 {
     using C = Tree<D>;
-    constexpr int LOOK = C::kPlaces - 1;         // tiles whose scores are asked for ahead
     constexpr uint32_t kScores = unit_kind(0, false, C::kTokens), kValues = unit_kind(1, true, D);
-    const uint32_t unit = sm.columns;
-    unsigned it = 0, jobs = 0;
-    const Job &j = walk.j;
-    auto run = [&]() -> bool {
-        while (walk.step(a)) {
-            if (j.tiles == 0) continue;
-            if (!wait_for(sm.q_full, jobs & 1, sm.failed)) return false;
-            for (int step = 0; step < j.tiles + LOOK; ++step) {
-                if (step < j.tiles) {
-                    const unsigned n = it + step, stage = n % C::kStages, place = n % C::kPlaces;
-                    if (!wait_for(sm.full[stage], n / C::kStages & 1, sm.failed)) return false;
-                    if (n >= C::kPlaces && !wait_for(sm.pv_done[place], (n / C::kPlaces - 1) & 1, sm.failed)) return false;
-                    unit_after_sync();
-                    const uint64_t keys = operand(stages + stage * C::kStageBytes, 16);
+    const uint32_t unit = __shfl_sync(0xffffffffu, sm.columns, 0);
+    const uint64_t keys0 = operand(stages, 16), values0 = operand(stages + C::kSide, C::kSlab);
+    bool ok = true;
+    Turn<D> scores, values;                      // of the tiles whose scores are asked for, whose values are multiplied
+    unsigned jobs = 0, asked = 0;
+    while (ok && walk.next(a, lane)) {
+        const int tiles = __shfl_sync(0xffffffffu, walk.j.tiles, 0);
+        if (tiles == 0) continue;
+        ok = wait_together(sm.q_full, jobs & 1, sm.failed);
+        unsigned long long idle = 0, began = 0;
+        for (int ts = 0, tv = 0; ok && tv < tiles;) {
+            const bool ask = ts < tiles && ts - tv < C::kPlaces && is_through(sm.full[scores.stage], scores.stage_phase) &&
+                             (asked < C::kPlaces || is_through(sm.pv_done[scores.place], scores.place_phase ^ 1));
+            if (__all_sync(0xffffffffu, ask)) {
+                unit_after_sync();
+                const uint64_t keys = keys0 + (scores.stage * C::kStageBytes >> 4);
+                const uint32_t to = unit + C::kS + scores.place * C::kTokens;
+                if (elected()) {
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
-                        unit_mma(unit + C::kS + place * C::kTokens, unit + C::kQ + k * 8, keys + ((k / 4 * C::kSlab + k % 4 * 32) >> 4), kScores, k > 0);
-                    unit_commit(sm.s_full[place]);
-                    if (step == j.tiles - 1) unit_commit(sm.q_free);
+                    for (int k = 0; k < D / 16; ++k) unit_mma(to, unit + C::kQ + k * 8, keys + ((k / 4 * C::kSlab + k % 4 * 32) >> 4), kScores, k > 0);
+                    unit_commit(sm.s_full[scores.place]);
+                    if (ts == tiles - 1) unit_commit(sm.q_free);
                 }
-                if (step >= LOOK) {
-                    const int t = step - LOOK;
-                    const unsigned n = it + t, stage = n % C::kStages, place = n % C::kPlaces;
-                    if (!wait_for(sm.p_full[place], n / C::kPlaces & 1, sm.failed)) return false;
-                    unit_after_sync();
-                    const uint64_t values = operand(stages + stage * C::kStageBytes + C::kSide, C::kSlab);
-                    const uint32_t o = unit + C::kO + n % C::kGroups * D, p = unit + C::kS + place * C::kTokens;
+                __syncwarp();
+                scores.next();
+                asked += asked < C::kPlaces;
+                ++ts;
+                idle = 0;
+            }
+            if (__all_sync(0xffffffffu, tv < ts && is_through(sm.p_full[values.place], values.place_phase))) {
+                unit_after_sync();
+                const uint64_t at = values0 + (values.stage * C::kStageBytes >> 4);
+                const uint32_t o = unit + C::kO + values.group * D, p = unit + C::kS + values.place * C::kTokens;
+                const bool add = tv >= C::kGroups;
+                if (elected()) {
 #pragma unroll
                     for (int half = 0; half < 2; ++half)
 #pragma unroll
-                        for (int k = 0; k < C::kTokens / 16; ++k)
-                            unit_mma(o, p + half * (C::kTokens / 2) + k * 8, values + (k * 2048 >> 4), kValues, t >= C::kGroups || half > 0 || k > 0);
-                    unit_commit(sm.pv_done[place]);
-                    unit_commit(sm.free[stage]);
+                        for (int k = 0; k < C::kTokens / 16; ++k) unit_mma(o, p + half * (C::kTokens / 2) + k * 8, at + (k * 2048 >> 4), kValues, add || half > 0 || k > 0);
+                    unit_commit(sm.pv_done[values.place]);
+                    unit_commit(sm.free[values.stage]);
                 }
+                __syncwarp();
+                values.next();
+                ++tv;
+                idle = 0;
+                continue;
             }
-            it += j.tiles;
-            ++jobs;
+            // (others want to issue; the limit of a wait is looked at now and then)
+            __nanosleep(20);
+            if ((++idle & 1023) == 0) {
+                const unsigned long long t = now_ns();
+                if (idle == 1024) began = t;
+                if (t - began > kWaitLimit) *(volatile int *)&sm.failed = 1;
+                ok = __all_sync(0xffffffffu, !*(volatile int *)&sm.failed);
+            }
         }
-        return true;
-    };
-    if (!run()) {                                // what is under way has to end before the unit's memory is given back
-        unit_commit(sm.drained);
-        int own = 0;
-        wait_for(sm.drained, 0, own);
+        ++jobs;
     }
+    if (!ok) {                                   // what is under way has to end before the unit's memory is given back
+        if (elected()) unit_commit(sm.drained);
+        int own = 0;
+        wait_together(sm.drained, 0, own);
+    }
+}
+
+// Two fp32 values at a time
+__device__ __forceinline__ unsigned long long two(float x, float y)
+{
+    unsigned long long v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
+    return v;
+}
+__device__ __forceinline__ void apart(unsigned long long v, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ unsigned long long fma_two(unsigned long long a, unsigned long long b, unsigned long long c)
+{
+    unsigned long long v;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+    return v;
+}
+__device__ __forceinline__ unsigned long long mul_two(unsigned long long a, unsigned long long b)
+{
+    unsigned long long v;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
+}
+__device__ __forceinline__ unsigned long long add_two(unsigned long long a, unsigned long long b)
+{
+    unsigned long long v;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
 }
 
 // ---- the softmax -----------------------------------------------------------------------------------------
@@ -514,6 +619,7 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
     const uint32_t unit = sm.columns + ((uint32_t)(warp % 4 * 32) << 16);
     const long long share = blockIdx.x;
     bool ok = true;
+    Turn<D> turn;
     unsigned it = 0, jobs = 0;
     const Job &j = walk.j;
     const Request &rq = walk.rq;
@@ -522,60 +628,100 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
         const unsigned parity = jobs & 1;
         const bool live = warp % 4 * 32 < j.rows;                // (the rows of a warp are all past the end, or not)
         const int base = rq.length - rq.count, my_row = min(row, j.rows - 1);
-        float ref = kNoRef, sum = 0.f, vref = 0.f, vref_inverse = 0.f, factor = 0.f;
+        float ref = kNoRef, sum = 0.f, vref = 0.f, factor = 0.f;
         const int t_first = (group - (int)it) & (GROUPS - 1);    // tiles go to the groups in turn, from job to job
-        for (int t = t_first; t < tiles; t += GROUPS) {
-            const unsigned n = it + t, place = n % C::kPlaces;
-            ok = ok && wait_together(sm.full[n % C::kStages], n / C::kStages & 1, sm.failed) && wait_together(sm.s_full[place], n / C::kPlaces & 1, sm.failed);
+        for (int t = 0; t < tiles; ++t, turn.next()) {
+            if (GROUPS == 2 && t % 2 != t_first) continue;
+            ok = ok && wait_together(sm.s_full[turn.place], turn.place_phase, sm.failed);
             if (!ok) break;
-            if (t == t_first) factor = sm.factor[parity][row];
             if (live) {
                 unit_after_sync();
-                const uint32_t at = unit + C::kS + place * N;
+                const uint32_t at = unit + C::kS + turn.place * N;
                 uint32_t s[N];
+                const float *x = reinterpret_cast<const float *>(s);
 #pragma unroll
                 for (int i = 0; i < N; i += 32) load_columns(at + i, reinterpret_cast<uint32_t (&)[32]>(s[i]));
-                const Meta &m = sm.meta[n % kMetaRing];
-                const int tok = (j.p0 + t) * N;
-                float c[N / 16], vf[N / 16], vmax = 0.f;
-#pragma unroll
-                for (int i = 0; i < N / 16; ++i) {
-                    c[i] = factor * m.ks[i];
-                    vf[i] = m.vs[i];
-                    if (vf[i] < INFINITY) vmax = fmaxf(vmax, vf[i]);
+                const Meta &m = sm.meta[(it + t) % kMetaRing];
+                const float4 ks = *reinterpret_cast<const float4 *>(m.ks), fs = *reinterpret_cast<const float4 *>(m.f), other = *reinterpret_cast<const float4 *>(&m.vref);
+                if (t == t_first) factor = sm.factor[parity][row];
+                const float c[4] = {factor * ks.x, factor * ks.y, factor * ks.z, factor * ks.w}, f[4] = {fs.x, fs.y, fs.z, fs.w};
+                const bool edge = __float_as_int(other.z), plain = !edge && fminf(fminf(c[0], c[1]), fminf(c[2], c[3])) >= 0.f;
+                float rescale = 1.f;
+                if (vref != other.x) {           // (the same for every row)
+                    rescale = vref / other.x;
+                    vref = other.x;
                 }
-                const bool edge = tok + N > base || m.none;
                 unsigned long long bits = ~0ull;
                 if (edge) {
-                    bits = seen_bits(a, rq, j.row0 + my_row, tok);
+                    bits = seen_bits(a, rq, j.row0 + my_row, (j.p0 + t) * N);
 #pragma unroll
                     for (int i = 0; i < N / 16; ++i)
-                        if (m.none >> i & 1) bits &= ~(0xffffull << (i * 16));
+                        if (__float_as_int(other.y) >> i & 1) bits &= ~(0xffffull << (i * 16));
                 }
-                // ---- the largest score against the lagging reference
                 loads_done();
+                // ---- the largest score against the lagging reference (scores times c, which is formed with the exponents)
                 float most = -INFINITY;
-                float *x = reinterpret_cast<float *>(s);
+                if (plain) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    x[i] *= c[i / 16];
-                    if (edge && !(bits >> i & 1)) x[i] = -INFINITY;
-                    most = fmaxf(most, x[i]);
+                    for (int i = 0; i < N / 16; ++i) {
+                        float top[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) top[k] = fmaxf(fmaxf(x[i * 16 + k], x[i * 16 + 4 + k]), fmaxf(x[i * 16 + 8 + k], x[i * 16 + 12 + k]));
+                        most = fmaxf(most, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c[i]);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+                        if (bits >> i & 1) most = fmaxf(most, x[i] * c[i / 16]);
                 }
-                float rescale = 1.f;
                 if (most > ref + 15.f) {
-                    const float now = most - 7.f;
-                    rescale = exp2_fast(ref - now);
+                    const float now = most - 7.f, less = exp2_fast(ref - now);
                     ref = now;
-                    sum *= rescale;
+                    sum *= less;
+                    rescale *= less;
                 }
-                if (vmax >= 7.888609052210118e-31f && (vref == 0.f || vmax > vref * kValueLag)) {        // (the same for every row)
-                    rescale *= vref / vmax;
-                    vref = vmax;
-                    vref_inverse = kPart<FMT> / vmax;
+                // ---- probabilities, 16 tokens at a time
+                const unsigned long long minus_ref = two(-ref, -ref), minus_one = two(-1.f, -1.f);
+                unsigned long long sums = two(sum, 0.f);
+#pragma unroll
+                for (int i = 0; i < N / 16; ++i) {
+                    const unsigned long long c2 = two(c[i], c[i]), f2 = two(f[i], f[i]);
+                    float q[16];
+#pragma unroll
+                    for (int k = 0; k < 16; k += 2) {
+                        apart(fma_two(two(x[i * 16 + k], x[i * 16 + k + 1]), c2, minus_ref), q[k], q[k + 1]);
+                        q[k] = exp2_fast(q[k]);
+                        q[k + 1] = exp2_fast(q[k + 1]);
+                    }
+                    if (edge) {
+#pragma unroll
+                        for (int k = 0; k < 16; ++k)
+                            if (!(bits >> (i * 16 + k) & 1)) q[k] = 0.f;
+                    }
+                    uint32_t upper[8], rest[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const unsigned long long pair = two(q[2 * k], q[2 * k + 1]);
+                        sums = add_two(sums, pair);
+                        const unsigned long long w = mul_two(pair, f2);
+                        float w0, w1, r0, r1;
+                        apart(w, w0, w1);
+                        const __nv_bfloat162 u = __floats2bfloat162_rn(w0, w1);
+                        upper[k] = *reinterpret_cast<const uint32_t *>(&u);
+                        apart(fma_two(two(__uint_as_float(upper[k] << 16), __uint_as_float(upper[k] & 0xffff0000u)), minus_one, w), r0, r1);
+                        const __nv_bfloat162 r = __floats2bfloat162_rn(r0, r1);
+                        rest[k] = *reinterpret_cast<const uint32_t *>(&r);
+                    }
+                    store_columns(at + i * 8, upper);
+                    store_columns(at + N / 2 + i * 8, rest);
+                }
+                {
+                    float s0, s1;
+                    apart(sums, s0, s1);
+                    sum = s0 + s1;
                 }
                 if (t >= GROUPS && __any_sync(0xffffffffu, rescale != 1.f)) {
-                    const unsigned before = n - GROUPS;          // the last tile that went to the same sums
+                    const unsigned before = it + t - GROUPS;     // the last tile that went to the same sums
                     ok = wait_together(sm.pv_done[before % C::kPlaces], before / C::kPlaces & 1, sm.failed);
                     unit_after_sync();
                     const uint32_t o = unit + C::kO + group * D;
@@ -589,25 +735,11 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
                         store_columns(o + i, v);
                     }
                 }
-                // ---- probabilities, 16 tokens at a time
-#pragma unroll
-                for (int i = 0; i < N / 16; ++i) {
-                    const float f = edge && !(vf[i] < INFINITY) ? 0.f : vf[i] * vref_inverse;
-                    uint32_t upper[8], rest[8];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const float p0 = exp2_fast(x[i * 16 + 2 * k] - ref), p1 = exp2_fast(x[i * 16 + 2 * k + 1] - ref);
-                        sum += p0 + p1;
-                        split_bfloat2(p0 * f, p1 * f, upper[k], rest[k]);
-                    }
-                    store_columns(at + i * 8, upper);
-                    store_columns(at + N / 2 + i * 8, rest);
-                }
                 stores_done();
                 unit_before_sync();
             }
             __syncwarp();
-            if (lane == 0) arrive(sm.p_full[place]);
+            if (lane == 0) arrive(sm.p_full[turn.place]);
         }
         // ---- the end of the job: sums of both groups
         sm.m[group][row] = ref;
@@ -688,34 +820,55 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
                 __threadfence();
                 const int parts = c1 - c0 + 1;
                 auto slot_of = [&](int c) { return (long long)(c0 + c) * 2 + (c == 0); };
-                for (int r = warp; r < j.rows; r += C::kSoft / 32) {
-                    float m = -INFINITY, l = 0.f;
-                    for (int c = lane; c < parts; c += 32) {
-                        const float x = __ldcg(a.partial_lse + slot_of(c) * kRows + r), m_now = fmaxf(m, x);
-                        l = l * (m == -INFINITY ? 0.f : exp2_fast(m - m_now)) + (x == -INFINITY ? 0.f : exp2_fast(x - m_now));
-                        m = m_now;
+                for (int r = tid; r < j.rows; r += C::kSoft) {
+                    float top = -INFINITY, l = 0.f;
+                    bool nan = false;
+#pragma unroll 8
+                    for (int c = 0; c < parts; ++c) {
+                        const float x = __ldcg(a.partial_lse + slot_of(c) * kRows + r);
+                        top = fmaxf(top, x);
+                        nan |= x != x;
                     }
-                    float top = m;
-                    for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-                    l *= m == -INFINITY ? (l == l ? 0.f : 1.f) : exp2_fast(m - top);
-                    for (int x = 16; x; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
-                    if (lane == 0) {
-                        sm.join_max[r] = top == -INFINITY ? 0.f : top;
-                        sm.join_inv[r] = l == 0.f ? 0.f : 1.f / l;
-                        sm.join_lse[r] = l == 0.f ? -INFINITY : top + log2f(l);
+#pragma unroll 8
+                    for (int c = 0; c < parts; ++c) {
+                        const float x = __ldcg(a.partial_lse + slot_of(c) * kRows + r);
+                        l += x == -INFINITY ? 0.f : exp2_fast(x - top);
                     }
+                    if (nan) l = NAN;
+                    sm.join_max[r] = top == -INFINITY ? 0.f : top;
+                    sm.join_inv[r] = l == 0.f ? 0.f : 1.f / l;
+                    sm.join_lse[r] = l == 0.f ? -INFINITY : top + log2f(l);
                 }
                 sync_some<2, C::kSoft>();
-                for (int i = tid; i < j.rows * (D / 4); i += C::kSoft) {
-                    const int r = i / (D / 4), d = i % (D / 4) * 4;
-                    float v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+                constexpr int kEach = 8;         // pieces of four elements of a thread, under way together
+                const int items = j.rows * (D / 4);
+                for (int first = tid; first < items; first += C::kSoft * kEach) {
+                    float v[kEach][4];
+#pragma unroll
+                    for (int k = 0; k < kEach; ++k) v[k][0] = v[k][1] = v[k][2] = v[k][3] = 0.f;
                     for (int c = 0; c < parts; ++c) {
-                        const float f = exp2_fast(__ldcg(a.partial_lse + slot_of(c) * kRows + r) - sm.join_max[r]) * sm.join_inv[r];
-                        const float4 y = __ldcg(reinterpret_cast<const float4 *>(a.partial + (slot_of(c) * kRows + r) * D + d));
-                        v[0] += f * y.x; v[1] += f * y.y; v[2] += f * y.z; v[3] += f * y.w;
+                        const float *lse = a.partial_lse + slot_of(c) * kRows;
+                        const float4 *o = reinterpret_cast<const float4 *>(a.partial + slot_of(c) * kRows * D);
+                        float4 y[kEach];
+                        float f[kEach];
+#pragma unroll
+                        for (int k = 0; k < kEach; ++k) {
+                            const int i = min(first + k * C::kSoft, items - 1);
+                            y[k] = __ldcg(o + i);
+                            f[k] = __ldcg(lse + i / (D / 4));
+                        }
+#pragma unroll
+                        for (int k = 0; k < kEach; ++k) {
+                            const int r = min(first + k * C::kSoft, items - 1) / (D / 4);
+                            f[k] = exp2_fast(f[k] - sm.join_max[r]) * sm.join_inv[r];
+                            v[k][0] += f[k] * y[k].x; v[k][1] += f[k] * y[k].y; v[k][2] += f[k] * y[k].z; v[k][3] += f[k] * y[k].w;
+                        }
                     }
-                    write_out(r, d, v, sm.join_lse[r]);
+#pragma unroll
+                    for (int k = 0; k < kEach; ++k) {
+                        const int i = first + k * C::kSoft;
+                        if (i < items) write_out(i / (D / 4), i % (D / 4) * 4, v[k], sm.join_lse[i / (D / 4)]);
+                    }
                 }
                 if (tid == 0) a.arrived[c0] = 0;
             }
@@ -735,7 +888,7 @@ __global__ void __launch_bounds__(Tree<D>::kThreads, 1) tree_attend_kernel(const
     using C = Tree<D>;
     extern __shared__ unsigned char smem_tree[];
     const uint32_t tiles = (shared_address(smem_tree) + 1023) & ~1023u;
-    TreeShared<D> &sm = *reinterpret_cast<TreeShared<D> *>(smem_tree + (tiles - shared_address(smem_tree)) + C::kStages * C::kStageBytes);
+    TreeShared<D> &sm = *reinterpret_cast<TreeShared<D> *>(smem_tree + (tiles - shared_address(smem_tree)) + C::kStages * C::kStageBytes + C::kRing * C::kRingBytes);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
     let_successor_start();
@@ -810,14 +963,13 @@ __global__ void __launch_bounds__(Tree<D>::kThreads, 1) tree_attend_kernel(const
     if (lane == 0) sm.walk[warp] = walk;
     __syncwarp();
     if (warp < C::kSoft / 32) {
-        if constexpr (C::kSplit) take_registers<112>();
+        if constexpr (C::kSplit) take_registers<120>();
         softmax_role<D, FMT, T>(a, sm, sm.walk[warp], size, over, tid);
     } else if (warp < kIssuer) {
-        if constexpr (C::kSplit) leave_registers<80>();
+        if constexpr (C::kSplit) leave_registers<72>();
         convert_role<D, FMT, T>(a, sm, tiles, sm.walk[warp], tid - C::kSoft);
     } else {
-        if (lane == 0) product_role<D>(a, sm, tiles, walk);
-        __syncwarp();
+        product_role<D>(a, sm, tiles, sm.walk[warp], lane);
     }
     unit_before_sync();
     __syncthreads();
@@ -830,7 +982,7 @@ constexpr size_t kTreeCounterBytes = (kMaxSms * sizeof(unsigned) + 255) / 256 * 
 
 template <int D, int FMT, typename T> cudaError_t run_tree(const Args &a, cudaStream_t s)
 {
-    const size_t smem = 1024 + Tree<D>::kStages * Tree<D>::kStageBytes + sizeof(TreeShared<D>);
+    const size_t smem = 1024 + Tree<D>::kStages * Tree<D>::kStageBytes + Tree<D>::kRing * Tree<D>::kRingBytes + sizeof(TreeShared<D>);
     static std::atomic<bool> opted[fb::kMaxDevices];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
