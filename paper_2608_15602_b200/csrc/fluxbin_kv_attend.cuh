@@ -861,13 +861,11 @@ template <int D, int FMT, typename T, bool TREE> cudaError_t run_rows(const Args
     // 8190 tokens: 24 rows 109 us against 117 in one tile, 32 112 against 119, 40 169 against 122, 64 213 in both, 72 256 against
     // 215 in two, 112 337 against 324 in three; at 64 tiles of 40 never won)
     const long long rows = (long long)(a.q_heads / a.c.kv_heads) * ((a.tokens + a.batch - 1) / a.batch);
-    if constexpr (!TREE && D == 128) {
+    if constexpr (!TREE && D == 128) {           // (many rows of trees are another kernel's)
         if ((rows + 39) / 40 * 11 < (rows + 15) / 16 * 5) return run<D, FMT, 5, T, TREE>(a, s);
     }
     // (9 to 16 rows in one tile of 16 instead of two of 8: 68 against 80 us at 128, 92 against 138 at 256, 41 against 48 at 64)
-    if constexpr (!TREE) {                       // (many rows of trees are another kernel's)
-        if (rows > 8) return run<D, FMT, 2, T, TREE>(a, s);
-    }
+    if (rows > 8) return run<D, FMT, 2, T, TREE>(a, s);
     return run<D, FMT, 1, T, TREE>(a, s);
 }
 template <int D, typename T, bool TREE> cudaError_t run_format(const Args &a, cudaStream_t s)

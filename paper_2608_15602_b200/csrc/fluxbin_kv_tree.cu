@@ -3,8 +3,10 @@
 
 namespace {
 
-// rows that share a key head in an average request: the kernel for few rows has tiles of 8
-constexpr long long kFewRows = 8;
+// Rows that share a key head in an average request up to which the kernel for few rows is ahead: 16 requests of 8190 tokens, this kernel
+// against the other, 16 rows 85 us and 118 at head dimension 128, 54 and 77 at 256, 49 and 90 at 64; 24 rows 160 and 118 at 128;
+// 32 rows 87 and 82 at 256, 98 and 90 at 64.
+constexpr long long kFewRows = 16;
 
 // A workspace of both kernels: the counters of the one for few rows, the partial results of either (of one call at a time), the
 // counters of this one -- behind all that the other writes, since each finds its own zeroed.

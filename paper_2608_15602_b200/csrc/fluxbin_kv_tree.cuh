@@ -13,7 +13,7 @@
 // tiles ahead; the same thread converts them into swizzled tiles.  (A tile or two in registers instead: 174 us against 120 with 128
 // rows on 16 requests of 8190 tokens, and a warp that waits for the older one's bytes waits for the younger one's too.)
 //
-// Warps: four or eight for the softmax, eight that load and convert, one that issues the products.  At head dimension 64 and 128
+// Warps: four or eight for the softmax, eight that load and convert, two that issue the products.  At head dimension 64 and 128
 // the softmax is two groups of four warps that take the tiles in turn, each with accumulators of its own; what they have at the end
 // of a job is put together as parts of the line are (at 256 the accumulators of one group fill half of the unit's memory: one
 // group).  Scores and probabilities go through three places in turn, so that the scores of the next two tiles are under way
@@ -28,7 +28,9 @@
 namespace {
 
 constexpr int kRows = 128;                   // of a tile: the lanes of the matrix unit's memory
-constexpr int kTreeJobCost = 4;              // units that it costs to begin a job
+// Units that it costs to begin a job.  Measured 2, 4, 8, 14: 132, 132, 131, 130 us with 128 rows on 16 requests of 8190 tokens, 55, 47, 48, 55 on 64
+// requests of 100, 241, 240, 237, 232 with 256 rows on one of 131071.
+constexpr int kTreeJobCost = 8;
 constexpr int kMetaRing = 32;                // tiles whose scales are kept
 constexpr float kValueLag = 1048576.f;       // 2^20: value scales may pass the largest one met so far by this much before O is rescaled
 constexpr unsigned long long kWaitLimit = 2000000000ull;         // ns
@@ -39,13 +41,13 @@ template <int D> struct Tree {
     static constexpr int kStages = D == 64 ? 6 : 4;              // tiles in shared memory
     static constexpr int kRing = D == 64 ? 6 : 4;                // tiles on their way there
     static constexpr int kConverters = 8;                        // warps
-    static constexpr int kSoft = 128 * kGroups, kThreads = kSoft + kConverters * 32 + 32;
+    static constexpr int kSoft = 128 * kGroups, kThreads = kSoft + kConverters * 32 + 64;
     static constexpr int kSlab = kTokens * 128;                  // 64 elements of every token
     static constexpr int kSide = D / 64 * kSlab, kStageBytes = 2 * kSide, kRingBytes = 2 * kTokens * D;
     // columns of the unit's memory: the sums, the queries, three places for scores and then probabilities
     static constexpr int kO = 0, kQ = kGroups * D, kS = kQ + D / 2, kPlaces = 3, kColumns = 512;
     static_assert(kS + kPlaces * kTokens <= kColumns, "the unit's memory");
-    // With 17 warps 96 registers a thread are there, 52224 in all: 120 for the softmax, 72 for the converters
+    // With 18 warps 96 registers a thread are there, 55296 in all: 120 for the softmax, 72 for the converters
     static constexpr bool kSplit = kGroups == 2;
 };
 
@@ -62,12 +64,6 @@ __device__ __forceinline__ bool try_wait(uint32_t b, unsigned parity)
 {
     unsigned ok;
     asm volatile("{ .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n }" : "=r"(ok) : "r"(b), "r"(parity) : "memory");
-    return ok;
-}
-__device__ __forceinline__ bool is_through(unsigned long long &barrier, unsigned parity)
-{
-    unsigned ok;
-    asm volatile("{ .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n }" : "=r"(ok) : "r"(shared_address(&barrier)), "r"(parity) : "memory");
     return ok;
 }
 __device__ __forceinline__ unsigned long long now_ns()
@@ -210,14 +206,14 @@ template <int D> struct Walk {
 };
 
 template <int D> struct TreeShared {
-    float factor[2][kRows];                      // by the parity of the job, as all that is
-    uint32_t nan[2][kRows][D / 32];
+    uint32_t nan[2][kRows][D / 32];              // by the parity of the job
     int any_nan[2];
     float m[2][kRows], l[2][kRows], vref[2];     // of the two softmax groups
+    float largest[2][kRows];                     // of the parts of the query rows
     float join_max[kRows], join_inv[kRows], join_lse[kRows];
     Meta meta[kMetaRing];
     unsigned long long full[Tree<D>::kStages], free[Tree<D>::kStages];
-    unsigned long long q_full, q_free, s_full[3], p_full[3], pv_done[3], ended[2], drained;
+    unsigned long long q_full, s_full[3], p_full[3], pv_done[3], ended[2], drained[2];
     long long place[Tree<D>::kConverters][2][32];                // of each converting warp: where 16 tokens lie
     uint32_t none[Tree<D>::kConverters][2];                      // which of them are in no block (and read the cache's first one instead)
     long long scan[32], before;
@@ -225,6 +221,15 @@ template <int D> struct TreeShared {
     uint32_t columns;
     Walk<D> walk[Tree<D>::kThreads / 32];        // of each warp: in registers only while it is looked at
 };
+
+// bf16 elements times 2^-e as fp16 (half2_of_bf16), by two products, since 2^-e may pass fp32's range
+struct Power { float first, second; };
+__device__ __forceinline__ Power power_of(int e) { return {__int_as_float((127 - (e >> 1)) << 23), __int_as_float((127 - (e - (e >> 1))) << 23)}; }
+__device__ __forceinline__ uint32_t half2_scaled(uint32_t w, const Power &p)
+{
+    const __half2 h = __floats2half2_rn(__uint_as_float(w << 16) * p.first * p.second, __uint_as_float(w & 0xffff0000u) * p.first * p.second);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
 
 // which of the tokens tok .. tok + 63 a row sees: those before the new ones, of those what its mask says, none past the length
 __device__ __forceinline__ unsigned long long seen_bits(const Args &a, const Request &rq, int row, int tok)
@@ -289,6 +294,7 @@ __device__ __forceinline__ void convert_role(const Args &a, TreeShared<D> &sm, u
     // chunks go to all banks
     const int piece = lane % 4 + lane / (128 / PIECES) * 4, sub = warp * (32 / PIECES) + lane / 4 % (32 / PIECES);
     const uint32_t to0 = piece / 4 * C::kSlab + sub * 128 + (((uint32_t)(piece % 4 * 2) ^ (sub & 7)) << 4);
+    const int shift = bs & (bs - 1) ? -1 : 31 - __clz(bs);       // (blocks are mostly of a power of two tokens)
     const uint32_t ring = stages + C::kStages * C::kStageBytes + tid * 16;
     unsigned stage = 0, stage_phase = 1;         // (the first time round a stage is free)
     bool ok = true;
@@ -310,14 +316,15 @@ __device__ __forceinline__ void convert_role(const Args &a, TreeShared<D> &sm, u
         auto block_of = [&](int group) {
             const int tok = tok0 + group * 16;
             if (group >= tiles * GROUPS || tok >= rq.length) return -1;
-            const int id = a.table[j.r * a.table_stride + tok / bs];
+            const int id = a.table[j.r * a.table_stride + (shift >= 0 ? tok >> shift : tok / bs)];
             return id >= 0 && id < a.c.num_blocks ? id : -1;
         };
         struct Place { long long at; float ks, vs; };
         auto place_of = [&](int id, int group) {
             Place x = {-1, 0.f, 0.f};
             if (id >= 0) {
-                x.at = id * a.c.block_stride + (tok0 + group * 16) % bs * a.c.token_stride;
+                const int tok = tok0 + group * 16;
+                x.at = id * a.c.block_stride + (shift >= 0 ? tok & (bs - 1) : tok % bs) * a.c.token_stride;
                 if (warp == 0) {
                     x.ks = a.c.d_k_scale[(long long)id * H + j.h];
                     x.vs = a.c.d_v_scale[(long long)id * H + j.h];
@@ -347,11 +354,13 @@ __device__ __forceinline__ void convert_role(const Args &a, TreeShared<D> &sm, u
                 float most = vs < INFINITY ? vs : 0.f, own = 0.f;
 #pragma unroll
                 for (int o = GROUPS / 2; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-                for (int t = 0; t < BATCH; ++t) {
-                    const float m = __shfl_sync(0xffffffffu, most, t * GROUPS);
-                    if (m >= 7.888609052210118e-31f && (vref == 0.f || m > vref * kValueLag)) vref = m;
-                    if (t == mine) own = vref;
-                }
+                if (__any_sync(0xffffffffu, vref == 0.f || most > vref * kValueLag)) {
+                    for (int t = 0; t < BATCH; ++t) {
+                        const float m = __shfl_sync(0xffffffffu, most, t * GROUPS);
+                        if (m >= 7.888609052210118e-31f && (vref == 0.f || m > vref * kValueLag)) vref = m;
+                        if (t == mine) own = vref;
+                    }
+                } else own = vref;
                 Meta &m = sm.meta[(it + batch * BATCH + mine) % kMetaRing];
                 m.ks[lane % GROUPS] = x.ks;
                 m.f[lane % GROUPS] = vs * (own == 0.f ? 0.f : kPart<FMT> / own);
@@ -390,49 +399,6 @@ __device__ __forceinline__ void convert_role(const Args &a, TreeShared<D> &sm, u
         };
 #pragma unroll 1
         for (int t = 0; t < RING - 1; ++t) load(t);
-
-        // ---- the query rows, a lane for each: two warps share 32 rows, each writes half of their elements
-        if (jobs >= 1) ok = ok && wait_together(sm.q_free, (jobs - 1) & 1, sm.failed);
-        {
-            unit_after_sync();
-            const int row = (warp & 3) * 32 + lane, g = j.row0 + row, half = warp >> 2;
-            const bool live = row < j.rows;
-            const uint4 *x = reinterpret_cast<const uint4 *>((const T *)a.q + (long long)(rq.first + (live ? g / G : 0)) * a.q_token + (long long)(j.h * G + (live ? g % G : 0)) * a.q_head);
-            float f = a.scale * 1.4426950408889634f;
-            int e = 0;
-            if constexpr (!std::is_same<T, __half>::value) {
-                float largest = 0.f;
-#pragma unroll 4
-                for (int i = 0; i < D / 8; ++i) {
-                    const uint4 v = live ? x[i] : make_uint4(0, 0, 0, 0);
-                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) largest = fmaxf(largest, fmaxf(fabsf(__uint_as_float(w[k] << 16)), fabsf(__uint_as_float(w[k] & 0xffff0000u))));
-                }
-                e = exponent_of(largest);
-                f = ldexpf(f, e);
-            }
-            const uint32_t to = sm.columns + ((uint32_t)((warp & 3) * 32) << 16) + C::kQ + half * (D / 4);
-#pragma unroll 1
-            for (int i = 0; i < D / 16; i += 2) {
-                uint32_t w[8];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const uint4 v = live ? x[half * (D / 16) + i + k] : make_uint4(0, 0, 0, 0);
-                    w[4 * k] = v.x; w[4 * k + 1] = v.y; w[4 * k + 2] = v.z; w[4 * k + 3] = v.w;
-                }
-                if constexpr (!std::is_same<T, __half>::value) {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) w[k] = half2_of_bf16(w[k], e);
-                }
-                store_columns(to + i * 4, w);
-            }
-            if (half == 0) sm.factor[parity][row] = f;
-            stores_done();
-            unit_before_sync();
-            __syncwarp();
-            if (lane == 0) arrive(sm.q_full);
-        }
 
         // ---- tile after tile
 #pragma unroll 1
@@ -506,81 +472,69 @@ template <int D> struct Turn {
     }
 };
 
-// The whole warp goes along, so that what it works out is the same for all lanes and stays in the registers that the unit's
-// instructions take; one lane issues them.  The next tile's scores are asked for as soon as there is a place, a tile's values
-// multiplied as soon as its probabilities are there, whichever comes first.  (One after the other: 180 us against 150 with 128 rows
-// on 16 requests of 8190 tokens.)
-template <int D>
+// Two warps issue the products, one the scores', one the values', so that neither waits for what the other waits for.  The whole
+// warp goes along, so that what it works out is the same for all lanes and stays in the registers that the unit's instructions
+// take; one lane issues them.  (One warp for both, whichever comes first: 140 us against 120 with 128 rows on 16 requests of 8190
+// tokens; in a fixed order 180.)
+template <int D, bool VALUES>
 __device__ __forceinline__ void product_role(const Args &a, TreeShared<D> &sm, uint32_t stages, Walk<D> &walk, int lane)
 {
     using C = Tree<D>;
-    constexpr uint32_t kScores = unit_kind(0, false, C::kTokens), kValues = unit_kind(1, true, D);
+    constexpr uint32_t kind = VALUES ? unit_kind(1, true, D) : unit_kind(0, false, C::kTokens);
     const uint32_t unit = __shfl_sync(0xffffffffu, sm.columns, 0);
-    const uint64_t keys0 = operand(stages, 16), values0 = operand(stages + C::kSide, C::kSlab);
+    const uint64_t operands = VALUES ? operand(stages + C::kSide, C::kSlab) : operand(stages, 16);
     bool ok = true;
-    Turn<D> scores, values;                      // of the tiles whose scores are asked for, whose values are multiplied
+    Turn<D> turn;
     unsigned jobs = 0, asked = 0;
     while (ok && walk.next(a, lane)) {
         const int tiles = __shfl_sync(0xffffffffu, walk.j.tiles, 0);
         if (tiles == 0) continue;
-        ok = wait_together(sm.q_full, jobs & 1, sm.failed);
-        unsigned long long idle = 0, began = 0;
-        for (int ts = 0, tv = 0; ok && tv < tiles;) {
-            const bool ask = ts < tiles && ts - tv < C::kPlaces && is_through(sm.full[scores.stage], scores.stage_phase) &&
-                             (asked < C::kPlaces || is_through(sm.pv_done[scores.place], scores.place_phase ^ 1));
-            if (__all_sync(0xffffffffu, ask)) {
+        if (!VALUES) ok = wait_together(sm.q_full, jobs & 1, sm.failed);
+        for (int t = 0; ok && t < tiles; ++t, turn.next()) {
+            const uint32_t place = unit + C::kS + turn.place * C::kTokens;
+            const uint64_t b = operands + (turn.stage * C::kStageBytes >> 4);
+            if constexpr (!VALUES) {
+                ok = (asked < C::kPlaces || wait_together(sm.pv_done[turn.place], turn.place_phase ^ 1, sm.failed)) && wait_together(sm.full[turn.stage], turn.stage_phase, sm.failed);
+                if (!ok) break;
                 unit_after_sync();
-                const uint64_t keys = keys0 + (scores.stage * C::kStageBytes >> 4);
-                const uint32_t to = unit + C::kS + scores.place * C::kTokens;
                 if (elected()) {
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) unit_mma(to, unit + C::kQ + k * 8, keys + ((k / 4 * C::kSlab + k % 4 * 32) >> 4), kScores, k > 0);
-                    unit_commit(sm.s_full[scores.place]);
-                    if (ts == tiles - 1) unit_commit(sm.q_free);
+                    for (int k = 0; k < D / 16; ++k) unit_mma(place, unit + C::kQ + k * 8, b + ((k / 4 * C::kSlab + k % 4 * 32) >> 4), kind, k > 0);
+                    unit_commit(sm.s_full[turn.place]);
                 }
-                __syncwarp();
-                scores.next();
                 asked += asked < C::kPlaces;
-                ++ts;
-                idle = 0;
-            }
-            if (__all_sync(0xffffffffu, tv < ts && is_through(sm.p_full[values.place], values.place_phase))) {
+            } else {
+                ok = wait_together(sm.p_full[turn.place], turn.place_phase, sm.failed);
+                if (!ok) break;
                 unit_after_sync();
-                const uint64_t at = values0 + (values.stage * C::kStageBytes >> 4);
-                const uint32_t o = unit + C::kO + values.group * D, p = unit + C::kS + values.place * C::kTokens;
-                const bool add = tv >= C::kGroups;
+                const uint32_t o = unit + C::kO + turn.group * D;
                 if (elected()) {
 #pragma unroll
                     for (int half = 0; half < 2; ++half)
 #pragma unroll
-                        for (int k = 0; k < C::kTokens / 16; ++k) unit_mma(o, p + half * (C::kTokens / 2) + k * 8, at + (k * 2048 >> 4), kValues, add || half > 0 || k > 0);
-                    unit_commit(sm.pv_done[values.place]);
-                    unit_commit(sm.free[values.stage]);
+                        for (int k = 0; k < C::kTokens / 16; ++k)
+                            unit_mma(o, place + half * (C::kTokens / 2) + k * 8, b + (k * 2048 >> 4), kind, t >= C::kGroups || half > 0 || k > 0);
+                    unit_commit(sm.pv_done[turn.place]);
+                    unit_commit(sm.free[turn.stage]);
                 }
-                __syncwarp();
-                values.next();
-                ++tv;
-                idle = 0;
-                continue;
             }
-            // (others want to issue; the limit of a wait is looked at now and then)
-            __nanosleep(20);
-            if ((++idle & 1023) == 0) {
-                const unsigned long long t = now_ns();
-                if (idle == 1024) began = t;
-                if (t - began > kWaitLimit) *(volatile int *)&sm.failed = 1;
-                ok = __all_sync(0xffffffffu, !*(volatile int *)&sm.failed);
-            }
+            __syncwarp();
         }
         ++jobs;
     }
     if (!ok) {                                   // what is under way has to end before the unit's memory is given back
-        if (elected()) unit_commit(sm.drained);
+        if (elected()) unit_commit(sm.drained[VALUES]);
         int own = 0;
-        wait_together(sm.drained, 0, own);
+        wait_together(sm.drained[VALUES], 0, own);
     }
 }
 
+__device__ __forceinline__ float max_of(float x, float y, float z)
+{
+    float v;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(v) : "f"(x), "f"(y), "f"(z));
+    return v;
+}
 // Two fp32 values at a time
 __device__ __forceinline__ unsigned long long two(float x, float y)
 {
@@ -628,7 +582,57 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
         const unsigned parity = jobs & 1;
         const bool live = warp % 4 * 32 < j.rows;                // (the rows of a warp are all past the end, or not)
         const int base = rq.length - rq.count, my_row = min(row, j.rows - 1);
-        float ref = kNoRef, sum = 0.f, vref = 0.f, factor = 0.f;
+        float ref = kNoRef, sum = 0.f, vref = 0.f, factor = a.scale * 1.4426950408889634f;
+        if (tiles > 0) {
+            // ---- the query row to the unit's memory, a part of it by each group (the last job's products are through)
+            constexpr int PARTS = D / 8 / GROUPS, HELD = PARTS < 8 ? PARTS : 8;
+            const int g = j.row0 + my_row;
+            const uint4 *q = reinterpret_cast<const uint4 *>((const T *)a.q + (long long)(rq.first + g / G) * a.q_token + (long long)(j.h * G + g % G) * a.q_head) + group * PARTS;
+            uint4 v[HELD];
+            auto load = [&](int first) {
+#pragma unroll
+                for (int i = 0; i < HELD; ++i) v[i] = row < j.rows ? q[first + i] : make_uint4(0, 0, 0, 0);
+            };
+            Power power = {1.f, 1.f};
+            if constexpr (!std::is_same<T, __half>::value) {
+                float largest = 0.f;
+#pragma unroll 1
+                for (int first = PARTS - HELD; first >= 0; first -= HELD) {
+                    load(first);
+#pragma unroll
+                    for (int i = 0; i < HELD; ++i) {
+                        const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) largest = fmaxf(largest, fmaxf(fabsf(__uint_as_float(w[k] << 16)), fabsf(__uint_as_float(w[k] & 0xffff0000u))));
+                    }
+                }
+                if (GROUPS == 2) {
+                    sm.largest[group][row] = largest;
+                    sync_some<2, C::kSoft>();
+                    largest = fmaxf(largest, sm.largest[group ^ 1][row]);
+                }
+                const int e = exponent_of(largest);
+                power = power_of(e);
+                factor = ldexpf(factor, e);
+            } else load(0);
+#pragma unroll 1
+            for (int first = 0; first < PARTS; first += HELD) {
+                if (first > 0) load(first);      // (the first are still held)
+#pragma unroll
+                for (int i = 0; i < HELD; i += 2) {
+                    uint32_t w[8] = {v[i].x, v[i].y, v[i].z, v[i].w, v[i + 1].x, v[i + 1].y, v[i + 1].z, v[i + 1].w};
+                    if constexpr (!std::is_same<T, __half>::value) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) w[k] = half2_scaled(w[k], power);
+                    }
+                    store_columns(unit + C::kQ + (group * PARTS + first + i) * 4, w);
+                }
+            }
+            stores_done();
+            unit_before_sync();
+            __syncwarp();
+            if (lane == 0) arrive(sm.q_full);
+        }
         const int t_first = (group - (int)it) & (GROUPS - 1);    // tiles go to the groups in turn, from job to job
         for (int t = 0; t < tiles; ++t, turn.next()) {
             if (GROUPS == 2 && t % 2 != t_first) continue;
@@ -643,7 +647,6 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
                 for (int i = 0; i < N; i += 32) load_columns(at + i, reinterpret_cast<uint32_t (&)[32]>(s[i]));
                 const Meta &m = sm.meta[(it + t) % kMetaRing];
                 const float4 ks = *reinterpret_cast<const float4 *>(m.ks), fs = *reinterpret_cast<const float4 *>(m.f), other = *reinterpret_cast<const float4 *>(&m.vref);
-                if (t == t_first) factor = sm.factor[parity][row];
                 const float c[4] = {factor * ks.x, factor * ks.y, factor * ks.z, factor * ks.w}, f[4] = {fs.x, fs.y, fs.z, fs.w};
                 const bool edge = __float_as_int(other.z), plain = !edge && fminf(fminf(c[0], c[1]), fminf(c[2], c[3])) >= 0.f;
                 float rescale = 1.f;
@@ -664,10 +667,9 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
                 if (plain) {
 #pragma unroll
                     for (int i = 0; i < N / 16; ++i) {
-                        float top[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) top[k] = fmaxf(fmaxf(x[i * 16 + k], x[i * 16 + 4 + k]), fmaxf(x[i * 16 + 8 + k], x[i * 16 + 12 + k]));
-                        most = fmaxf(most, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c[i]);
+                        const float *y = x + i * 16;
+                        const float t0 = max_of(y[0], y[1], y[2]), t1 = max_of(y[3], y[4], y[5]), t2 = max_of(y[6], y[7], y[8]), t3 = max_of(y[9], y[10], y[11]), t4 = max_of(y[12], y[13], y[14]);
+                        most = fmaxf(most, max_of(max_of(t0, t1, y[15]), t2, max_of(t3, t4, t4)) * c[i]);
                     }
                 } else {
 #pragma unroll
@@ -685,7 +687,7 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
                 unsigned long long sums = two(sum, 0.f);
 #pragma unroll
                 for (int i = 0; i < N / 16; ++i) {
-                    const unsigned long long c2 = two(c[i], c[i]), f2 = two(f[i], f[i]);
+                    const unsigned long long c2 = two(c[i], c[i]);
                     float q[16];
 #pragma unroll
                     for (int k = 0; k < 16; k += 2) {
@@ -698,6 +700,7 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
                         for (int k = 0; k < 16; ++k)
                             if (!(bits >> (i * 16 + k) & 1)) q[k] = 0.f;
                     }
+                    const unsigned long long f2 = two(f[i], f[i]);
                     uint32_t upper[8], rest[8];
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
@@ -706,9 +709,9 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
                         const unsigned long long w = mul_two(pair, f2);
                         float w0, w1, r0, r1;
                         apart(w, w0, w1);
-                        const __nv_bfloat162 u = __floats2bfloat162_rn(w0, w1);
-                        upper[k] = *reinterpret_cast<const uint32_t *>(&u);
-                        apart(fma_two(two(__uint_as_float(upper[k] << 16), __uint_as_float(upper[k] & 0xffff0000u)), minus_one, w), r0, r1);
+                        // (cut off, not rounded: what is left is exact in fp32 and rounded to eight bits more)
+                        upper[k] = __byte_perm(__float_as_uint(w0), __float_as_uint(w1), 0x7632);
+                        apart(fma_two(two(__uint_as_float(__float_as_uint(w0) & 0xffff0000u), __uint_as_float(__float_as_uint(w1) & 0xffff0000u)), minus_one, w), r0, r1);
                         const __nv_bfloat162 r = __floats2bfloat162_rn(r0, r1);
                         rest[k] = *reinterpret_cast<const uint32_t *>(&r);
                     }
@@ -775,20 +778,21 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
             if (!ok) l = NAN;
             const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m + log2f(l);
             const bool any_nan = tiles > 0 && sm.any_nan[parity];
-#pragma unroll 1
+#pragma unroll 2
             for (int d0 = group * (D / GROUPS); d0 < (group + 1) * (D / GROUPS); d0 += 16) {
                 float v[16];
 #pragma unroll
                 for (int k = 0; k < 16; ++k) v[k] = ok ? 0.f : NAN;
+                uint32_t o[GROUPS][16];
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g) load_columns(unit + C::kO + g * D + d0, o[g]);
+                loads_done();
 #pragma unroll
                 for (int g = 0; g < GROUPS; ++g) {
                     if (tiles <= ((g - (int)it) & (GROUPS - 1)) || !ok) continue;           // no tile was this group's
-                    uint32_t o[16];
-                    load_columns(unit + C::kO + g * D + d0, o);
-                    loads_done();
                     const float fv = f[g] * sm.vref[g];
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) v[k] += fv * (__uint_as_float(o[k]) * inv);
+                    for (int k = 0; k < 16; ++k) v[k] += fv * (__uint_as_float(o[g][k]) * inv);
                 }
                 if (any_nan) {
                     const uint32_t nan = sm.nan[parity][row][d0 / 32] >> (d0 % 32);
@@ -822,19 +826,12 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
                 auto slot_of = [&](int c) { return (long long)(c0 + c) * 2 + (c == 0); };
                 for (int r = tid; r < j.rows; r += C::kSoft) {
                     float top = -INFINITY, l = 0.f;
-                    bool nan = false;
 #pragma unroll 8
                     for (int c = 0; c < parts; ++c) {
-                        const float x = __ldcg(a.partial_lse + slot_of(c) * kRows + r);
-                        top = fmaxf(top, x);
-                        nan |= x != x;
+                        const float x = __ldcg(a.partial_lse + slot_of(c) * kRows + r), now = fmaxf(top, x);
+                        l = l * (top == -INFINITY ? 0.f : exp2_fast(top - now)) + (x == -INFINITY ? 0.f : exp2_fast(x - now));
+                        top = now;
                     }
-#pragma unroll 8
-                    for (int c = 0; c < parts; ++c) {
-                        const float x = __ldcg(a.partial_lse + slot_of(c) * kRows + r);
-                        l += x == -INFINITY ? 0.f : exp2_fast(x - top);
-                    }
-                    if (nan) l = NAN;
                     sm.join_max[r] = top == -INFINITY ? 0.f : top;
                     sm.join_inv[r] = l == 0.f ? 0.f : 1.f / l;
                     sm.join_lse[r] = l == 0.f ? -INFINITY : top + log2f(l);
@@ -933,20 +930,21 @@ __global__ void __launch_bounds__(Tree<D>::kThreads, 1) tree_attend_kernel(const
             barrier_init(sm.full[i], C::kConverters);
             barrier_init(sm.free[i], 1);
         }
-        barrier_init(sm.q_full, C::kConverters);
-        barrier_init(sm.q_free, 1);
-        barrier_init(sm.drained, 1);
+        barrier_init(sm.q_full, C::kSoft / 32);
         for (int i = 0; i < C::kPlaces; ++i) {
             barrier_init(sm.s_full[i], 1);
             barrier_init(sm.p_full[i], 4);
             barrier_init(sm.pv_done[i], 1);
         }
-        for (int i = 0; i < 2; ++i) barrier_init(sm.ended[i], 1);
+        for (int i = 0; i < 2; ++i) {
+            barrier_init(sm.ended[i], 1);
+            barrier_init(sm.drained[i], 1);
+        }
         sm.failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    constexpr int kIssuer = C::kThreads / 32 - 1;
+    constexpr int kIssuer = C::kThreads / 32 - 2;
     if (warp == kIssuer) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(&sm.columns)), "n"(C::kColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -968,9 +966,8 @@ __global__ void __launch_bounds__(Tree<D>::kThreads, 1) tree_attend_kernel(const
     } else if (warp < kIssuer) {
         if constexpr (C::kSplit) leave_registers<72>();
         convert_role<D, FMT, T>(a, sm, tiles, sm.walk[warp], tid - C::kSoft);
-    } else {
-        product_role<D>(a, sm, tiles, sm.walk[warp], lane);
-    }
+    } else if (warp == kIssuer) product_role<D, false>(a, sm, tiles, sm.walk[warp], lane);
+    else product_role<D, true>(a, sm, tiles, sm.walk[warp], lane);
     unit_before_sync();
     __syncthreads();
     unit_after_sync();
