@@ -210,17 +210,22 @@ class NormedRotary:
         """q, k [tokens][heads][head_dim] normed and turned to positions [tokens] (int32); outputs may be the inputs.  Returns
         (q_out, k_out), k_out None without k.  New outputs carry gradients (of the heads and of the gains, the first ones; they are
         formed on the stream that the gradients come on); outputs that were given are written without."""
-        if q_out is None and k_out is None and torch.is_grad_enabled() and any(x is not None and x.requires_grad for x in (q, k, self.q_weight, self.k_weight)):
-            return _NormedAndTurned.apply(self, q, k, self.q_weight, self.k_weight, positions, stream)
-        return self._apply(q, k, self.q_weight, self.k_weight, positions, q_out, k_out, stream)
+        qw, kw = self.q_weight, self.k_weight
+        if q_out is None and k_out is None and torch.is_grad_enabled() and (
+                q.requires_grad or (k is not None and k.requires_grad) or (qw is not None and qw.requires_grad) or (kw is not None and kw.requires_grad)):
+            return _NormedAndTurned.apply(self, q, k, qw, kw, positions, stream)
+        return self._apply(q, k, qw, kw, positions, q_out, k_out, stream)
 
     def _weights(self, q_weight, k_weight):
         """(type, addresses)"""
-        for w in (q_weight, k_weight):
-            if w is not None and w.get_device() != _device():
-                raise ValueError("the gains have to lie on the current CUDA device")
-        given = q_weight if q_weight is not None else k_weight
-        return (fluxbin.TYPE_FP32 if given is None else _TYPES[given.dtype], *(0 if w is None else w.data_ptr() for w in (q_weight, k_weight)))
+        here, kind, qp, kp = _device(), fluxbin.TYPE_FP32, 0, 0
+        if k_weight is not None:
+            kind, kp = _TYPES[k_weight.dtype], k_weight.data_ptr()
+        if q_weight is not None:
+            kind, qp = _TYPES[q_weight.dtype], q_weight.data_ptr()
+        if (qp and q_weight.get_device() != here) or (kp and k_weight.get_device() != here):
+            raise ValueError("the gains have to lie on the current CUDA device")
+        return kind, qp, kp
 
     def _check(self, q):
         if q.dtype not in _TYPES:
@@ -492,9 +497,8 @@ class DraftTree:
             raise ValueError("nodes: 1 to 1024 are wanted")
         pointers = _int32(query_start, B + 1, "query_start"), _int32(lengths, B, "lengths"), _int32(parents, n, "parents")
         self.parents, self.query_start, self.nodes = parents, query_start, nodes
-        words = -(-nodes // 32)
-        both = _made(stream, lambda: torch.empty(n * (words + 1), dtype=torch.int32, device=parents.device))
-        self.mask, self.positions = both[:n * words].view(n, words), both[n * words:]
+        self.mask = _made(stream, lambda: torch.empty((n, -(-nodes // 32)), dtype=torch.int32, device=parents.device))
+        self.positions = _made(stream, lambda: torch.empty_like(parents))
         fluxbin.draft_tree_call(B, n, nodes, *pointers, self.mask.data_ptr(), self.positions.data_ptr(), _stream(stream))
 
     def accept(self, drafted: torch.Tensor, answers: torch.Tensor, stream=None) -> SimpleNamespace:
@@ -504,9 +508,12 @@ class DraftTree:
         comes after it, `surplus`, what is to be dropped (as BlockTables.advance takes it)."""
         n, B = self.parents.shape[0], self.query_start.shape[0] - 1
         inputs = (_int32(self.query_start, B + 1, "query_start"), _int32(self.parents, n, "parents"), _int32(drafted, n, "drafted"), _int32(answers, n, "answers"))
-        path, *rest = _made(stream, lambda: torch.empty(n + 3 * B, dtype=torch.int32, device=self.parents.device)).split((n, B, B, B))
-        fluxbin.draft_accept_call(B, n, self.nodes, *inputs, path.data_ptr(), *(x.data_ptr() for x in rest), _stream(stream))
-        return SimpleNamespace(path=path, **dict(zip(("count", "answer", "surplus"), rest)))
+        path = _made(stream, lambda: torch.empty_like(self.parents))
+        three = _made(stream, lambda: torch.empty((3, B), dtype=torch.int32, device=self.parents.device))
+        at = three.data_ptr()
+        fluxbin.draft_accept_call(B, n, self.nodes, *inputs, path.data_ptr(), at, at + 4 * B, at + 8 * B, _stream(stream))
+        count, answer, surplus = three.unbind()
+        return SimpleNamespace(path=path, count=count, answer=answer, surplus=surplus)
 
 
 class AttentionBlock:

@@ -4,11 +4,13 @@
 //     e = turn_p^-1(dy),  dx = r (w e - n mean(w e n)),  dw = sum e n     backward: reads x and dy, writes dx
 //
 // A head is held by head_dim / 16 neighbouring lanes, two pieces of eight elements each -- the two halves of eight pairs, or
-// 16 neighbours where pairs are neighbours -- so a turn is a lane's own business and a mean is a few shuffles.  The CTAs that
-// are resident go over the tokens, all heads of a token at a time: its angles are formed once, gains stay in shared memory.
+// 16 neighbours where pairs are neighbours -- so a turn is a lane's own business and a mean is a few shuffles.  A warp takes a token,
+// or a part of its heads: it forms the token's angles for itself, keeps them and the gains in registers, and has two heads of
+// each lane under way.  No barrier of a CTA: with one for each token 8191 tokens of 72 heads took 92 us.
 // The backward pass forms r again (one more sum beside mean(w e n), on the same shuffles) instead of reading it: nothing is
 // kept from the forward pass but its inputs.  Gradients of the gains are summed in registers over all that a thread sees,
 // then over the CTA, then by a second launch over the CTAs: no atomics, the same sums each time.
+// Bound by memory.
 #include "fluxbin_rotary.cuh"
 
 using namespace fbd;
@@ -29,7 +31,9 @@ struct NormSide {
 struct NormArgs {
     fluxbin_rotary_t rot;
     float eps;
-    int tokens, weight_dtype, heads_each;
+    int tokens, weight_dtype;
+    unsigned splits;
+    int heads_each;
     const int *positions;
     NormSide q, k;
 };
@@ -107,79 +111,112 @@ template <int LANES> __device__ __forceinline__ float sum_of(float v)
     return v;
 }
 
+// What a warp's item is: a token and a range of its heads
+struct Item { int t, h0, h1; };
+__device__ __forceinline__ Item item_of(const NormArgs &a, unsigned i)
+{
+    Item x;
+    x.t = (int)(i / a.splits);
+    x.h0 = (int)(i % a.splits) * a.heads_each;
+    x.h1 = min(x.h0 + a.heads_each, a.q.heads + a.k.heads);
+    return x;
+}
+// Gains and a token's angles as the lanes want them: 16 values of each lane, four at a time, side by side
+template <int LANES> struct Lanes {
+    float4 weight[2][4][LANES];
+    float4 angles[kThreads / 32][4][LANES];
+};
+template <bool INTER, int LANES> __device__ __forceinline__ void keep_weights(const NormArgs &a, Lanes<LANES> &sm)
+{
+    for (int i = threadIdx.x; i < 2 * LANES * 16; i += kThreads) {
+        const int side = i / (LANES * 16), u = i / 16 % LANES, k = i % 16;
+        const Place p = place_of<INTER>(a.rot, u);
+        reinterpret_cast<float *>(&sm.weight[side][k / 4][u])[k % 4] = p.there ? gain(side ? a.k.weight : a.q.weight, a.weight_dtype, k < 8 ? p.e0 + k : p.e1 + k - 8) : 0.f;
+    }
+    __syncthreads();
+}
+// f(element, gain) for a lane's 16 elements, gains from shared memory each time: registers are what limits the bytes under way
+template <int LANES, typename F> __device__ __forceinline__ void with_weights(const Lanes<LANES> &sm, int side, int u, F f)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float4 w = sm.weight[side][k][u];
+        f(4 * k, w.x);
+        f(4 * k + 1, w.y);
+        f(4 * k + 2, w.z);
+        f(4 * k + 3, w.w);
+    }
+}
+template <int LANES> __device__ __forceinline__ void lane_angles(const NormArgs &a, Lanes<LANES> &sm, int position, int warp, int lane, float2 (&cs)[8])
+{
+    __syncwarp();                                // the last token's have been read
+    for (int p = lane; p < a.rot.rotary_dim / 2; p += 32) {
+        float2 x;
+        pair_angle(position, a.rot.d_turns[p], a.rot.magnitude, 1.f, x.x, x.y);
+        reinterpret_cast<float2 *>(&sm.angles[warp][p % 8 / 2][p / 8])[p & 1] = x;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) *reinterpret_cast<float4 *>(cs + 2 * k) = sm.angles[warp][k][lane % LANES];
+}
+
 template <typename T, bool INTER, int LANES>
 __global__ void __launch_bounds__(kThreads, 3) norm_kernel(const __grid_constant__ NormArgs a)
 {
-    constexpr int ROWS = kThreads / LANES, BATCH = 2;
-    __shared__ __align__(16) float2 angles[2][kMaxPairs];
-    __shared__ __align__(16) float weight[2][kMaxDim];
-    const int tid = threadIdx.x, row = tid / LANES, D = a.rot.head_dim;
-    const Place at = place_of<INTER>(a.rot, tid % LANES);
-    const float inverse_dim = 1.f / D;
+    constexpr int ROWS = 32 / LANES, AHEAD = sizeof(T) == 4 ? 1 : 2;
+    __shared__ Lanes<LANES> sm;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, row = lane / LANES, u = lane % LANES;
+    const Place at = place_of<INTER>(a.rot, u);
+    const float inverse_dim = 1.f / a.rot.head_dim;
     let_successor_start();
     wait_for_predecessor();
-    const int h0 = blockIdx.y * a.heads_each, h1 = min(h0 + a.heads_each, a.q.heads + a.k.heads);
-    for (int e = tid; e < D; e += kThreads) {
-        weight[0][e] = gain(a.q.weight, a.weight_dtype, e);
-        weight[1][e] = gain(a.k.weight, a.weight_dtype, e);
-    }
-    int position = a.positions[blockIdx.x], buffer = 0;
-    // (two sets of angles: a thread may form the next token's while another still reads these)
-    for (int t = blockIdx.x; t < a.tokens; t += gridDim.x, buffer ^= 1) {
-        const int next = t + (int)gridDim.x < a.tokens ? a.positions[t + gridDim.x] : 0;
-        token_angles(a.rot, position, 1.f, angles[buffer], tid, kThreads);
-        __syncthreads();
-        position = next;
+    keep_weights<INTER, LANES>(a, sm);
+    const unsigned items = (unsigned)a.tokens * a.splits, step = gridDim.x * (kThreads / 32);          // (more than 2^31 tokens are not split)
+    for (unsigned i = blockIdx.x * (kThreads / 32) + warp; i < items; i += step) {
+        const Item item = item_of(a, i);
         float2 cs[8];
-        if (at.there && at.turns) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) cs[i] = angles[buffer][tid % LANES * 8 + i];
-        }
+        bool formed = false;
 #pragma unroll 1
         for (int side = 0; side < 2; ++side) {
             const NormSide &S = side ? a.k : a.q;
-            const int lo = max(h0 - (side ? a.q.heads : 0), 0), hi = min(h1 - (side ? a.q.heads : 0), S.heads);
+            const int lo = max(item.h0 - (side ? a.q.heads : 0), 0), hi = min(item.h1 - (side ? a.q.heads : 0), S.heads);
             if (lo >= hi) continue;
-            float w[16];
-            if (at.there) {
-#pragma unroll
-                for (int i = 0; i < 8; i += 4) {
-                    *reinterpret_cast<float4 *>(w + i) = *reinterpret_cast<const float4 *>(&weight[side][at.e0 + i]);
-                    *reinterpret_cast<float4 *>(w + 8 + i) = *reinterpret_cast<const float4 *>(&weight[side][at.e1 + i]);
+            const T *x = (const T *)S.x + item.t * S.x_token + (long long)(lo + row) * S.x_head;
+            T *y = (T *)S.y + item.t * S.y_token + (long long)(lo + row) * S.y_head;
+            Piece<T> p[AHEAD][2];
+            auto load = [&](int h, Piece<T> (&to)[2]) {
+                if (at.there && h + row < hi) {
+                    to[0].load(x + at.e0);
+                    to[1].load(x + at.e1);
                 }
-            }
-            const T *x = (const T *)S.x + t * S.x_token + (long long)(lo + row) * S.x_head;
-            T *y = (T *)S.y + t * S.y_token + (long long)(lo + row) * S.y_head;
+                x += ROWS * S.x_head;
+            };
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) load(lo + j * ROWS, p[j]);
+            if (!formed) lane_angles<LANES>(a, sm, a.positions[item.t], warp, lane, cs);         // (while the first heads are on their way)
+            formed = true;
             // (every lane goes as many rounds: they meet in the shuffles)
-            for (int h = lo; h < hi; h += BATCH * ROWS, x += BATCH * ROWS * S.x_head, y += BATCH * ROWS * S.y_head) {
-                Piece<T> p[BATCH][2];
+            for (int h0 = lo; h0 < hi; h0 += AHEAD * ROWS)
 #pragma unroll
-                for (int j = 0; j < BATCH; ++j)
-                    if (at.there && h + row + j * ROWS < hi) {
-                        p[j][0].load(x + j * ROWS * S.x_head + at.e0);
-                        p[j][1].load(x + j * ROWS * S.x_head + at.e1);
-                    }
-#pragma unroll
-                for (int j = 0; j < BATCH; ++j) {
-                    if (h + j * ROWS >= hi) break;
-                    const bool mine = at.there && h + row + j * ROWS < hi;
+                for (int j = 0; j < AHEAD; ++j, y += ROWS * S.y_head) {
+                    const int h = h0 + j * ROWS;
+                    if (h >= hi) break;
+                    const bool mine = at.there && h + row < hi;
                     float v[16], squares = 0.f;
+                    p[j][0].get(v);
+                    p[j][1].get(v + 8);
+                    load(h + AHEAD * ROWS, p[j]);
                     if (mine) {
-                        p[j][0].get(v);
-                        p[j][1].get(v + 8);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) squares = fmaf(v[i], v[i], squares);
+                        for (int k = 0; k < 16; ++k) squares = fmaf(v[k], v[k], squares);
                     }
                     const float r = __frsqrt_rn(fmaf(sum_of<LANES>(squares), inverse_dim, a.eps));
                     if (!mine) continue;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = v[i] * r * w[i];
+                    with_weights<LANES>(sm, side, u, [&](int k, float w) { v[k] = v[k] * r * w; });
                     if (at.turns) turn_all<INTER>(v, cs, 1.f);
-                    T *to = y + j * ROWS * S.y_head;
-                    Piece<T>::put(to + at.e0, v);
-                    Piece<T>::put(to + at.e1, v + 8);
+                    Piece<T>::put(y + at.e0, v);
+                    Piece<T>::put(y + at.e1, v + 8);
                 }
-            }
         }
     }
 }
@@ -187,96 +224,93 @@ __global__ void __launch_bounds__(kThreads, 3) norm_kernel(const __grid_constant
 template <typename T, bool INTER, int LANES>
 __global__ void __launch_bounds__(kThreads, 2) norm_backward_kernel(const __grid_constant__ NormArgs a)
 {
-    constexpr int ROWS = kThreads / LANES;
-    __shared__ __align__(16) float2 angles[2][kMaxPairs];
-    __shared__ __align__(16) float weight[2][kMaxDim];
-    __shared__ float sums[16][kThreads];
-    const int tid = threadIdx.x, row = tid / LANES, D = a.rot.head_dim;
-    const Place at = place_of<INTER>(a.rot, tid % LANES);
+    constexpr int ROWS = 32 / LANES;
+    __shared__ union { Lanes<LANES> lanes; float sums[16][kThreads]; } sm;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32, row = lane / LANES, u = lane % LANES, D = a.rot.head_dim;
+    const Place at = place_of<INTER>(a.rot, u);
     const float inverse_dim = 1.f / D;
     let_successor_start();
     wait_for_predecessor();
-    const int h0 = blockIdx.y * a.heads_each, h1 = min(h0 + a.heads_each, a.q.heads + a.k.heads);
-    for (int e = tid; e < D; e += kThreads) {
-        weight[0][e] = gain(a.q.weight, a.weight_dtype, e);
-        weight[1][e] = gain(a.k.weight, a.weight_dtype, e);
-    }
+    keep_weights<INTER, LANES>(a, sm.lanes);
     float dw[2][16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) dw[0][i] = dw[1][i] = 0.f;
-    int position = a.positions[blockIdx.x], buffer = 0;
-    for (int t = blockIdx.x; t < a.tokens; t += gridDim.x, buffer ^= 1) {
-        const int next = t + (int)gridDim.x < a.tokens ? a.positions[t + gridDim.x] : 0;
-        token_angles(a.rot, position, 1.f, angles[buffer], tid, kThreads);
-        __syncthreads();
-        position = next;
+    const unsigned items = (unsigned)a.tokens * a.splits, step = gridDim.x * (kThreads / 32);          // (more than 2^31 tokens are not split)
+    for (unsigned i = blockIdx.x * (kThreads / 32) + warp; i < items; i += step) {
+        const Item item = item_of(a, i);
         float2 cs[8];
-        if (at.there && at.turns) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) cs[i] = angles[buffer][tid % LANES * 8 + i];
-        }
+        bool formed = false;
 #pragma unroll
         for (int side = 0; side < 2; ++side) {
             const NormSide &S = side ? a.k : a.q;
-            const int lo = max(h0 - (side ? a.q.heads : 0), 0), hi = min(h1 - (side ? a.q.heads : 0), S.heads);
+            const int lo = max(item.h0 - (side ? a.q.heads : 0), 0), hi = min(item.h1 - (side ? a.q.heads : 0), S.heads);
             if (lo >= hi) continue;
-            const T *x = (const T *)S.x + t * S.x_token + (long long)(lo + row) * S.x_head;
-            const T *g = (const T *)S.grad + t * S.g_token + (long long)(lo + row) * S.g_head;
-            T *dx = S.y ? (T *)S.y + t * S.y_token + (long long)(lo + row) * S.y_head : nullptr;
-            for (int h = lo; h < hi; h += ROWS, x += ROWS * S.x_head, g += ROWS * S.g_head) {
-                const bool mine = at.there && h + row < hi;
-                float v[16], e[16], squares = 0.f, both = 0.f;
-                if (mine) {
-                    Piece<T> p[4];
+            const T *x = (const T *)S.x + item.t * S.x_token + (long long)(lo + row) * S.x_head;
+            const T *g = (const T *)S.grad + item.t * S.g_token + (long long)(lo + row) * S.g_head;
+            T *dx = S.y ? (T *)S.y + item.t * S.y_token + (long long)(lo + row) * S.y_head : nullptr;
+            Piece<T> p[4];
+            auto load = [&](int h) {
+                if (at.there && h + row < hi) {
                     p[0].load(x + at.e0);
                     p[1].load(x + at.e1);
                     p[2].load(g + at.e0);
                     p[3].load(g + at.e1);
-                    p[0].get(v);
-                    p[1].get(v + 8);
-                    p[2].get(e);
-                    p[3].get(e + 8);
+                }
+            };
+            load(lo);
+            if (!formed) lane_angles<LANES>(a, sm.lanes, a.positions[item.t], warp, lane, cs);
+            formed = true;
+            for (int h = lo; h < hi; h += ROWS) {
+                const bool mine = at.there && h + row < hi;
+                float v[16], e[16], squares = 0.f, both = 0.f;
+                p[0].get(v);
+                p[1].get(v + 8);
+                p[2].get(e);
+                p[3].get(e + 8);
+                x += ROWS * S.x_head;
+                g += ROWS * S.g_head;
+                if (sizeof(T) == 2) load(h + ROWS);              // (registers for the next ones)
+                if (mine) {
                     if (at.turns) turn_all<INTER>(e, cs, -1.f);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        squares = fmaf(v[i], v[i], squares);
-                        both = fmaf(weight[side][i < 8 ? at.e0 + i : at.e1 + i - 8] * e[i], v[i], both);
-                    }
+                    with_weights<LANES>(sm.lanes, side, u, [&](int k, float w) {
+                        squares = fmaf(v[k], v[k], squares);
+                        both = fmaf(w * e[k], v[k], both);
+                    });
                 }
                 squares = sum_of<LANES>(squares);
                 both = sum_of<LANES>(both);
-                if (!mine) continue;
-                const float r = __frsqrt_rn(fmaf(squares, inverse_dim, a.eps)), mean = both * r * inverse_dim;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float n = v[i] * r;
-                    dw[side][i] = fmaf(e[i], n, dw[side][i]);
-                    v[i] = r * fmaf(-n, mean, weight[side][i < 8 ? at.e0 + i : at.e1 + i - 8] * e[i]);
+                if (mine) {
+                    const float r = __frsqrt_rn(fmaf(squares, inverse_dim, a.eps)), mean = both * r * inverse_dim;
+                    with_weights<LANES>(sm.lanes, side, u, [&](int k, float w) {
+                        const float n = v[k] * r;
+                        dw[side][k] = fmaf(e[k], n, dw[side][k]);
+                        v[k] = r * fmaf(-n, mean, w * e[k]);
+                    });
+                    if (dx) {
+                        Piece<T>::put(dx + at.e0, v);
+                        Piece<T>::put(dx + at.e1, v + 8);
+                    }
                 }
-                if (dx) {
-                    T *to = dx + (h - lo) * S.y_head;
-                    Piece<T>::put(to + at.e0, v);
-                    Piece<T>::put(to + at.e1, v + 8);
-                }
+                if (dx) dx += ROWS * S.y_head;
+                if (sizeof(T) != 2) load(h + ROWS);
             }
         }
     }
-    const int part = blockIdx.y * gridDim.x + blockIdx.x;
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
         float *to = side ? a.k.part : a.q.part;
         if (!to) continue;                       // (the same for every thread)
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sums[i][tid] = dw[side][i];
+        for (int i = 0; i < 16; ++i) sm.sums[i][tid] = dw[side][i];
         __syncthreads();
         for (int j = tid; j < LANES * 16; j += kThreads) {
-            const int u = j / 16, i = j % 16;
-            const Place p = place_of<INTER>(a.rot, u);
+            const int lane_of = j / 16, i = j % 16;
+            const Place p = place_of<INTER>(a.rot, lane_of);
             if (!p.there) continue;
             float s = 0.f;
-            for (int k = 0; k < ROWS; ++k) s += sums[i][k * LANES + u];
-            to[(long long)part * D + (i < 8 ? p.e0 + i : p.e1 + i - 8)] = s;
+            for (int k = 0; k < kThreads / LANES; ++k) s += sm.sums[i][k * LANES + lane_of];
+            to[(long long)blockIdx.x * D + (i < 8 ? p.e0 + i : p.e1 + i - 8)] = s;
         }
     }
 }
@@ -427,16 +461,18 @@ template <typename T> bool wide(const NormArgs &a, bool backward)
 
 template <typename T, bool INTER, int LANES> cudaError_t run_wide(NormArgs a, bool backward, int &parts, cudaStream_t s)
 {
-    // CTAs that are resident at once go over the tokens; few tokens split their heads
-    constexpr int ROWS = kThreads / LANES;
-    const int ctas = 148 * (backward ? 2 : 3), heads = a.q.heads + a.k.heads;
-    const int x = a.tokens < ctas ? a.tokens : ctas;
-    int y = ctas / x, most = (heads + ROWS - 1) / ROWS;
-    if (y > most) y = most;
-    a.heads_each = (heads + y - 1) / y;
-    y = (heads + a.heads_each - 1) / a.heads_each;
-    parts = x * y;
-    const dim3 grid((unsigned)x, (unsigned)y);
+    // Resident warps go over tokens.  Tokens are split into parts of their heads until there are three for every warp, but no part is
+    // less than four rounds of heads, since the angles are formed for each; fewer tokens than warps are split until every warp has one.
+    constexpr int ROWS = 32 / LANES, WARPS = kThreads / 32;
+    const long long heads = a.q.heads + a.k.heads, rounds = (heads + ROWS - 1) / ROWS, ctas = 148 * (backward ? 2 : 3), warps = ctas * WARPS;
+    long long splits = (3 * warps + a.tokens - 1) / a.tokens, most = rounds / 4 > 1 ? rounds / 4 : 1;
+    if (splits > most) splits = most;
+    if (a.tokens * splits < warps) splits = (warps + a.tokens - 1) / a.tokens < rounds ? (warps + a.tokens - 1) / a.tokens : rounds;
+    a.heads_each = (int)((rounds + splits - 1) / splits) * ROWS;
+    a.splits = (unsigned)((heads + a.heads_each - 1) / a.heads_each);
+    const long long items = (long long)a.tokens * a.splits, need = (items + WARPS - 1) / WARPS;
+    parts = (int)(need < ctas ? need : ctas);
+    const dim3 grid((unsigned)parts);
     return backward ? launch(norm_backward_kernel<T, INTER, LANES>, grid, kThreads, 0, s, a) : launch(norm_kernel<T, INTER, LANES>, grid, kThreads, 0, s, a);
 }
 template <typename T, bool INTER> cudaError_t run_lanes(const NormArgs &a, bool backward, int &parts, cudaStream_t s)
