@@ -210,7 +210,6 @@ template <int D> struct TreeShared {
     int any_nan[2];
     float m[2][kRows], l[2][kRows], vref[2];     // of the two softmax groups
     float largest[2][kRows];                     // of the parts of the query rows
-    float join_max[kRows], join_inv[kRows], join_lse[kRows];
     Meta meta[kMetaRing];
     unsigned long long full[Tree<D>::kStages], free[Tree<D>::kStages];
     unsigned long long q_full, s_full[3], p_full[3], pv_done[3], ended[2], drained[2];
@@ -289,7 +288,7 @@ __device__ __forceinline__ void convert_role(const Args &a, TreeShared<D> &sm, u
     using C = Tree<D>;
     constexpr int PIECES = D / 16, THREADS = C::kConverters * 32, PASS = THREADS / PIECES, N = C::kTokens / PASS, GROUPS = C::kTokens / 16, BATCH = 32 / GROUPS, RING = C::kRing;
     static_assert(PASS % 16 == 0 && C::kStages + RING + BATCH + 1 <= kMetaRing && RING <= BATCH, "places and scales ahead");
-    const int lane = tid & 31, warp = tid >> 5, bs = a.c.block_tokens, H = a.c.kv_heads, G = a.q_heads / H;
+    const int lane = tid & 31, warp = tid >> 5, bs = a.c.block_tokens, H = a.c.kv_heads;
     // a thread's 16 elements of tokens sub, sub + PASS ...; eight neighbouring lanes hold four pieces of two neighbouring tokens: their
     // chunks go to all banks
     const int piece = lane % 4 + lane / (128 / PIECES) * 4, sub = warp * (32 / PIECES) + lane / 4 % (32 / PIECES);
@@ -581,7 +580,7 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
         const int tiles = j.tiles;
         const unsigned parity = jobs & 1;
         const bool live = warp % 4 * 32 < j.rows;                // (the rows of a warp are all past the end, or not)
-        const int base = rq.length - rq.count, my_row = min(row, j.rows - 1);
+        const int my_row = min(row, j.rows - 1);
         float ref = kNoRef, sum = 0.f, vref = 0.f, factor = a.scale * 1.4426950408889634f;
         if (tiles > 0) {
             // ---- the query row to the unit's memory, a part of it by each group (the last job's products are through)
@@ -756,15 +755,21 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
         unit_after_sync();
         const bool whole = j.p0 == 0 && j.p1 == rq.pieces;
         const long long slot = share * 2 + (j.p0 == 0);
-        float *part = a.partial + slot * kRows * D, *part_lse = a.partial_lse + slot * kRows;
-        auto write_out = [&](int r, int d, const float (&v)[4], float lse2) {
-            const int g = j.row0 + r, head = j.h * G + g % G;
+        // partial results lie element by element with the rows side by side, four elements together
+        auto part_of = [&](long long slot) { return reinterpret_cast<float4 *>(a.partial + slot * kRows * D) + row; };
+        auto put_eight = [&](int d, const float *v) {
+            const int g = j.row0 + my_row, head = j.h * G + g % G;
             const long long tok = rq.first + g / G;
-            T *op = (T *)a.out + tok * a.out_token + (long long)head * a.out_head + d;
-            __align__(8) T e[4] = {from_float<T>(v[0]), from_float<T>(v[1]), from_float<T>(v[2]), from_float<T>(v[3])};
-            *reinterpret_cast<uint2 *>(op) = *reinterpret_cast<const uint2 *>(e);
-            if (d == 0 && a.lse) a.lse[tok * a.q_heads + head] = lse2 * 0.6931471805599453f;
+            __align__(16) T e[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) e[k] = from_float<T>(v[k]);
+            *reinterpret_cast<uint4 *>((T *)a.out + tok * a.out_token + (long long)head * a.out_head + d) = *reinterpret_cast<const uint4 *>(e);
         };
+        auto put_lse = [&](float lse2) {
+            const int g = j.row0 + my_row;
+            if (group == 0 && a.lse) a.lse[(long long)(rq.first + g / G) * a.q_heads + j.h * G + g % G] = lse2 * 0.6931471805599453f;
+        };
+        constexpr int OWN = D / GROUPS;          // elements of a thread
         if (live) {
             float m = -INFINITY, l = 0.f, f[GROUPS];
 #pragma unroll
@@ -778,7 +783,7 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
             if (!ok) l = NAN;
             const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m + log2f(l);
             const bool any_nan = tiles > 0 && sm.any_nan[parity];
-#pragma unroll 2
+#pragma unroll 1
             for (int d0 = group * (D / GROUPS); d0 < (group + 1) * (D / GROUPS); d0 += 16) {
                 float v[16];
 #pragma unroll
@@ -801,14 +806,18 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
                         if (nan >> k & 1) v[k] = NAN;
                 }
                 if (row < j.rows) {
+                    if (whole) {
+                        put_eight(d0, v);
+                        put_eight(d0 + 8, v + 8);
+                    } else {
 #pragma unroll
-                    for (int k = 0; k < 16; k += 4) {
-                        const float e[4] = {v[k], v[k + 1], v[k + 2], v[k + 3]};
-                        if (whole) write_out(row, d0 + k, e, lse2);
-                        else *reinterpret_cast<float4 *>(part + row * D + d0 + k) = make_float4(e[0], e[1], e[2], e[3]);
+                        for (int k = 0; k < 16; k += 4) part_of(slot)[(d0 + k) / 4 * kRows] = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
                     }
-                    if (!whole && d0 == 0) part_lse[row] = lse2;
                 }
+            }
+            if (row < j.rows) {
+                if (whole) put_lse(lse2);
+                else if (group == 0) a.partial_lse[slot * kRows + row] = lse2;
             }
             unit_before_sync();
         }
@@ -824,47 +833,36 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
                 __threadfence();
                 const int parts = c1 - c0 + 1;
                 auto slot_of = [&](int c) { return (long long)(c0 + c) * 2 + (c == 0); };
-                for (int r = tid; r < j.rows; r += C::kSoft) {
+                if (row < j.rows) {
                     float top = -INFINITY, l = 0.f;
 #pragma unroll 8
                     for (int c = 0; c < parts; ++c) {
-                        const float x = __ldcg(a.partial_lse + slot_of(c) * kRows + r), now = fmaxf(top, x);
+                        const float x = __ldcg(a.partial_lse + slot_of(c) * kRows + row), now = fmaxf(top, x);
                         l = l * (top == -INFINITY ? 0.f : exp2_fast(top - now)) + (x == -INFINITY ? 0.f : exp2_fast(x - now));
                         top = now;
                     }
-                    sm.join_max[r] = top == -INFINITY ? 0.f : top;
-                    sm.join_inv[r] = l == 0.f ? 0.f : 1.f / l;
-                    sm.join_lse[r] = l == 0.f ? -INFINITY : top + log2f(l);
-                }
-                sync_some<2, C::kSoft>();
-                constexpr int kEach = 8;         // pieces of four elements of a thread, under way together
-                const int items = j.rows * (D / 4);
-                for (int first = tid; first < items; first += C::kSoft * kEach) {
-                    float v[kEach][4];
+                    put_lse(l == 0.f ? -INFINITY : top + log2f(l));
+                    if (top == -INFINITY) top = 0.f;
+                    l = l == 0.f ? 0.f : 1.f / l;
+                    constexpr int AT_ONCE = 16;
+#pragma unroll 1
+                    for (int d0 = group * OWN; d0 < (group + 1) * OWN; d0 += AT_ONCE) {
+                        float v[AT_ONCE];
 #pragma unroll
-                    for (int k = 0; k < kEach; ++k) v[k][0] = v[k][1] = v[k][2] = v[k][3] = 0.f;
-                    for (int c = 0; c < parts; ++c) {
-                        const float *lse = a.partial_lse + slot_of(c) * kRows;
-                        const float4 *o = reinterpret_cast<const float4 *>(a.partial + slot_of(c) * kRows * D);
-                        float4 y[kEach];
-                        float f[kEach];
+                        for (int k = 0; k < AT_ONCE; ++k) v[k] = 0.f;
+#pragma unroll 1
+                        for (int c = 0; c < parts; ++c) {
+                            float4 y[AT_ONCE / 4];
 #pragma unroll
-                        for (int k = 0; k < kEach; ++k) {
-                            const int i = min(first + k * C::kSoft, items - 1);
-                            y[k] = __ldcg(o + i);
-                            f[k] = __ldcg(lse + i / (D / 4));
+                            for (int k = 0; k < AT_ONCE / 4; ++k) y[k] = __ldcg(part_of(slot_of(c)) + (d0 / 4 + k) * kRows);
+                            const float w = exp2_fast(__ldcg(a.partial_lse + slot_of(c) * kRows + row) - top) * l;
+#pragma unroll
+                            for (int k = 0; k < AT_ONCE / 4; ++k) {
+                                v[4 * k] += w * y[k].x; v[4 * k + 1] += w * y[k].y; v[4 * k + 2] += w * y[k].z; v[4 * k + 3] += w * y[k].w;
+                            }
                         }
 #pragma unroll
-                        for (int k = 0; k < kEach; ++k) {
-                            const int r = min(first + k * C::kSoft, items - 1) / (D / 4);
-                            f[k] = exp2_fast(f[k] - sm.join_max[r]) * sm.join_inv[r];
-                            v[k][0] += f[k] * y[k].x; v[k][1] += f[k] * y[k].y; v[k][2] += f[k] * y[k].z; v[k][3] += f[k] * y[k].w;
-                        }
-                    }
-#pragma unroll
-                    for (int k = 0; k < kEach; ++k) {
-                        const int i = first + k * C::kSoft;
-                        if (i < items) write_out(i / (D / 4), i % (D / 4) * 4, v[k], sm.join_lse[i / (D / 4)]);
+                        for (int k = 0; k < AT_ONCE; k += 8) put_eight(d0 + k, v + k);
                     }
                 }
                 if (tid == 0) a.arrived[c0] = 0;
@@ -890,8 +888,6 @@ __global__ void __launch_bounds__(Tree<D>::kThreads, 1) tree_attend_kernel(const
 
     let_successor_start();
     wait_for_predecessor();
-    if (a.query_start) empty_rows<D, T>(a, tid, C::kThreads);
-
     // ---- where this CTA's part begins: a sum over the requests, each thread over a run of them
     const int per = (a.batch + C::kThreads - 1) / C::kThreads, r_lo = min(tid * per, a.batch), r_hi = min(r_lo + per, a.batch);
     auto units = [&](int r) {
@@ -913,6 +909,7 @@ __global__ void __launch_bounds__(Tree<D>::kThreads, 1) tree_attend_kernel(const
         total += sm.scan[w];
     }
     const long long active = min((long long)gridDim.x, total);
+    if (a.query_start) empty_rows<D, T>(a, tid, C::kThreads);
     if (blockIdx.x >= active) return;            // (the whole CTA)
     const long long size = total / active, over = total - size * active;
     auto cut = [&](long long i) { return i * size + min(i, over); };
