@@ -3,10 +3,10 @@
 
 namespace {
 
-// Rows that share a key head in an average request up to which the kernel for few rows is ahead: 16 requests of 8190 tokens, this kernel
-// against the other, 16 rows 85 us and 118 at head dimension 128, 54 and 77 at 256, 49 and 90 at 64; 24 rows 160 and 118 at 128;
-// 32 rows 87 and 82 at 256, 98 and 90 at 64.
-constexpr long long kFewRows = 16;
+// Rows that share a key head in an average request up to which the kernel for few rows is ahead.  16 requests of 8190 tokens, that kernel
+// against the other: head dimension 128 16 rows 94 us and 115, 24 rows 160 and 116; 64 16 rows 49 and 82, 32 rows 78 and 82, 64 rows
+// 148 and 82; 256 16 rows 56 and 77, 32 rows 87 and 88, 128 rows 293 and 93.
+int few_rows(int head_dim) { return head_dim == 128 ? 16 : 32; }
 
 // A workspace of both kernels: the counters of the one for few rows, the partial results of either (of one call at a time), the
 // counters of this one -- behind all that the other writes, since each finds its own zeroed.
@@ -18,7 +18,7 @@ size_t counters_at(int head_dim)
 template <typename T> cudaError_t run_type(Args a, char *workspace, cudaStream_t s)
 {
     const long long rows = (long long)(a.q_heads / a.c.kv_heads) * ((a.tokens + a.batch - 1) / a.batch);
-    if (rows <= kFewRows) return run_dim<T, true>(a, s);
+    if (rows <= few_rows(a.c.head_dim)) return run_dim<T, true>(a, s);
     a.arrived = (unsigned *)(workspace + counters_at(a.c.head_dim));
     a.partial_lse = (float *)(workspace + kCounterBytes);
     a.partial = (float *)(workspace + kCounterBytes + kTreeLseBytes);

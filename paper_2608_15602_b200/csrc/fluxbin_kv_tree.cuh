@@ -10,8 +10,8 @@
 //   P      times its token's value scale: two bf16 numbers, written where S was, which lose 2^-16 of it and flush nothing
 //          short of fp32's range (see the kernel for few rows); so the second product is made twice
 // The cache's bytes come in by asynchronous copies, 16 a thread, into places of shared memory that only this thread reads again, a few
-// tiles ahead; the same thread converts them into swizzled tiles.  (A tile or two in registers instead: 174 us against 120 with 128
-// rows on 16 requests of 8190 tokens, and a warp that waits for the older one's bytes waits for the younger one's too.)
+// tiles ahead; the same thread converts them into swizzled tiles.  (In registers instead a warp that waits for the older tile's bytes
+// waits for the younger one's too.)
 //
 // Warps: four or eight for the softmax, eight that load and convert, two that issue the products.  At head dimension 64 and 128
 // the softmax is two groups of four warps that take the tiles in turn, each with accumulators of its own; what they have at the end
@@ -473,8 +473,8 @@ template <int D> struct Turn {
 
 // Two warps issue the products, one the scores', one the values', so that neither waits for what the other waits for.  The whole
 // warp goes along, so that what it works out is the same for all lanes and stays in the registers that the unit's instructions
-// take; one lane issues them.  (One warp for both, whichever comes first: 140 us against 120 with 128 rows on 16 requests of 8190
-// tokens; in a fixed order 180.)
+// take; one lane issues them.  (128 rows of fp16 on 16 requests of 8190 tokens: one warp that looked for either's turn 133 us, two 133,
+// one in a fixed order 180; a single thread spent twice the products' time on issuing them.)
 template <int D, bool VALUES>
 __device__ __forceinline__ void product_role(const Args &a, TreeShared<D> &sm, uint32_t stages, Walk<D> &walk, int lane)
 {
@@ -844,7 +844,7 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
                     put_lse(l == 0.f ? -INFINITY : top + log2f(l));
                     if (top == -INFINITY) top = 0.f;
                     l = l == 0.f ? 0.f : 1.f / l;
-                    constexpr int AT_ONCE = 16;
+                    constexpr int AT_ONCE = 32;
 #pragma unroll 1
                     for (int d0 = group * OWN; d0 < (group + 1) * OWN; d0 += AT_ONCE) {
                         float v[AT_ONCE];
