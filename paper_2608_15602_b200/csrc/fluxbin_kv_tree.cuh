@@ -753,6 +753,7 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
         }
         sync_some<2, C::kSoft>();
         unit_after_sync();
+        ok = ok && !*(volatile int *)&sm.failed;                 // (the other group's waits count too)
         const bool whole = j.p0 == 0 && j.p1 == rq.pieces;
         const long long slot = share * 2 + (j.p0 == 0);
         // partial results lie element by element with the rows side by side, four elements together

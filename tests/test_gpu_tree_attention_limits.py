@@ -1,0 +1,146 @@
+"""Attention under masks and keeping at the ends of their ranges: caches whose entries lie past 32 bits, many requests, long trees, scales
+below 0, workspaces and streams that calls share."""
+import numpy as np
+import pytest
+
+from oracle import drafts as od
+from test_gpu_attention import U, at, dev, f64, normal, setup  # noqa: F401
+from test_gpu_drafts import batch_of, grow
+from test_gpu_tree_attention import check_tree, clean
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("Hq,H,D,nodes", [(8, 2, 128, 3), (32, 2, 128, 20)])
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 2.5])
+def test_any_scale(at, Hq, H, D, nodes, scale):  # noqa: F811
+    lengths = [75, nodes, 300]
+    c, table = setup(at, "int8", 16, H, D, lengths, 3)
+    parents, starts = batch_of(np.random.default_rng(1), [nodes] * 3, "tree")
+    tree = at.DraftTree(dev(parents), dev(starts), dev(lengths), nodes)
+    q = normal(8, (3 * nodes, Hq, D), "bf16", 0.5)
+    out, lse = c.attend(q, dev(table), dev(lengths), c.workspace(3, 3 * nodes, Hq, tree=True), query_start=dev(starts), scale=scale, with_lse=True, tree=tree.mask)
+    check_tree(c, q, table, lengths, starts, tree.mask.cpu().numpy(), scale, out, lse, "bf16")
+
+
+@pytest.mark.parametrize("order", [1, -1])
+@pytest.mark.parametrize("Hq,H,D,nodes", [(4, 4, 128, 2), (64, 4, 128, 9), (32, 4, 64, 12)])
+def test_a_cache_past_32_bits(at, Hq, H, D, nodes, order):  # noqa: F811
+    """Blocks that begin past 2^31 and 2^32 bytes; the others are never touched."""
+    bs = 128
+    nb = (1 << 32) // (bs * H * D) + 40
+    k, v = (torch.empty(nb, H, bs, D, dtype=torch.int8, device="cuda") for _ in range(2))
+    ks, vs = (torch.zeros(nb, H, device="cuda") for _ in range(2))
+    big = at.KVCache.wrap(k, v, ks, vs)
+    ids = np.array([[nb - 1, nb // 2 + 1, 3], [nb - 7, nb - 30, nb // 2 + 5]])[:, ::order]
+    lengths = [2 * bs + 77, 3 * bs]
+    small, table = setup(at, "int8", bs, H, D, lengths, 7)
+    for r in range(2):
+        for i in range(3):
+            for x, y in ((big.k, small.k), (big.v, small.v), (big.k_scale, small.k_scale), (big.v_scale, small.v_scale)):
+                x[ids[r, i]] = y[table[r, i]]
+    parents, starts = batch_of(np.random.default_rng(1), [nodes] * 2, "tree")
+    tree = at.DraftTree(dev(parents), dev(starts), dev(lengths), nodes)
+    q = normal(8, (2 * nodes, Hq, D), "fp16")
+    ws = big.workspace(2, 2 * nodes, Hq, tree=True)
+    a = big.attend(q, dev(ids.copy()), dev(lengths), ws, query_start=dev(starts), with_lse=True, tree=tree.mask)
+    b = small.attend(q, dev(table), dev(lengths), ws, query_start=dev(starts), with_lse=True, tree=tree.mask)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    check_tree(small, q, table, lengths, starts, tree.mask.cpu().numpy(), D ** -0.5, *b, "fp16")
+    slots = lambda t: np.concatenate([t[r, (n - nodes + np.arange(nodes)) // bs] * bs + (n - nodes + np.arange(nodes)) % bs for r, n in enumerate(lengths)])  # noqa: E731
+    path = np.tile(np.r_[np.arange(0, nodes, 2), [-1] * (nodes // 2)], 2)
+    assert slots(ids).max() * H * D > 2 ** (31 if order == 1 else 32)   # the new tokens are in the last blocks
+    big.keep(dev(slots(ids)), dev(starts), dev(path))
+    small.keep(dev(slots(table)), dev(starts), dev(path))
+    for r in range(2):
+        for i in range(3):
+            for x, y in ((big.k, small.k), (big.v, small.v), (big.k_scale, small.k_scale), (big.v_scale, small.v_scale)):
+                assert torch.equal(x[ids[r, i]], y[table[r, i]])
+
+
+@pytest.mark.parametrize("Hq,H,D,fmt", [(6, 2, 64, "int8"), (48, 2, 64, "e4m3"), (24, 1, 128, "int8")])
+def test_many_requests(at, Hq, H, D, fmt):  # noqa: F811
+    """More requests than a CTA has threads, some without new tokens, over blocks that they share."""
+    B, rng = 900, np.random.default_rng(5)
+    lengths = rng.integers(0, 60, B)
+    new = np.minimum(rng.integers(0, 5, B), lengths)
+    c, small = setup(at, fmt, 16, H, D, [64] * 8, 5)
+    clean(c)
+    table = small[rng.integers(0, 8, B)]
+    parents, starts = batch_of(rng, list(new), "tree")
+    tree = at.DraftTree(dev(parents), dev(starts), dev(lengths), 4)
+    q = normal(9, (int(new.sum()), Hq, D), "fp16")
+    out, lse = c.attend(q, dev(table), dev(lengths), c.workspace(B, len(q), Hq, tree=True), query_start=dev(starts), with_lse=True, tree=tree.mask)
+    check_tree(c, q, table, list(lengths), starts, tree.mask.cpu().numpy(), D ** -0.5, out, lse, "fp16")
+
+
+def test_a_row_of_blocks_for_all_requests_and_long_trees(at):  # noqa: F811
+    """Several trees behind one prompt whose block row is expanded; trees of several tiles of rows and many words."""
+    Hq, H, D, n, L, B = 16, 1, 64, 130, 200, 3
+    c, table = setup(at, "int8", 16, H, D, [L], 2)
+    parents, starts = batch_of(np.random.default_rng(2), [n] * B, "tree")
+    tree = at.DraftTree(dev(parents), dev(starts), dev([L] * B), n)
+    q = normal(3, (n * B, Hq, D), "bf16")
+    row = dev(table).expand(B, -1)
+    out, lse = c.attend(q, row, dev([L] * B), c.workspace(B, n * B, Hq, tree=True), query_start=dev(starts), with_lse=True, tree=tree.mask)
+    check_tree(c, q, np.repeat(table, B, 0), [L] * B, starts, tree.mask.cpu().numpy(), D ** -0.5, out, lse, "bf16")
+
+
+def test_graphs_that_share_a_workspace_and_calls_at_once(at):  # noqa: F811
+    """Two captured calls and eager ones of both kernels on one workspace, one after the other; two streams with one each."""
+    H, D, lengths = 2, 128, [3000, 40, 777]
+    c, table = setup(at, "int8", 16, H, D, lengths, 6)
+    table, ln = dev(table), dev(lengths)
+    calls = []
+    for Hq, n in ((32, 6), (4, 3)):
+        parents, starts = batch_of(np.random.default_rng(n), [n] * 3, "tree")
+        starts = dev(starts)
+        tree = at.DraftTree(dev(parents), starts, ln, n)
+        q = normal(n, (3 * n, Hq, D), "fp16")
+        calls.append(lambda ws, q=q, starts=starts, tree=tree, **kw: c.attend(q, table, ln, ws, query_start=starts, tree=tree.mask, with_lse=True, **kw))
+    ws, other = c.workspace(3, 18, 32, tree=True), c.workspace(3, 18, 32, tree=True)
+    want = [f(ws) for f in calls]
+    chain = c.attend(normal(1, (3, 32, D), "fp16"), table, ln, ws)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for f in calls:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            outs.append(f(ws))
+        graphs.append(g)
+    for _ in range(3):
+        for g, o, w in zip(graphs, outs, want):
+            o[0].zero_()
+            g.replay()
+            assert torch.equal(o[0], w[0]) and torch.equal(o[1], w[1])
+        for f, w in zip(calls, want):
+            assert torch.equal(f(ws)[0], w[0])
+        assert torch.equal(c.attend(normal(1, (3, 32, D), "fp16"), table, ln, ws), chain)
+    torch.cuda.synchronize()
+    for _ in range(5):                                     # at once, each stream with its own workspace
+        a, b = calls[0](ws), calls[0](other, stream=side)
+        d = calls[0](ws)
+        side.synchronize()
+        assert all(torch.equal(x[0], want[0][0]) for x in (a, b, d))
+
+
+def test_chains_and_stars(at):  # noqa: F811
+    """A chain sees what attend() without a mask sees; children of one token see it and themselves."""
+    Hq, H, D, n, L = 16, 1, 128, 40, 333
+    c, table = setup(at, "e4m3", 32, H, D, [L], 4)
+    q = normal(4, (n, Hq, D), "bf16")
+    ws = c.workspace(1, n, Hq, tree=True)
+    plain, plain_lse = c.attend(q, dev(table), dev([L]), ws, query_start=dev([0, n]), with_lse=True)
+    for kind in ("chain", "star"):
+        tree = at.DraftTree(dev(grow(None, n, kind)), dev([0, n]), dev([L]), n)
+        out, lse = c.attend(q, dev(table), dev([L]), ws, query_start=dev([0, n]), with_lse=True, tree=tree.mask)
+        check_tree(c, q, table, [L], [0, n], tree.mask.cpu().numpy(), D ** -0.5, out, lse, "bf16")
+        if kind == "chain":
+            # both within the bound above of the same numbers: one step of bf16 and the sums' errors
+            assert (np.abs(f64(out) - f64(plain)) <= 3 * U["bf16"] * np.abs(f64(plain)) + 2.0 ** -13 * np.abs(f64(plain)).max()).all()
+            assert torch.allclose(lse, plain_lse, rtol=0, atol=1e-4)
+        else:
+            mask, _ = od.tree(grow(None, n, kind), [0, n], [L], n)
+            assert (mask[5] == np.array([1 | 32, 0], np.int32)).all()
