@@ -887,7 +887,6 @@ __global__ void __launch_bounds__(Tree<D>::kThreads, 1) tree_attend_kernel(const
     TreeShared<D> &sm = *reinterpret_cast<TreeShared<D> *>(smem_tree + (tiles - shared_address(smem_tree)) + C::kStages * C::kStageBytes + C::kRing * C::kRingBytes);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
-    let_successor_start();
     wait_for_predecessor();
     // ---- where this CTA's part begins: a sum over the requests, each thread over a run of them
     const int per = (a.batch + C::kThreads - 1) / C::kThreads, r_lo = min(tid * per, a.batch), r_hi = min(r_lo + per, a.batch);
@@ -950,6 +949,7 @@ __global__ void __launch_bounds__(Tree<D>::kThreads, 1) tree_attend_kernel(const
     unit_before_sync();
     __syncthreads();
     unit_after_sync();
+    let_successor_start();                       // (not before: it might take some of the unit's memory and wait for this kernel with it)
     Walk<D> walk;
     walk.u = u;
     walk.u_end = u_end;

@@ -144,3 +144,49 @@ def test_chains_and_stars(at):  # noqa: F811
         else:
             mask, _ = od.tree(grow(None, n, kind), [0, n], [L], n)
             assert (mask[5] == np.array([1 | 32, 0], np.int32)).all()
+
+
+@pytest.mark.parametrize("Hq,H,D", [(32, 2, 128), (8, 2, 128), (64, 2, 64)])
+def test_a_captured_call_follows_its_inputs(at, Hq, H, D):  # noqa: F811
+    """One capture of tree and attention; lengths, starts, parents, blocks and queries change in place between replays."""
+    B, T, nodes, rng = 4, 40, 12, np.random.default_rng(6)
+    c, table = setup(at, "int8", 16, H, D, [900] * B, 6)
+    t, ln, starts, parents, q = dev(table), dev([900] * B), dev([0, 10, 20, 30, 40]), dev(np.full(T, -1)), normal(1, (T, Hq, D), "fp16")
+    ws = c.workspace(B, T, Hq, tree=True)
+
+    def step():
+        tree = at.DraftTree(parents, starts, ln, nodes)
+        return tree, *c.attend(q, t, ln, ws, query_start=starts, with_lse=True, tree=tree.mask)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tree, out, lse = step()
+    for lengths, new in (([900, 12, 7, 333], [10, 12, 7, 11]), ([0, 64, 1, 5], [0, 12, 1, 5]), ([9] * 4, [0, 0, 9, 0]), ([880, 891, 1, 900], [12, 12, 1, 12])):
+        p, s = batch_of(rng, new, "tree")
+        parents.fill_(-1)
+        parents[:len(p)] = dev(p)
+        starts.copy_(dev(s))
+        ln.copy_(dev(lengths))
+        t.copy_(dev(rng.permutation(table.reshape(-1)).reshape(table.shape)))
+        q.copy_(normal(int(s[-1]), (T, Hq, D), "fp16"))
+        out.fill_(7.0)
+        graph.replay()
+        check_tree(c, q[:s[-1]], t.cpu().numpy(), lengths, s, tree.mask.cpu().numpy(), D ** -0.5, out[:s[-1]], lse[:s[-1]], "fp16")
+        assert (out[int(s[-1]):] == 0).all()               # rows of no request
+
+
+def test_thousands_of_trees(at):  # noqa: F811
+    B, rng = 5000, np.random.default_rng(8)
+    new = rng.integers(0, 9, B)
+    parents, starts = batch_of(rng, list(new), "tree")
+    lengths = rng.integers(8, 100, B)
+    drafted, answers = rng.integers(0, 2, (2, len(parents))).astype(np.int32)
+    tree = at.DraftTree(dev(parents), dev(starts), dev(lengths), 8)
+    kept = tree.accept(dev(drafted), dev(answers))
+    mask, positions = od.tree(parents, starts, lengths, 8)
+    assert np.array_equal(tree.mask.cpu().numpy(), mask) and np.array_equal(tree.positions.cpu().numpy(), positions)
+    want = od.accept(parents, drafted, answers, starts, B, 8)
+    for got, w in zip((kept.path, kept.count, kept.answer, kept.surplus), want):
+        assert np.array_equal(got.cpu().numpy(), w)
