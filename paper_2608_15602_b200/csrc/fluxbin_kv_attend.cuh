@@ -194,15 +194,8 @@ __device__ __forceinline__ float exp2_fast(float x)         // relative error 2^
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// Copies from the cache into a lane's own places of the ring, past L1 (the cache is read once).  A lane reads back only
-// what it copied itself, so its own wait is all the order that is needed.
-template <int N> __device__ __forceinline__ void copy_ahead(uint32_t to, const unsigned char *from)
-{
-    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int PENDING> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
+// The cache comes by asynchronous copies into a lane's own places of the ring, past L1 (it is read once).  A lane reads back
+// only what it copied itself, so its own wait is all the order that is needed.
 template <int N> struct Words { uint32_t w[N]; };
 template <int N> __device__ __forceinline__ Words<N> take(uint32_t from)
 {

@@ -534,33 +534,6 @@ __device__ __forceinline__ float max_of(float x, float y, float z)
     asm("max.f32 %0, %1, %2, %3;" : "=f"(v) : "f"(x), "f"(y), "f"(z));
     return v;
 }
-// Two fp32 values at a time
-__device__ __forceinline__ unsigned long long two(float x, float y)
-{
-    unsigned long long v;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
-    return v;
-}
-__device__ __forceinline__ void apart(unsigned long long v, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
-__device__ __forceinline__ unsigned long long fma_two(unsigned long long a, unsigned long long b, unsigned long long c)
-{
-    unsigned long long v;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
-    return v;
-}
-__device__ __forceinline__ unsigned long long mul_two(unsigned long long a, unsigned long long b)
-{
-    unsigned long long v;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
-    return v;
-}
-__device__ __forceinline__ unsigned long long add_two(unsigned long long a, unsigned long long b)
-{
-    unsigned long long v;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
-    return v;
-}
-
 // ---- the softmax -----------------------------------------------------------------------------------------
 
 template <int D, int FMT, typename T>

@@ -4,14 +4,17 @@
 //     e = turn_p^-1(dy),  dx = r (w e - n mean(w e n)),  dw = sum e n     backward: reads x and dy, writes dx
 //
 // A head is held by head_dim / 16 neighbouring lanes, two pieces of eight elements each -- the two halves of eight pairs, or
-// 16 neighbours where pairs are neighbours -- so a turn is a lane's own business and a mean is a few shuffles.  A warp takes a token,
-// or a part of its heads: it forms the token's angles for itself, keeps them and the gains in registers, and has two heads of
-// each lane under way.  No barrier of a CTA: with one for each token 8191 tokens of 72 heads took 92 us.
+// 16 neighbours where pairs are neighbours -- so a turn is a lane's own business and a mean is a few shuffles.  Warps go on their own,
+// without a barrier (with one for each token 8191 tokens of 72 heads took 92 us), over equal parts of all tokens' heads; a warp forms a
+// token's angles for itself and holds them and the gains in registers.
 // The backward pass forms r again (one more sum beside mean(w e n), on the same shuffles) instead of reading it: nothing is
-// kept from the forward pass but its inputs.  Gradients of the gains are summed in registers over all that a thread sees,
-// then over the CTA, then by a second launch over the CTAs: no atomics, the same sums each time.
-// Bound by memory.
+// kept from the forward pass but its inputs.  Gradients of the gains are summed in registers over a token's heads, then in
+// shared memory over all that a thread sees, then over the CTA, then by a second launch over the CTAs: no atomics, the same sums each time.
+// Bound by memory, with instructions close behind (a value at a time instead of two 109 us for the backward pass of 8190 tokens of 80
+// heads of 128 in bf16, two 85: 503 MB, 5.9 TB/s).  8191 tokens of 72 heads forward: 53 us, 302 MB, 5.7 TB/s.
 #include "fluxbin_rotary.cuh"
+
+#include <atomic>
 
 using namespace fbd;
 
@@ -32,8 +35,8 @@ struct NormArgs {
     fluxbin_rotary_t rot;
     float eps;
     int tokens, weight_dtype;
-    unsigned splits;
-    int heads_each;
+    long long share, over;                       // rounds of a warp; so many of the first warps have one more
+    int rounds, q_rounds;                        // of a token, of its query heads
     const int *positions;
     NormSide q, k;
 };
@@ -92,17 +95,49 @@ template <bool INTER> __device__ __forceinline__ Place place_of(const fluxbin_ro
     }
     return p;
 }
-// the eight pairs of a lane's 16 elements
-template <bool INTER> __device__ __forceinline__ void turn_all(float (&v)[16], const float2 (&a)[8], float sign)
+// A lane's 16 elements are held two at a time (the unit for two fp32 values makes both in one instruction): the first elements
+// of its eight pairs, then the second ones
+typedef unsigned long long Two;
+template <bool INTER> __device__ __forceinline__ int element(const Place &p, int k)
 {
+    return INTER ? p.e0 + (k < 8 ? 2 * k : 2 * k - 15) : k < 8 ? p.e0 + k : p.e1 + k - 8;
+}
+template <typename T, bool INTER> __device__ __forceinline__ void get_all(const Piece<T> (&p)[2], Two (&v)[8])
+{
+    float f[16];
+    p[0].get(f);
+    p[1].get(f + 8);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = !INTER ? two(f[2 * i], f[2 * i + 1]) : i < 4 ? two(f[4 * i], f[4 * i + 2]) : two(f[4 * i - 15], f[4 * i - 13]);
+}
+template <typename T, bool INTER> __device__ __forceinline__ void put_all(T *to, const Place &at, const Two (&v)[8])
+{
+    float f[16], x, y;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int x = INTER ? 2 * i : i, y = INTER ? 2 * i + 1 : i + 8;
-        float f, g;
-        turn_pair(v[x], v[y], a[i].x, sign * a[i].y, f, g);
-        v[x] = f;
-        v[y] = g;
+        apart(v[i], x, y);
+        f[!INTER ? 2 * i : i < 4 ? 4 * i : 4 * i - 15] = x;
+        f[!INTER ? 2 * i + 1 : i < 4 ? 4 * i + 2 : 4 * i - 13] = y;
     }
+    Piece<T>::put(to + at.e0, f);
+    Piece<T>::put(to + at.e1, f + 8);
+}
+// (as turn_pair; BACK: the other way round)
+template <bool BACK> __device__ __forceinline__ void turn_all(Two (&v)[8], const Two (&c)[4], const Two (&s)[4])
+{
+    constexpr Two SIGNS = 0x8000000080000000ull;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const Two x = v[i], y = v[i + 4];
+        v[i] = fma_two(x, c[i], mul_two(y, BACK ? s[i] : s[i] ^ SIGNS));
+        v[i + 4] = fma_two(y, c[i], mul_two(x, BACK ? s[i] ^ SIGNS : s[i]));
+    }
+}
+__device__ __forceinline__ float sum_of_two(Two v)
+{
+    float x, y;
+    apart(v, x, y);
+    return x + y;
 }
 template <int LANES> __device__ __forceinline__ float sum_of(float v)
 {
@@ -111,17 +146,103 @@ template <int LANES> __device__ __forceinline__ float sum_of(float v)
     return v;
 }
 
-// What a warp's item is: a token and a range of its heads
-struct Item { int t, h0, h1; };
-__device__ __forceinline__ Item item_of(const NormArgs &a, unsigned i)
+// A round is ROWS heads of q or of k of a token, those that a warp's lanes hold side by side.  The rounds of all tokens are a line
+// that is cut into equal parts for all warps, so that they end together wherever tokens do (with tokens whole, 8190 over 2368 warps
+// are three or four for each, and some wait while others have a fourth of the work to do).
+// A warp goes over its part of the line by runs: rounds of one token and side.
+struct Runs {
+    long long left;                              // rounds
+    int t, first, n;                             // the run's token, its first round and how many
+    bool k;
+    __device__ __forceinline__ void begin(const NormArgs &a, long long w)
+    {
+        const long long at = w * a.share + min(w, a.over);
+        left = a.share + (w < a.over);
+        t = at >> 32 ? (int)(at / a.rounds) : (int)((unsigned)at / (unsigned)a.rounds);
+        first = (int)(at - (long long)t * a.rounds);
+        k = first >= a.q_rounds;
+        if (k) first -= a.q_rounds;
+        measure(a);
+    }
+    __device__ __forceinline__ void measure(const NormArgs &a)
+    {
+        const int whole = (k ? a.rounds - a.q_rounds : a.q_rounds) - first;
+        n = left < whole ? (int)left : whole;
+        left -= n;
+    }
+    // the next one (n == 0: there is none); whether a token begins
+    __device__ __forceinline__ bool next(const NormArgs &a)
+    {
+        const bool both = !k && a.rounds > a.q_rounds;
+        k = both || a.q_rounds == 0;
+        t += !both;
+        first = 0;
+        measure(a);
+        return !both;
+    }
+};
+// What a round reads is brought by asynchronous copies, each thread's to places that only it reads again, rounds ahead
+template <typename T, int TENSORS> struct Ahead {
+    static constexpr int kPieces = TENSORS * (int)sizeof(T);     // of 16 bytes
+    static constexpr int kStages = sizeof(T) == 2 ? 7 - 2 * TENSORS : 4 - TENSORS;
+    static constexpr int kBytes = kStages * kPieces * kThreads * 16 + (TENSORS == 2 ? 2 * 8 * kThreads * (int)sizeof(Two) : 0);
+};
+template <typename T, int TENSORS, int ROWS> struct Bringer {
+    using A = Ahead<T, TENSORS>;
+    Runs runs;
+    const unsigned char *from[TENSORS];
+    long long step[TENSORS];
+    int heads;                                   // from this row on
+    uint32_t base, to;
+    __device__ __forceinline__ void begin(const NormArgs &a, const Runs &r, const uint4 *places, int row)
+    {
+        runs = r;
+        base = to = (uint32_t)__cvta_generic_to_shared(places);
+        aim(a, row);
+    }
+    __device__ __forceinline__ void aim(const NormArgs &a, int row)
+    {
+        const NormSide &S = runs.k ? a.k : a.q;
+        const int h = runs.first * ROWS + row;
+        heads = S.heads - h;
+        from[0] = (const unsigned char *)((const T *)S.x + runs.t * S.x_token + h * S.x_head);
+        step[0] = S.x_head * (ROWS * (int)sizeof(T));
+        if constexpr (TENSORS == 2) {
+            from[1] = (const unsigned char *)((const T *)S.grad + runs.t * S.g_token + h * S.g_head);
+            step[1] = S.g_head * (ROWS * (int)sizeof(T));
+        }
+    }
+    // a round's pieces at e0 and e1
+    __device__ __forceinline__ void bring(const NormArgs &a, const Place &at, int row)
+    {
+        constexpr int N = sizeof(T) / 2;
+        if (runs.n > 0) {
+            if (at.there && heads > 0) {
+#pragma unroll
+                for (int i = 0; i < TENSORS; ++i)
+#pragma unroll
+                    for (int k = 0; k < 2 * N; ++k)
+                        copy_ahead<16>(to + (i * 2 * N + k) * kThreads * 16, from[i] + (k < N ? at.e0 : at.e1) * (int)sizeof(T) + k % N * 16);
+            }
+#pragma unroll
+            for (int i = 0; i < TENSORS; ++i) from[i] += step[i];
+            heads -= ROWS;
+            if (--runs.n == 0 && runs.left > 0) {
+                runs.next(a);
+                aim(a, row);
+            }
+        }
+        copies_commit();
+        to = to == base + (A::kStages - 1) * A::kPieces * kThreads * 16 ? base : to + A::kPieces * kThreads * 16;
+    }
+};
+template <typename T> __device__ __forceinline__ void take_pieces(const uint4 *from, Piece<T> (&p)[2])
 {
-    Item x;
-    x.t = (int)(i / a.splits);
-    x.h0 = (int)(i % a.splits) * a.heads_each;
-    x.h1 = min(x.h0 + a.heads_each, a.q.heads + a.k.heads);
-    return x;
+    constexpr int N = sizeof(T) / 2;
+#pragma unroll
+    for (int i = 0; i < 2 * N; ++i) p[i / N].w[i % N] = from[i * kThreads];
 }
-// Gains and a token's angles as the lanes want them: 16 values of each lane, four at a time, side by side
+// Gains and a token's angles (cosines, then sines) as the lanes want them: 16 values of each lane, four at a time, side by side
 template <int LANES> struct Lanes {
     float4 weight[2][4][LANES];
     float4 angles[kThreads / 32][4][LANES];
@@ -131,186 +252,194 @@ template <bool INTER, int LANES> __device__ __forceinline__ void keep_weights(co
     for (int i = threadIdx.x; i < 2 * LANES * 16; i += kThreads) {
         const int side = i / (LANES * 16), u = i / 16 % LANES, k = i % 16;
         const Place p = place_of<INTER>(a.rot, u);
-        reinterpret_cast<float *>(&sm.weight[side][k / 4][u])[k % 4] = p.there ? gain(side ? a.k.weight : a.q.weight, a.weight_dtype, k < 8 ? p.e0 + k : p.e1 + k - 8) : 0.f;
+        reinterpret_cast<float *>(&sm.weight[side][k / 4][u])[k % 4] = p.there ? gain(side ? a.k.weight : a.q.weight, a.weight_dtype, element<INTER>(p, k)) : 0.f;
     }
     __syncthreads();
 }
-// f(element, gain) for a lane's 16 elements, gains from shared memory each time: registers are what limits the bytes under way
-template <int LANES, typename F> __device__ __forceinline__ void with_weights(const Lanes<LANES> &sm, int side, int u, F f)
+template <int LANES> __device__ __forceinline__ void take_weights(const Lanes<LANES> &sm, int side, int u, Two (&w)[8])
 {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const float4 w = sm.weight[side][k][u];
-        f(4 * k, w.x);
-        f(4 * k + 1, w.y);
-        f(4 * k + 2, w.z);
-        f(4 * k + 3, w.w);
+        const float4 x = sm.weight[side][k][u];
+        w[2 * k] = two(x.x, x.y);
+        w[2 * k + 1] = two(x.z, x.w);
     }
 }
-template <int LANES> __device__ __forceinline__ void lane_angles(const NormArgs &a, Lanes<LANES> &sm, int position, int warp, int lane, float2 (&cs)[8])
+template <int LANES> __device__ __forceinline__ void lane_angles(const NormArgs &a, Lanes<LANES> &sm, int position, int warp, int lane, Two (&c)[4], Two (&s)[4])
 {
     __syncwarp();                                // the last token's have been read
+    float *to = reinterpret_cast<float *>(sm.angles[warp]);
     for (int p = lane; p < a.rot.rotary_dim / 2; p += 32) {
-        float2 x;
-        pair_angle(position, a.rot.d_turns[p], a.rot.magnitude, 1.f, x.x, x.y);
-        reinterpret_cast<float2 *>(&sm.angles[warp][p % 8 / 2][p / 8])[p & 1] = x;
+        const int at = (p % 8 / 4 * LANES + p / 8) * 4 + p % 4;
+        pair_angle(position, a.rot.d_turns[p], a.rot.magnitude, 1.f, to[at], to[at + 2 * LANES * 4]);
     }
     __syncwarp();
 #pragma unroll
-    for (int k = 0; k < 4; ++k) *reinterpret_cast<float4 *>(cs + 2 * k) = sm.angles[warp][k][lane % LANES];
+    for (int k = 0; k < 2; ++k) {
+        const float4 x = sm.angles[warp][k][lane % LANES], y = sm.angles[warp][k + 2][lane % LANES];
+        c[2 * k] = two(x.x, x.y);
+        c[2 * k + 1] = two(x.z, x.w);
+        s[2 * k] = two(y.x, y.y);
+        s[2 * k + 1] = two(y.z, y.w);
+    }
 }
 
 template <typename T, bool INTER, int LANES>
-__global__ void __launch_bounds__(kThreads, 3) norm_kernel(const __grid_constant__ NormArgs a)
+__global__ void __launch_bounds__(kThreads, 2) norm_kernel(const __grid_constant__ NormArgs a)
 {
-    constexpr int ROWS = 32 / LANES, AHEAD = sizeof(T) == 4 ? 1 : 2;
+    using A = Ahead<T, 1>;
+    constexpr int ROWS = 32 / LANES;
     __shared__ Lanes<LANES> sm;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, row = lane / LANES, u = lane % LANES;
+    extern __shared__ uint4 brought[];           // [stage][piece][thread]
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32, row = lane / LANES, u = lane % LANES;
     const Place at = place_of<INTER>(a.rot, u);
     const float inverse_dim = 1.f / a.rot.head_dim;
     let_successor_start();
     wait_for_predecessor();
-    keep_weights<INTER, LANES>(a, sm);
-    const unsigned items = (unsigned)a.tokens * a.splits, step = gridDim.x * (kThreads / 32);          // (more than 2^31 tokens are not split)
-    for (unsigned i = blockIdx.x * (kThreads / 32) + warp; i < items; i += step) {
-        const Item item = item_of(a, i);
-        float2 cs[8];
-        bool formed = false;
+    Runs now;
+    now.begin(a, (long long)blockIdx.x * (kThreads / 32) + warp);
+    Bringer<T, 1, ROWS> ahead;
+    ahead.begin(a, now, brought + tid, row);
 #pragma unroll 1
-        for (int side = 0; side < 2; ++side) {
-            const NormSide &S = side ? a.k : a.q;
-            const int lo = max(item.h0 - (side ? a.q.heads : 0), 0), hi = min(item.h1 - (side ? a.q.heads : 0), S.heads);
-            if (lo >= hi) continue;
-            const T *x = (const T *)S.x + item.t * S.x_token + (long long)(lo + row) * S.x_head;
-            T *y = (T *)S.y + item.t * S.y_token + (long long)(lo + row) * S.y_head;
-            Piece<T> p[AHEAD][2];
-            auto load = [&](int h, Piece<T> (&to)[2]) {
-                if (at.there && h + row < hi) {
-                    to[0].load(x + at.e0);
-                    to[1].load(x + at.e1);
-                }
-                x += ROWS * S.x_head;
-            };
+    for (int i = 0; i < A::kStages - 1; ++i) ahead.bring(a, at, row);
+    int position = now.n > 0 ? a.positions[now.t] : 0;
+    keep_weights<INTER, LANES>(a, sm);
+    Two c[4], s[4];
+    int stage = 0;
+    for (bool begins = true; now.n > 0; begins = now.next(a)) {
+        if (begins) {
+            lane_angles<LANES>(a, sm, position, warp, lane, c, s);
+            if (now.t + 1 < a.tokens) position = a.positions[now.t + 1];
+        }
+        const NormSide &S = now.k ? a.k : a.q;
+        int h = now.first * ROWS + row;
+        T *y = (T *)S.y + now.t * S.y_token + h * S.y_head;
+        const long long y_step = S.y_head * ROWS;
+        const int heads = S.heads;
+        Two w[8];
+        take_weights<LANES>(sm, now.k, u, w);
+#pragma unroll 1
+        for (int i = now.n; i > 0; --i, h += ROWS, y += y_step) {
+            Two v[8], squares = 0;
+            copies_wait<A::kStages - 2>();
+            {
+                Piece<T> p[2];
+                take_pieces(brought + stage * A::kPieces * kThreads + tid, p);
+                get_all<T, INTER>(p, v);
+            }
+            stage = stage == A::kStages - 1 ? 0 : stage + 1;
+            ahead.bring(a, at, row);
+            const bool mine = at.there && h < heads;
+            if (mine) {
 #pragma unroll
-            for (int j = 0; j < AHEAD; ++j) load(lo + j * ROWS, p[j]);
-            if (!formed) lane_angles<LANES>(a, sm, a.positions[item.t], warp, lane, cs);         // (while the first heads are on their way)
-            formed = true;
-            // (every lane goes as many rounds: they meet in the shuffles)
-            for (int h0 = lo; h0 < hi; h0 += AHEAD * ROWS)
+                for (int k = 0; k < 8; ++k) squares = fma_two(v[k], v[k], squares);
+            }
+            const float r = __frsqrt_rn(fmaf(sum_of<LANES>(sum_of_two(squares)), inverse_dim, a.eps));
+            if (mine) {
+                const Two r2 = two(r, r);
 #pragma unroll
-                for (int j = 0; j < AHEAD; ++j, y += ROWS * S.y_head) {
-                    const int h = h0 + j * ROWS;
-                    if (h >= hi) break;
-                    const bool mine = at.there && h + row < hi;
-                    float v[16], squares = 0.f;
-                    p[j][0].get(v);
-                    p[j][1].get(v + 8);
-                    load(h + AHEAD * ROWS, p[j]);
-                    if (mine) {
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) squares = fmaf(v[k], v[k], squares);
-                    }
-                    const float r = __frsqrt_rn(fmaf(sum_of<LANES>(squares), inverse_dim, a.eps));
-                    if (!mine) continue;
-                    with_weights<LANES>(sm, side, u, [&](int k, float w) { v[k] = v[k] * r * w; });
-                    if (at.turns) turn_all<INTER>(v, cs, 1.f);
-                    Piece<T>::put(y + at.e0, v);
-                    Piece<T>::put(y + at.e1, v + 8);
-                }
+                for (int k = 0; k < 8; ++k) v[k] = mul_two(mul_two(v[k], r2), w[k]);
+                if (at.turns) turn_all<false>(v, c, s);
+                put_all<T, INTER>(y, at, v);
+            }
         }
     }
+    copies_wait<0>();
 }
 
 template <typename T, bool INTER, int LANES>
 __global__ void __launch_bounds__(kThreads, 2) norm_backward_kernel(const __grid_constant__ NormArgs a)
 {
+    using A = Ahead<T, 2>;
     constexpr int ROWS = 32 / LANES;
-    __shared__ union { Lanes<LANES> lanes; float sums[16][kThreads]; } sm;
+    __shared__ Lanes<LANES> sm;
+    extern __shared__ uint4 brought[];           // [stage][piece][thread], then the sums
     const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32, row = lane / LANES, u = lane % LANES, D = a.rot.head_dim;
     const Place at = place_of<INTER>(a.rot, u);
     const float inverse_dim = 1.f / D;
     let_successor_start();
     wait_for_predecessor();
-    keep_weights<INTER, LANES>(a, sm.lanes);
-    float dw[2][16];
+    Runs now;
+    now.begin(a, (long long)blockIdx.x * (kThreads / 32) + warp);
+    Bringer<T, 2, ROWS> ahead;
+    ahead.begin(a, now, brought + tid, row);
+#pragma unroll 1
+    for (int i = 0; i < A::kStages - 1; ++i) ahead.bring(a, at, row);
+    int position = now.n > 0 ? a.positions[now.t] : 0;
+    keep_weights<INTER, LANES>(a, sm);
+    // sums for the gradients of the gains: a run's in registers, all runs' in places of this thread
+    Two *sums = reinterpret_cast<Two *>(brought + A::kStages * A::kPieces * kThreads) + tid;           // [side][pair][thread]
 #pragma unroll
-    for (int i = 0; i < 16; ++i) dw[0][i] = dw[1][i] = 0.f;
-    const unsigned items = (unsigned)a.tokens * a.splits, step = gridDim.x * (kThreads / 32);          // (more than 2^31 tokens are not split)
-    for (unsigned i = blockIdx.x * (kThreads / 32) + warp; i < items; i += step) {
-        const Item item = item_of(a, i);
-        float2 cs[8];
-        bool formed = false;
+    for (int i = 0; i < 16; ++i) sums[i * kThreads] = 0;
+    Two c[4], s[4];
+    int stage = 0;
+    for (bool begins = true; now.n > 0; begins = now.next(a)) {
+        if (begins) {
+            lane_angles<LANES>(a, sm, position, warp, lane, c, s);
+            if (now.t + 1 < a.tokens) position = a.positions[now.t + 1];
+        }
+        const NormSide &S = now.k ? a.k : a.q;
+        int h = now.first * ROWS + row;
+        T *dx = (T *)S.y + now.t * S.y_token + h * S.y_head;
+        const long long dx_step = S.y_head * ROWS;
+        const int heads = S.heads;
+        const bool write = S.y != nullptr;
+        Two w[8], dw[8];
+        take_weights<LANES>(sm, now.k, u, w);
 #pragma unroll
-        for (int side = 0; side < 2; ++side) {
-            const NormSide &S = side ? a.k : a.q;
-            const int lo = max(item.h0 - (side ? a.q.heads : 0), 0), hi = min(item.h1 - (side ? a.q.heads : 0), S.heads);
-            if (lo >= hi) continue;
-            const T *x = (const T *)S.x + item.t * S.x_token + (long long)(lo + row) * S.x_head;
-            const T *g = (const T *)S.grad + item.t * S.g_token + (long long)(lo + row) * S.g_head;
-            T *dx = S.y ? (T *)S.y + item.t * S.y_token + (long long)(lo + row) * S.y_head : nullptr;
-            Piece<T> p[4];
-            auto load = [&](int h) {
-                if (at.there && h + row < hi) {
-                    p[0].load(x + at.e0);
-                    p[1].load(x + at.e1);
-                    p[2].load(g + at.e0);
-                    p[3].load(g + at.e1);
+        for (int k = 0; k < 8; ++k) dw[k] = 0;
+#pragma unroll 1
+        for (int i = now.n; i > 0; --i, h += ROWS, dx += dx_step) {
+            const bool mine = at.there && h < heads;
+            Two v[8], e[8], squares = 0, both = 0;
+            copies_wait<A::kStages - 2>();
+            {
+                Piece<T> p[2];
+                take_pieces(brought + stage * A::kPieces * kThreads + tid, p);
+                get_all<T, INTER>(p, v);
+                take_pieces(brought + (stage * A::kPieces + A::kPieces / 2) * kThreads + tid, p);
+                get_all<T, INTER>(p, e);
+            }
+            stage = stage == A::kStages - 1 ? 0 : stage + 1;
+            ahead.bring(a, at, row);
+            if (mine) {
+                if (at.turns) turn_all<true>(e, c, s);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    squares = fma_two(v[k], v[k], squares);
+                    both = fma_two(mul_two(w[k], e[k]), v[k], both);
                 }
-            };
-            load(lo);
-            if (!formed) lane_angles<LANES>(a, sm.lanes, a.positions[item.t], warp, lane, cs);
-            formed = true;
-            for (int h = lo; h < hi; h += ROWS) {
-                const bool mine = at.there && h + row < hi;
-                float v[16], e[16], squares = 0.f, both = 0.f;
-                p[0].get(v);
-                p[1].get(v + 8);
-                p[2].get(e);
-                p[3].get(e + 8);
-                x += ROWS * S.x_head;
-                g += ROWS * S.g_head;
-                if (sizeof(T) == 2) load(h + ROWS);              // (registers for the next ones)
-                if (mine) {
-                    if (at.turns) turn_all<INTER>(e, cs, -1.f);
-                    with_weights<LANES>(sm.lanes, side, u, [&](int k, float w) {
-                        squares = fmaf(v[k], v[k], squares);
-                        both = fmaf(w * e[k], v[k], both);
-                    });
+            }
+            const float r = __frsqrt_rn(fmaf(sum_of<LANES>(sum_of_two(squares)), inverse_dim, a.eps)), mean = sum_of<LANES>(sum_of_two(both)) * r * inverse_dim;
+            if (mine) {
+                const Two r2 = two(r, r), minus_mean = two(-mean, -mean);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    v[k] = mul_two(v[k], r2);
+                    dw[k] = fma_two(e[k], v[k], dw[k]);
+                    v[k] = mul_two(r2, fma_two(v[k], minus_mean, mul_two(w[k], e[k])));
                 }
-                squares = sum_of<LANES>(squares);
-                both = sum_of<LANES>(both);
-                if (mine) {
-                    const float r = __frsqrt_rn(fmaf(squares, inverse_dim, a.eps)), mean = both * r * inverse_dim;
-                    with_weights<LANES>(sm.lanes, side, u, [&](int k, float w) {
-                        const float n = v[k] * r;
-                        dw[side][k] = fmaf(e[k], n, dw[side][k]);
-                        v[k] = r * fmaf(-n, mean, w * e[k]);
-                    });
-                    if (dx) {
-                        Piece<T>::put(dx + at.e0, v);
-                        Piece<T>::put(dx + at.e1, v + 8);
-                    }
-                }
-                if (dx) dx += ROWS * S.y_head;
-                if (sizeof(T) != 2) load(h + ROWS);
+                if (write) put_all<T, INTER>(dx, at, v);
             }
         }
-    }
+        Two *to = sums + now.k * 8 * kThreads;
 #pragma unroll
+        for (int k = 0; k < 8; ++k) to[k * kThreads] = add_two(to[k * kThreads], dw[k]);
+    }
+    copies_wait<0>();
+    __syncthreads();
+#pragma unroll 1
     for (int side = 0; side < 2; ++side) {
         float *to = side ? a.k.part : a.q.part;
-        if (!to) continue;                       // (the same for every thread)
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sm.sums[i][tid] = dw[side][i];
-        __syncthreads();
+        if (!to) continue;
         for (int j = tid; j < LANES * 16; j += kThreads) {
             const int lane_of = j / 16, i = j % 16;
             const Place p = place_of<INTER>(a.rot, lane_of);
             if (!p.there) continue;
+            const float *from = reinterpret_cast<const float *>(sums - tid + (side * 8 + i / 2) * kThreads + lane_of) + i % 2;
             float s = 0.f;
-            for (int k = 0; k < kThreads / LANES; ++k) s += sm.sums[i][k * LANES + lane_of];
-            to[(long long)blockIdx.x * D + (i < 8 ? p.e0 + i : p.e1 + i - 8)] = s;
+            for (int k = 0; k < kThreads / LANES; ++k) s += from[2 * k * LANES];
+            to[(long long)blockIdx.x * D + element<INTER>(p, i)] = s;
         }
     }
 }
@@ -459,21 +588,34 @@ template <typename T> bool wide(const NormArgs &a, bool backward)
     return true;
 }
 
+template <typename K> cudaError_t run_ahead(K kernel, std::atomic<bool> *opted, int ctas, int bytes, cudaStream_t s, const NormArgs &a)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= fb::kMaxDevices) return cudaErrorInvalidDevice;
+    if (!opted[dev].load(std::memory_order_relaxed)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != cudaSuccess) return e;
+        opted[dev].store(true, std::memory_order_relaxed);
+    }
+    return launch(kernel, dim3((unsigned)ctas), kThreads, (size_t)bytes, s, a);
+}
 template <typename T, bool INTER, int LANES> cudaError_t run_wide(NormArgs a, bool backward, int &parts, cudaStream_t s)
 {
-    // Resident warps go over tokens.  Tokens are split into parts of their heads until there are three for every warp, but no part is
-    // less than four rounds of heads, since the angles are formed for each; fewer tokens than warps are split until every warp has one.
     constexpr int ROWS = 32 / LANES, WARPS = kThreads / 32;
-    const long long heads = a.q.heads + a.k.heads, rounds = (heads + ROWS - 1) / ROWS, ctas = 148 * (backward ? 2 : 3), warps = ctas * WARPS;
-    long long splits = (3 * warps + a.tokens - 1) / a.tokens, most = rounds / 4 > 1 ? rounds / 4 : 1;
-    if (splits > most) splits = most;
-    if (a.tokens * splits < warps) splits = (warps + a.tokens - 1) / a.tokens < rounds ? (warps + a.tokens - 1) / a.tokens : rounds;
-    a.heads_each = (int)((rounds + splits - 1) / splits) * ROWS;
-    a.splits = (unsigned)((heads + a.heads_each - 1) / a.heads_each);
-    const long long items = (long long)a.tokens * a.splits, need = (items + WARPS - 1) / WARPS;
+    a.q_rounds = (a.q.heads + ROWS - 1) / ROWS;
+    a.rounds = a.q_rounds + (a.k.heads + ROWS - 1) / ROWS;
+    // Two CTAs an SM are resident; the forward pass cuts the line finer, so that SMs that get more of the memory's rate do more of it (resident
+    // CTAs once, twice, three, four times: 8191 tokens of 72 heads 54.5, 53.1, 54.0, 56.4 us; the backward pass, whose
+    // sums cost each CTA something, 8190 tokens of 80 heads with the forward one: 149, 153, 160, 160)
+    const long long total = (long long)a.tokens * a.rounds, ctas = 148 * 2 * (backward ? 1 : 2), need = (total + WARPS - 1) / WARPS;
     parts = (int)(need < ctas ? need : ctas);
-    const dim3 grid((unsigned)parts);
-    return backward ? launch(norm_backward_kernel<T, INTER, LANES>, grid, kThreads, 0, s, a) : launch(norm_kernel<T, INTER, LANES>, grid, kThreads, 0, s, a);
+    a.share = total / (parts * WARPS);
+    a.over = total - a.share * parts * WARPS;
+    static std::atomic<bool> opted[2][fb::kMaxDevices];
+    if (backward) return run_ahead(norm_backward_kernel<T, INTER, LANES>, opted[1], parts, Ahead<T, 2>::kBytes, s, a);
+    return run_ahead(norm_kernel<T, INTER, LANES>, opted[0], parts, Ahead<T, 1>::kBytes, s, a);
 }
 template <typename T, bool INTER> cudaError_t run_lanes(const NormArgs &a, bool backward, int &parts, cudaStream_t s)
 {
