@@ -716,7 +716,8 @@ fluxbin_status_t fluxbin_kv_attend_tree(const fluxbin_kv_cache_t *cache, int32_t
  *   d_path      DEVICE int32 [tokens], out: places among the request's new tokens in the path's order, from d_query_start[r] on,
  *               then -1; -1 for tokens that are no request's
  *   d_count, d_answer, d_surplus   DEVICE int32 [batch], out: tokens of the path; the answer at its end, which comes next (-1
- *               without new tokens); the path's tokens less the new ones, which is what fluxbin_kv_advance is to drop
+ *               without new tokens); the path's tokens less the new ones, which is what fluxbin_kv_advance is to drop (of
+ *               requests that were granted their blocks: the tokens of the others were not added, so nothing of them is)
  * Only the first `nodes` new tokens of a request are looked at.  The rest as fluxbin_draft_tree.  Errors: as there.
  */
 fluxbin_status_t fluxbin_draft_accept(int32_t batch, int32_t tokens, int32_t nodes, const int32_t *d_query_start, const int32_t *d_parents,

@@ -22,7 +22,7 @@ that are turned already.  A step that checks a tree of drafted tokens at once:
     out = cache.attend(q, tables.table, step.lengths, ws, query_start=step.query_start, tree=tree.mask)
     kept = tree.accept(drafted, answers)                                  # the path that the model itself would have answered
     cache.keep(step.slots, step.query_start, kept.path)                   # its entries move to the step's first slots, in every layer
-    step = tables.advance(step.lengths, kept.surplus, step.num_free, 0)   # and the others are dropped
+    step = tables.advance(step.lengths, kept.surplus * step.granted, step.num_free, 0)    # and the others are dropped
 
 Rotary.apply and NormedRotary.apply carry gradients.  The other calls are those of answering: their results have none.
 """
@@ -505,7 +505,8 @@ class DraftTree:
         """fluxbin_draft_accept: the path of each request's tree that the model itself would have answered.  `drafted` int32
         [tokens]: the new tokens; `answers` int32 [tokens]: what the model answered at each.  Returns `path` int32 [tokens] (places
         among the request's new tokens, then -1: for KVCache.keep), and int32 [batch] `count`, tokens of the path, `answer`, what
-        comes after it, `surplus`, what is to be dropped (as BlockTables.advance takes it)."""
+        comes after it, `surplus`, what is to be dropped (as BlockTables.advance takes it; nothing of requests that were not granted
+        their blocks, whose tokens were not added: times the step's `granted`)."""
         n, B = self.parents.shape[0], self.query_start.shape[0] - 1
         inputs = (_int32(self.query_start, B + 1, "query_start"), _int32(self.parents, n, "parents"), _int32(drafted, n, "drafted"), _int32(answers, n, "answers"))
         path = _made(stream, lambda: torch.empty_like(self.parents))

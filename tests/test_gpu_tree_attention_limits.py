@@ -190,3 +190,31 @@ def test_thousands_of_trees(at):  # noqa: F811
     want = od.accept(parents, drafted, answers, starts, B, 8)
     for got, w in zip((kept.path, kept.count, kept.answer, kept.surplus), want):
         assert np.array_equal(got.cpu().numpy(), w)
+
+
+def test_a_request_without_blocks_keeps_what_it_has(at):  # noqa: F811
+    """A step in which one request is refused: its cached tokens, its length and its blocks stay, the others go on."""
+    B, n, nb = 3, 20, 8
+    ints = lambda v: dev(np.asarray(v))  # noqa: E731
+    cache, tables = at.KVCache(nb, 16, 2, 64), at.BlockTables.empty(B, 4, nb, 16)
+    step = tables.advance(ints([0] * B), ints([30, 33, 16]), ints([nb]), 79)          # 2 + 3 + 1 blocks
+    k, v = normal(1, (79, 2, 64), "fp16"), normal(2, (79, 2, 64), "fp16")
+    cache.append(k, v, step.slots)
+    old = [t.clone() for t in cache.read(step.slots)]
+    slots = step.slots.clone()
+    step = tables.advance(step.lengths, ints([n] * B), step.num_free, B * n)           # 2 + 1 + 2 wanted, 2 there
+    granted = step.granted.cpu().numpy()
+    assert granted.tolist().count(0) >= 1 and granted.tolist().count(1) >= 1
+    parents = np.tile(np.r_[-1, np.arange(n - 1) // 2], B)
+    tree = at.DraftTree(ints(parents), step.query_start, step.lengths, n)
+    cache.append(normal(3, (B * n, 2, 64), "fp16"), normal(4, (B * n, 2, 64), "fp16"), step.slots)
+    cache.attend(normal(5, (B * n, 8, 64), "fp16"), tables.table, step.lengths, cache.workspace(B, B * n, 8, tree=True), query_start=step.query_start, tree=tree.mask)
+    kept = tree.accept(ints([0] * B * n), ints([0] * B * n))
+    cache.keep(step.slots, step.query_start, kept.path)
+    before = [30, 33, 16]
+    after = tables.advance(step.lengths, kept.surplus * step.granted, step.num_free, 0)
+    count = kept.count.cpu().numpy()
+    assert after.lengths.tolist() == [b + c * g for b, c, g in zip(before, count, granted)]
+    refused = torch.from_numpy(np.repeat(granted == 0, before)).cuda()
+    for x, y in zip(old, cache.read(slots)):
+        assert torch.equal(x[refused], y[refused])
