@@ -625,8 +625,8 @@ fluxbin_status_t fluxbin_kv_read(const fluxbin_kv_cache_t *cache, int32_t dtype,
  * to 2^-39 of it.  Results do not depend on timing: sums are joined in a fixed order (which depends on the lengths of the whole
  * batch).
  * d_workspace: fluxbin_kv_attend_workspace_size bytes (13 MB at head_dim 128: the partial results of jobs that several CTAs
- * work at; it depends on head_dim alone, so one serves all calls), zeroed once with fluxbin_workspace_init; calls leave its
- * counters zeroed, and calls that share one must be ordered on a stream.
+ * work at; it depends on head_dim alone, and one of the largest head_dim serves the calls of every one), zeroed once with
+ * fluxbin_workspace_init; calls leave its counters zeroed, and calls that share one must be ordered on a stream.
  * Errors: as fluxbin_kv_validate; NULL, RANGE (q_heads no multiple of kv_heads, tokens != batch without query_start, 2^31
  * rows or more for a key head),
  * UNSUPPORTED (dtype), ALIGNMENT, BUFFER_TOO_SMALL, CUDA.
@@ -695,7 +695,7 @@ fluxbin_status_t fluxbin_draft_tree(int32_t batch, int32_t tokens, int32_t nodes
  *                 it sees its request's j-th new token (of its count in d_query_start; later ones and those past the words are
  *                 not seen).  fluxbin_draft_tree makes them; any other masks will do.
  *   d_workspace   fluxbin_kv_attend_tree_workspace_size bytes, zeroed once with fluxbin_workspace_init; it serves
- *                 fluxbin_kv_attend too, and calls that share one must be ordered on a stream.
+ *                 fluxbin_kv_attend too, and smaller head dimensions; calls that share one must be ordered on a stream.
  * All else as fluxbin_kv_attend.  Errors: as there.
  */
 size_t fluxbin_kv_attend_tree_workspace_size(int32_t batch, int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim);

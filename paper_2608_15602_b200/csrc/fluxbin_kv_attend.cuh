@@ -870,7 +870,10 @@ template <typename T, bool TREE> cudaError_t run_dim(const Args &a, cudaStream_t
     return a.c.head_dim == 64 ? run_format<64, T, TREE>(a, s) : a.c.head_dim == 128 ? run_format<128, T, TREE>(a, s) : run_format<256, T, TREE>(a, s);
 }
 
-constexpr size_t kCounterBytes = ((1 + kMaxShares) * sizeof(unsigned) + 255) / 256 * 256;
+// A workspace begins with the counters of this kernel, then those of the one for many rows, at the same places for every head
+// dimension; partial results of either come behind both.  So a workspace that is large enough serves calls of every kind: none writes
+// where another one looks for zeros.
+constexpr size_t kManyCountersAt = ((1 + kMaxShares) * sizeof(unsigned) + 255) / 256 * 256, kCounterBytes = kManyCountersAt + (kMaxSms * sizeof(unsigned) + 255) / 256 * 256;
 // the most rows that partial results of a launch take: those of the CTAs on an SM, two shares each, two parts a share
 constexpr size_t kPartRows = (size_t)kMaxSms * 40 * 2 * 2, kLseBytes = kPartRows * sizeof(float);
 

@@ -8,18 +8,11 @@ namespace {
 // 148 and 82; 256 16 rows 56 and 77, 32 rows 87 and 88, 128 rows 293 and 93.
 int few_rows(int head_dim) { return head_dim == 128 ? 16 : 32; }
 
-// A workspace of both kernels: the counters of the one for few rows, the partial results of either (of one call at a time), the
-// counters of this one -- behind all that the other writes, since each finds its own zeroed.
-size_t counters_at(int head_dim)
-{
-    const size_t few = kCounterBytes + kLseBytes * (1 + (size_t)head_dim), many = kCounterBytes + kTreeLseBytes * (1 + (size_t)head_dim);
-    return few > many ? few : many;
-}
 template <typename T> cudaError_t run_type(Args a, char *workspace, cudaStream_t s)
 {
     const long long rows = (long long)(a.q_heads / a.c.kv_heads) * ((a.tokens + a.batch - 1) / a.batch);
     if (rows <= few_rows(a.c.head_dim)) return run_dim<T, true>(a, s);
-    a.arrived = (unsigned *)(workspace + counters_at(a.c.head_dim));
+    a.arrived = (unsigned *)(workspace + kManyCountersAt);
     a.partial_lse = (float *)(workspace + kCounterBytes);
     a.partial = (float *)(workspace + kCounterBytes + kTreeLseBytes);
     const bool bf16 = !std::is_same<T, __half>::value;
@@ -31,7 +24,7 @@ template <typename T> cudaError_t run_type(Args a, char *workspace, cudaStream_t
 extern "C" size_t fluxbin_kv_attend_tree_workspace_size(int32_t batch, int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim)
 {
     if (fluxbin_kv_attend_workspace_size(batch, tokens, q_heads, kv_heads, head_dim) == 0) return 0;
-    return counters_at(head_dim) + kTreeCounterBytes;
+    return kCounterBytes + (kLseBytes > kTreeLseBytes ? kLseBytes : kTreeLseBytes) * (1 + (size_t)head_dim);
 }
 
 extern "C" fluxbin_status_t fluxbin_kv_attend_tree(const fluxbin_kv_cache_t *cache, int32_t dtype, int32_t batch, int32_t tokens,

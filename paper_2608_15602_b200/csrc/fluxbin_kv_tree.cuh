@@ -946,7 +946,7 @@ __global__ void __launch_bounds__(Tree<D>::kThreads, 1) tree_attend_kernel(const
 }
 
 // CTAs of a launch, and what their partial results take: two parts each
-constexpr size_t kTreeCounterBytes = (kMaxSms * sizeof(unsigned) + 255) / 256 * 256, kTreePartRows = (size_t)kMaxSms * 2 * kRows, kTreeLseBytes = kTreePartRows * sizeof(float);
+constexpr size_t kTreePartRows = (size_t)kMaxSms * 2 * kRows, kTreeLseBytes = kTreePartRows * sizeof(float);
 
 template <int D, int FMT, typename T> cudaError_t run_tree(const Args &a, cudaStream_t s)
 {
