@@ -729,7 +729,8 @@ fluxbin_status_t fluxbin_draft_accept(int32_t batch, int32_t tokens, int32_t nod
  * stored at slot d_slots[query_start[r] + j], as fluxbin_kv_append stores new keys and values (tokens of the path that are where
  * they belong already are left as they are, with the scale of their block, unless a moved entry makes that grow).
  *   d_slots   DEVICE int32 [tokens]: the slots the new tokens were appended at, as fluxbin_kv_advance gave them.  A token of a slot
- *             outside the cache is not moved; one whose source is outside becomes 0.
+ *             outside the cache is not moved; one whose source is outside becomes 0.  Those of one block are together in the call
+ *             (slots outside the cache may lie between them), at ascending offsets.
  *   d_path    DEVICE int32 [tokens]: ascending, entry j not below j; the first one that is not ends the path (fluxbin_draft_accept)
  * Requests must not share blocks of new tokens.  Errors: as fluxbin_kv_append.
  */

@@ -1,8 +1,9 @@
 // Moving the entries of accepted paths to the first slots of their step's tokens (fluxbin_kv_keep).
 //
 // A warp for each request, key head and side.  The path ascends and no entry of it moves up, so going along it in order never
-// writes an entry that is still to be read, and what is read for a block lies in that block or behind it; the scale of a block
-// is changed only after the last entry that goes there has been read.  Entries are read for the largest magnitude, several tokens
+// writes an entry that is still to be read, and what is read for a block lies in that block or behind it.  A block's tokens are one
+// run, or several where slots outside the cache or offsets that are left out lie between them: what a later run reads of the block
+// is still under the scale that the block had when its first run began.  Entries are read for the largest magnitude, several tokens
 // of each lane at once, and stored from registers, those of long runs read again.  Bound by a chain of dependent accesses
 // (start, path, slots, entries).  256 requests with 40 heads of 128: 30 us (read twice, one token of a lane after the other, 31).
 #include "fluxbin_cache.cuh"
@@ -61,6 +62,8 @@ __global__ void __launch_bounds__(kWarps * 32) keep_kernel(const __grid_constant
     }
     const int sub = lane / LANES, e0 = lane % LANES * 16;
     const float top_inverse = 1.f / Entry<FMT>::kTop;
+    int held = -1;                               // the block of the last run, and its scale before the first one there
+    float held_scale = 0.f;
     for (int j = begin; j < end;) {
         const int s0 = slots[j];
         if (s0 < 0 || s0 >= limit) {
@@ -79,7 +82,11 @@ __global__ void __launch_bounds__(kWarps * 32) keep_kernel(const __grid_constant
         }
         unsigned char *to = cells + block * a.c.block_stride;
         float *scale = scales + (long long)block * H;
-        const float before = offset ? *scale : 0.f;
+        const float now = *scale, before = offset ? now : 0.f;
+        if (block != held) {
+            held = block;
+            held_scale = now;
+        }
         // entries of `count` tokens of the run from `first` on, a lane's 16 of every AT_ONCE-th; -1 for a source outside the cache: zeros
         uint4 x[DEEP];
         float scale_of_x[DEEP];
@@ -91,7 +98,7 @@ __global__ void __launch_bounds__(kWarps * 32) keep_kernel(const __grid_constant
                 const int i = first + k * AT_ONCE + sub, f = __shfl_sync(0xffffffffu, from, i & 31);
                 const bool live = i < upto && f >= 0 && f < limit;
                 x[k] = live ? *reinterpret_cast<const uint4 *>(cells + f / bs * a.c.block_stride + f % bs * a.c.token_stride + e0) : make_uint4(0, 0, 0, 0);
-                scale_of_x[k] = live ? scales[(long long)(f / bs) * H] : 0.f;
+                scale_of_x[k] = !live ? 0.f : f / bs == held ? held_scale : scales[(long long)(f / bs) * H];
             }
         };
         unsigned most = 0;
