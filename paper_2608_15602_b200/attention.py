@@ -198,12 +198,8 @@ class NormedRotary:
     def __init__(self, rotary: Rotary, q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, eps: float = 1e-6):
         if not 0.0 < eps < 3e38:
             raise ValueError("eps: a positive number is wanted")
-        for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-            if w is not None and (w.dtype not in _TYPES or w.shape != (rotary.head_dim,) or not w.is_contiguous()):
-                raise ValueError(f"{what}: a contiguous tensor of {rotary.head_dim} gains in fp16, bf16 or fp32 is wanted")
-        if q_weight is not None and k_weight is not None and q_weight.dtype is not k_weight.dtype:
-            raise TypeError("q_weight, k_weight: one type is wanted")
         self.rotary, self.q_weight, self.k_weight, self.eps = rotary, q_weight, k_weight, float(eps)
+        self._gains(q_weight, k_weight)
 
     def apply(self, q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor, q_out: torch.Tensor | None = None,
               k_out: torch.Tensor | None = None, stream=None):
@@ -216,16 +212,32 @@ class NormedRotary:
             return _NormedAndTurned.apply(self, q, k, qw, kw, positions, stream)
         return self._apply(q, k, qw, kw, positions, q_out, k_out, stream)
 
+    def _gains(self, q_weight, k_weight):
+        """What gains have to be."""
+        for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            if w is not None and (w.dtype not in _TYPES or w.shape != (self.rotary.head_dim,) or not w.is_contiguous()):
+                raise ValueError(f"{what}: a contiguous tensor of {self.rotary.head_dim} gains in fp16, bf16 or fp32 is wanted")
+        if q_weight is not None and k_weight is not None and q_weight.dtype is not k_weight.dtype:
+            raise TypeError("q_weight, k_weight: one type is wanted")
+
     def _weights(self, q_weight, k_weight):
-        """(type, addresses)"""
-        here, kind, qp, kp = _device(), fluxbin.TYPE_FP32, 0, 0
-        if k_weight is not None:
-            kind, kp = _TYPES[k_weight.dtype], k_weight.data_ptr()
+        """(type, addresses); parameters may have been given another type or size since the last call"""
+        here, D, kind, qp, kp = _device(), self.rotary.head_dim, torch.float32, 0, 0
         if q_weight is not None:
-            kind, qp = _TYPES[q_weight.dtype], q_weight.data_ptr()
-        if (qp and q_weight.get_device() != here) or (kp and k_weight.get_device() != here):
-            raise ValueError("the gains have to lie on the current CUDA device")
-        return kind, qp, kp
+            kind, qp = q_weight.dtype, q_weight.data_ptr()
+            if q_weight.numel() != D or not q_weight.is_contiguous():
+                self._gains(q_weight, k_weight)
+            if q_weight.get_device() != here:
+                raise ValueError("the gains have to lie on the current CUDA device")
+        if k_weight is not None:
+            if k_weight.numel() != D or not k_weight.is_contiguous() or (qp and k_weight.dtype is not kind):
+                self._gains(q_weight, k_weight)
+            if k_weight.get_device() != here:
+                raise ValueError("the gains have to lie on the current CUDA device")
+            kind, kp = k_weight.dtype, k_weight.data_ptr()
+        if kind not in _TYPES:
+            self._gains(q_weight, k_weight)
+        return _TYPES[kind], qp, kp
 
     def _check(self, q):
         if q.dtype not in _TYPES:
