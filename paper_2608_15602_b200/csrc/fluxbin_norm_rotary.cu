@@ -21,7 +21,7 @@ using namespace fbd;
 namespace {
 
 constexpr int kThreads = 256, kMaxDim = 512;
-constexpr int kMaxParts = 148 * 4;               // CTAs of a backward pass
+constexpr int kMaxParts = 148 * 2;               // CTAs of a backward pass at most, each with its sums for the gradients of the gains
 
 struct NormSide {
     const void *x, *weight;
@@ -609,7 +609,7 @@ template <typename T, bool INTER, int LANES> cudaError_t run_wide(NormArgs a, bo
     // Two CTAs an SM are resident; the forward pass cuts the line finer, so that SMs that get more of the memory's rate do more of it (resident
     // CTAs once, twice, three, four times: 8191 tokens of 72 heads 54.5, 53.1, 54.0, 56.4 us; the backward pass, whose
     // sums cost each CTA something, 8190 tokens of 80 heads with the forward one: 149, 153, 160, 160)
-    const long long total = (long long)a.tokens * a.rounds, ctas = 148 * 2 * (backward ? 1 : 2), need = (total + WARPS - 1) / WARPS;
+    const long long total = (long long)a.tokens * a.rounds, ctas = backward ? kMaxParts : 148 * 4, need = (total + WARPS - 1) / WARPS;
     parts = (int)(need < ctas ? need : ctas);
     a.share = total / (parts * WARPS);
     a.over = total - a.share * parts * WARPS;
@@ -629,7 +629,7 @@ template <typename T> cudaError_t run(const NormArgs &a, bool backward, int &par
 {
     if (wide<T>(a, backward)) return a.rot.interleaved ? run_lanes<T, true>(a, backward, parts, s) : run_lanes<T, false>(a, backward, parts, s);
     const long long rows = (long long)a.tokens * (a.q.heads + a.k.heads), ctas = (rows + kThreads / 32 - 1) / (kThreads / 32);
-    const long long most = backward ? 148 * 2 : 148 * 8;
+    const long long most = backward ? kMaxParts : 148 * 8;
     parts = (int)(ctas < most ? ctas : most);
     if (backward) return launch(norm_any_backward_kernel<T>, dim3((unsigned)parts), kThreads, sizeof(float) * (kThreads / 32) * 2 * a.rot.head_dim, s, a);
     return launch(norm_any_kernel<T>, dim3((unsigned)parts), kThreads, 0, s, a);
