@@ -150,8 +150,15 @@ class Rotary:
         """q, k [tokens][heads][head_dim] turned to positions [tokens] (int32); outputs may be the inputs.  `inverse` turns
         back: the gradient of the turned heads with respect to q and k.  Returns (q_out, k_out), k_out None without k.  New
         outputs of heads that require a gradient carry it; outputs that were given are written without one."""
-        if q_out is None and k_out is None and (q.requires_grad or (k is not None and k.requires_grad)) and torch.is_grad_enabled():
-            return _Turned.apply(self, q, k, positions, inverse, stream)
+        if k is None:
+            k_out = None
+        wanted = q_out is None and q.requires_grad, k is not None and k_out is None and k.requires_grad
+        if (wanted[0] or wanted[1]) and torch.is_grad_enabled():
+            if q_out is None and k_out is None:
+                return _Turned.apply(self, q, k, positions, inverse, stream)
+            if wanted[0]:                                # (each by itself)
+                return _Turned.apply(self, q, None, positions, inverse, stream)[0], self._turn(k, None, positions, inverse, k_out, None, stream)[0]
+            return self._turn(q, None, positions, inverse, q_out, None, stream)[0], _Turned.apply(self, k, None, positions, inverse, stream)[0]
         return self._turn(q, k, positions, inverse, q_out, k_out, stream)
 
     def _turn(self, q, k, positions, inverse, q_out, k_out, stream):
@@ -207,9 +214,17 @@ class NormedRotary:
         (q_out, k_out), k_out None without k.  New outputs carry gradients (of the heads and of the gains, the first ones; they are
         formed on the stream that the gradients come on); outputs that were given are written without."""
         qw, kw = self.q_weight, self.k_weight
-        if q_out is None and k_out is None and torch.is_grad_enabled() and (
-                q.requires_grad or (k is not None and k.requires_grad) or (qw is not None and qw.requires_grad) or (kw is not None and kw.requires_grad)):
-            return _NormedAndTurned.apply(self, q, k, qw, kw, positions, stream)
+        if k is None:
+            k_out = None
+        if torch.is_grad_enabled():
+            wanted = (q_out is None and (q.requires_grad or (qw is not None and qw.requires_grad)),
+                      k is not None and k_out is None and (k.requires_grad or (kw is not None and kw.requires_grad)))
+            if wanted[0] or wanted[1]:
+                if q_out is None and k_out is None:
+                    return _NormedAndTurned.apply(self, q, k, qw, kw, positions, stream)
+                if wanted[0]:                            # (each by itself)
+                    return _NormedAndTurned.apply(self, q, None, qw, None, positions, stream)[0], self._apply(k, None, kw, None, positions, k_out, None, stream)[0]
+                return self._apply(q, None, qw, None, positions, q_out, None, stream)[0], _NormedAndTurned.apply(self, k, None, kw, None, positions, stream)[0]
         return self._apply(q, k, qw, kw, positions, q_out, k_out, stream)
 
     def _gains(self, q_weight, k_weight):
