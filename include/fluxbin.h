@@ -697,6 +697,9 @@ fluxbin_status_t fluxbin_draft_tree(int32_t batch, int32_t tokens, int32_t nodes
  *   d_workspace   fluxbin_kv_attend_tree_workspace_size bytes, zeroed once with fluxbin_workspace_init; it serves
  *                 fluxbin_kv_attend too, and smaller head dimensions; calls that share one must be ordered on a stream.
  * All else as fluxbin_kv_attend.  Errors: as there.
+ * From 17 rows a key head on (33 at head_dim 64 and 256) a CTA's warps wait for one another, for two seconds of its running time at most.
+ * A wait that runs out -- a fault of the machine -- makes the rows that the CTA worked at NaN, in d_out and d_lse; the call has returned
+ * FLUXBIN_OK by then, and the workspace stays good for the next one.
  */
 size_t fluxbin_kv_attend_tree_workspace_size(int32_t batch, int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim);
 fluxbin_status_t fluxbin_kv_attend_tree(const fluxbin_kv_cache_t *cache, int32_t dtype, int32_t batch, int32_t tokens,
@@ -706,6 +709,12 @@ fluxbin_status_t fluxbin_kv_attend_tree(const fluxbin_kv_cache_t *cache, int32_t
                                         const int32_t *d_block_table, int64_t block_table_stride, int32_t block_table_width,
                                         float scale, void *d_out, int64_t out_token, int64_t out_head, float *d_lse,
                                         void *d_workspace, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * Test hook for those waits: from now on, in this process, they take limit_ns at most (0: two seconds; more are RANGE), and, with
+ * withheld >= 0, whoever waits for that stage of a CTA's ring of tiles waits in vain.  (0, -1) sets everything back.
+ */
+fluxbin_status_t fluxbin_debug_tree_waits(int64_t limit_ns, int32_t withheld);
 
 /*
  * The path of each request's tree that the model itself would have answered, token after token (greedy): its first new token --

@@ -56,6 +56,8 @@ struct AttendArgs {
     const uint32_t *tree;                       // TREE: bit j of a token's words: it sees its request's j-th new token
     long long tree_stride;
     int tree_words;
+    unsigned wait_limit;                        // of the kernel for many rows, ns
+    int withheld;                               // a stage that is never full, for the test of it; -1
 };
 
 } // namespace fbd

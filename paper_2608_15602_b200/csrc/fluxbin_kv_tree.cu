@@ -8,6 +8,10 @@ namespace {
 // 148 and 82; 256 16 rows 56 and 77, 32 rows 87 and 88, 128 rows 293 and 93.
 int few_rows(int head_dim) { return head_dim == 128 ? 16 : 32; }
 
+// (what fluxbin_debug_tree_waits set)
+std::atomic<unsigned> g_wait_limit{kWaitLimit};
+std::atomic<int> g_withheld{-1};
+
 template <typename T> cudaError_t run_type(Args a, char *workspace, cudaStream_t s)
 {
     const long long rows = (long long)(a.q_heads / a.c.kv_heads) * ((a.tokens + a.batch - 1) / a.batch);
@@ -15,6 +19,8 @@ template <typename T> cudaError_t run_type(Args a, char *workspace, cudaStream_t
     a.arrived = (unsigned *)(workspace + kManyCountersAt);
     a.partial_lse = (float *)(workspace + kCounterBytes);
     a.partial = (float *)(workspace + kCounterBytes + kTreeLseBytes);
+    a.wait_limit = g_wait_limit.load(std::memory_order_relaxed);
+    a.withheld = g_withheld.load(std::memory_order_relaxed);
     const bool bf16 = !std::is_same<T, __half>::value;
     return a.c.head_dim == 64 ? launch_tree_64(a, bf16, s) : a.c.head_dim == 128 ? launch_tree_128(a, bf16, s) : launch_tree_256(a, bf16, s);
 }
@@ -54,5 +60,13 @@ extern "C" fluxbin_status_t fluxbin_kv_attend_tree(const fluxbin_kv_cache_t *cac
                     (float *)((char *)d_workspace + kCounterBytes + kLseBytes), (const uint32_t *)d_tree, tree_stride, tree_words};
     cudaStream_t s = (cudaStream_t)cuda_stream;
     FBD_CUDA((dtype == FLUXBIN_TYPE_FP16 ? run_type<__half>(a, (char *)d_workspace, s) : run_type<__nv_bfloat16>(a, (char *)d_workspace, s)));
+    return FLUXBIN_OK;
+}
+
+extern "C" fluxbin_status_t fluxbin_debug_tree_waits(int64_t limit_ns, int32_t withheld)
+{
+    if (limit_ns < 0 || limit_ns > (int64_t)kWaitLimit || withheld < -1) return FLUXBIN_ERR_RANGE;
+    g_wait_limit.store(limit_ns ? (unsigned)limit_ns : kWaitLimit, std::memory_order_relaxed);
+    g_withheld.store(withheld, std::memory_order_relaxed);
     return FLUXBIN_OK;
 }

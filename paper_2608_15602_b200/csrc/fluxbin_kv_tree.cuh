@@ -20,6 +20,7 @@
 // while a tile's probabilities are formed.
 //
 // Every wait has a limit; one that runs out (a fault of the machine) ends the waiting of the whole CTA, and its jobs' rows become NaN.
+// Products that are under way then end before the unit's memory is given back, and the counters of cut jobs are as after any other call.
 #ifndef FLUXBIN_KV_TREE_CUH
 #define FLUXBIN_KV_TREE_CUH
 
@@ -33,7 +34,9 @@ constexpr int kRows = 128;                   // of a tile: the lanes of the matr
 constexpr int kTreeJobCost = 8;
 constexpr int kMetaRing = 32;                // tiles whose scales are kept
 constexpr float kValueLag = 1048576.f;       // 2^20: value scales may pass the largest one met so far by this much before O is rescaled
-constexpr unsigned long long kWaitLimit = 2000000000ull;         // ns
+// A wait's limit, in ns of a CTA that runs: between two looks at the clock no more counts than kWaitStep (the rest is time in which the
+// device was another context's)
+constexpr unsigned kWaitLimit = 2000000000u, kWaitStep = 10000000u;
 
 template <int D> struct Tree {
     static constexpr int kTokens = D == 256 ? 32 : 64;           // of a tile
@@ -66,33 +69,37 @@ __device__ __forceinline__ bool try_wait(uint32_t b, unsigned parity)
     asm volatile("{ .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n }" : "=r"(ok) : "r"(b), "r"(parity) : "memory");
     return ok;
 }
-__device__ __forceinline__ unsigned long long now_ns()
+__device__ __forceinline__ unsigned now_ns()         // modulo 2^32
 {
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    unsigned t;
+    asm volatile("mov.u32 %0, %globaltimer_lo;" : "=r"(t));
     return t;
 }
-// false once a wait of this CTA has run out
-__device__ __forceinline__ bool wait_for(unsigned long long &barrier, unsigned parity, int &failed)
+// Whether a wait of this CTA has run out, and what each may take
+struct Waits { int failed; unsigned limit; };
+// false once one has run out
+__device__ __forceinline__ bool wait_for(unsigned long long &barrier, unsigned parity, Waits &waits)
 {
     const uint32_t b = shared_address(&barrier);
 #pragma unroll 1
     for (int i = 0; i < 64; ++i)
         if (try_wait(b, parity)) return true;
-    const unsigned long long begin = now_ns();
-    for (;;) {
+    for (unsigned spent = 0, last = now_ns();;) {
 #pragma unroll 1
         for (int i = 0; i < 64; ++i)
             if (try_wait(b, parity)) return true;
-        if (*(volatile int *)&failed) return false;
-        if (now_ns() - begin > kWaitLimit) {
-            *(volatile int *)&failed = 1;
+        if (*(volatile int *)&waits.failed) return false;
+        const unsigned now = now_ns();
+        spent += min(now - last, kWaitStep);
+        last = now;
+        if (spent > waits.limit) {
+            *(volatile int *)&waits.failed = 1;
             return false;
         }
     }
 }
 // the same for a whole warp, which goes on together
-__device__ __forceinline__ bool wait_together(unsigned long long &barrier, unsigned parity, int &failed) { return __all_sync(0xffffffffu, wait_for(barrier, parity, failed)); }
+__device__ __forceinline__ bool wait_together(unsigned long long &barrier, unsigned parity, Waits &waits) { return __all_sync(0xffffffffu, wait_for(barrier, parity, waits)); }
 template <int ID, int THREADS> __device__ __forceinline__ void sync_some() { asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(THREADS) : "memory"); }
 
 __device__ __forceinline__ void unit_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -216,7 +223,8 @@ template <int D> struct TreeShared {
     long long place[Tree<D>::kConverters][2][32];                // of each converting warp: where 16 tokens lie
     uint32_t none[Tree<D>::kConverters][2];                      // which of them are in no block (and read the cache's first one instead)
     long long scan[32], before;
-    int request, last, failed;
+    int request, last;
+    Waits waits;
     uint32_t columns;
     Walk<D> walk[Tree<D>::kThreads / 32];        // of each warp: in registers only while it is looked at
 };
@@ -305,7 +313,7 @@ __device__ __forceinline__ void convert_role(const Args &a, TreeShared<D> &sm, u
         if (tiles == 0) continue;
         const unsigned parity = jobs & 1;
         // ---- what the job before the last left is done with
-        if (jobs >= 2) ok = ok && wait_together(sm.ended[parity], (jobs / 2 - 1) & 1, sm.failed);
+        if (jobs >= 2) ok = ok && wait_together(sm.ended[parity], (jobs / 2 - 1) & 1, sm.waits);
         for (int i = tid; i < kRows * (D / 32); i += C::kConverters * 32) sm.nan[parity][i / (D / 32)][i % (D / 32)] = 0;
         if (tid == 0) sm.any_nan[parity] = 0;
         sync_some<1, C::kConverters * 32>();
@@ -437,7 +445,7 @@ __device__ __forceinline__ void convert_role(const Args &a, TreeShared<D> &sm, u
                     }
                 }
             }
-            ok = ok && wait_together(sm.free[stage], stage_phase, sm.failed);
+            ok = ok && wait_together(sm.free[stage], stage_phase, sm.waits);
             const uint32_t to = stages + stage * C::kStageBytes + to0;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -488,12 +496,12 @@ __device__ __forceinline__ void product_role(const Args &a, TreeShared<D> &sm, u
     while (ok && walk.next(a, lane)) {
         const int tiles = __shfl_sync(0xffffffffu, walk.j.tiles, 0);
         if (tiles == 0) continue;
-        if (!VALUES) ok = wait_together(sm.q_full, jobs & 1, sm.failed);
+        if (!VALUES) ok = wait_together(sm.q_full, jobs & 1, sm.waits);
         for (int t = 0; ok && t < tiles; ++t, turn.next()) {
             const uint32_t place = unit + C::kS + turn.place * C::kTokens;
             const uint64_t b = operands + (turn.stage * C::kStageBytes >> 4);
             if constexpr (!VALUES) {
-                ok = (asked < C::kPlaces || wait_together(sm.pv_done[turn.place], turn.place_phase ^ 1, sm.failed)) && wait_together(sm.full[turn.stage], turn.stage_phase, sm.failed);
+                ok = (asked < C::kPlaces || wait_together(sm.pv_done[turn.place], turn.place_phase ^ 1, sm.waits)) && wait_together(sm.full[turn.stage], turn.stage_phase, sm.waits);
                 if (!ok) break;
                 unit_after_sync();
                 if (elected()) {
@@ -503,7 +511,7 @@ __device__ __forceinline__ void product_role(const Args &a, TreeShared<D> &sm, u
                 }
                 asked += asked < C::kPlaces;
             } else {
-                ok = wait_together(sm.p_full[turn.place], turn.place_phase, sm.failed);
+                ok = wait_together(sm.p_full[turn.place], turn.place_phase, sm.waits);
                 if (!ok) break;
                 unit_after_sync();
                 const uint32_t o = unit + C::kO + turn.group * D;
@@ -521,11 +529,10 @@ __device__ __forceinline__ void product_role(const Args &a, TreeShared<D> &sm, u
         }
         ++jobs;
     }
-    if (!ok) {                                   // what is under way has to end before the unit's memory is given back
-        if (elected()) unit_commit(sm.drained[VALUES]);
-        int own = 0;
-        wait_together(sm.drained[VALUES], 0, own);
-    }
+    // what was issued ends before the unit's memory is given back, whoever's wait may have run out
+    if (elected()) unit_commit(sm.drained[VALUES]);
+    Waits own = {0, kWaitLimit};
+    wait_together(sm.drained[VALUES], 0, own);
 }
 
 __device__ __forceinline__ float max_of(float x, float y, float z)
@@ -608,7 +615,7 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
         const int t_first = (group - (int)it) & (GROUPS - 1);    // tiles go to the groups in turn, from job to job
         for (int t = 0; t < tiles; ++t, turn.next()) {
             if (GROUPS == 2 && t % 2 != t_first) continue;
-            ok = ok && wait_together(sm.s_full[turn.place], turn.place_phase, sm.failed);
+            ok = ok && wait_together(sm.s_full[turn.place], turn.place_phase, sm.waits);
             if (!ok) break;
             if (live) {
                 unit_after_sync();
@@ -697,7 +704,7 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
                 }
                 if (t >= GROUPS && __any_sync(0xffffffffu, rescale != 1.f)) {
                     const unsigned before = it + t - GROUPS;     // the last tile that went to the same sums
-                    ok = wait_together(sm.pv_done[before % C::kPlaces], before / C::kPlaces & 1, sm.failed);
+                    ok = wait_together(sm.pv_done[before % C::kPlaces], before / C::kPlaces & 1, sm.waits);
                     unit_after_sync();
                     const uint32_t o = unit + C::kO + group * D;
 #pragma unroll 1
@@ -722,11 +729,11 @@ __device__ __forceinline__ void softmax_role(const Args &a, TreeShared<D> &sm, W
         if (row == 0) sm.vref[group] = vref;
         if (tiles > 0) {                       // (the products end in order)
             const unsigned n = it + tiles - 1;
-            ok = ok && wait_together(sm.pv_done[n % C::kPlaces], n / C::kPlaces & 1, sm.failed);
+            ok = ok && wait_together(sm.pv_done[n % C::kPlaces], n / C::kPlaces & 1, sm.waits);
         }
         sync_some<2, C::kSoft>();
         unit_after_sync();
-        ok = ok && !*(volatile int *)&sm.failed;                 // (the other group's waits count too)
+        ok = ok && !*(volatile int *)&sm.waits.failed;                 // (the other group's waits count too)
         const bool whole = j.p0 == 0 && j.p1 == rq.pieces;
         const long long slot = share * 2 + (j.p0 == 0);
         // partial results lie element by element with the rows side by side, four elements together
@@ -897,7 +904,7 @@ __global__ void __launch_bounds__(Tree<D>::kThreads, 1) tree_attend_kernel(const
     }
     if (tid == 0) {
         for (int i = 0; i < C::kStages; ++i) {
-            barrier_init(sm.full[i], C::kConverters);
+            barrier_init(sm.full[i], C::kConverters + (i == a.withheld));
             barrier_init(sm.free[i], 1);
         }
         barrier_init(sm.q_full, C::kSoft / 32);
@@ -910,7 +917,8 @@ __global__ void __launch_bounds__(Tree<D>::kThreads, 1) tree_attend_kernel(const
             barrier_init(sm.ended[i], 1);
             barrier_init(sm.drained[i], 1);
         }
-        sm.failed = 0;
+        sm.waits.failed = 0;
+        sm.waits.limit = a.wait_limit;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }

@@ -47,7 +47,8 @@ EXPORTS = ["fluxbin_packed_size", "fluxbin_validate", "fluxbin_pack_host", "flux
            "fluxbin_rotary_frequencies", "fluxbin_rotary", "fluxbin_kv_validate", "fluxbin_kv_append", "fluxbin_kv_read",
            "fluxbin_kv_attend_workspace_size", "fluxbin_kv_attend", "fluxbin_kv_advance", "fluxbin_norm_rotary",
            "fluxbin_norm_rotary_backward", "fluxbin_norm_rotary_backward_workspace_size", "fluxbin_draft_tree", "fluxbin_draft_accept",
-           "fluxbin_kv_attend_tree", "fluxbin_kv_attend_tree_workspace_size", "fluxbin_kv_keep", "fluxbin_call_words"]
+           "fluxbin_kv_attend_tree", "fluxbin_kv_attend_tree_workspace_size", "fluxbin_debug_tree_waits", "fluxbin_kv_keep",
+           "fluxbin_call_words"]
 
 TYPE_FP16, TYPE_FP32, TYPE_BF16 = 0, 1, 2
 CACHE_INT8, CACHE_E4M3 = 0, 1
@@ -162,6 +163,7 @@ def _lib():
         lib.fluxbin_kv_attend_tree_workspace_size.restype, lib.fluxbin_kv_attend_tree_workspace_size.argtypes = sz, [i32] * 5
         lib.fluxbin_kv_attend_tree.restype = ctypes.c_int
         lib.fluxbin_kv_attend_tree.argtypes = [vp, i32, i32, i32] + heads + [vp, vp, vp, i64, i32, vp, i64, i32, f32, vp, i64, i64, vp, vp, sz, vp]
+        lib.fluxbin_debug_tree_waits.restype, lib.fluxbin_debug_tree_waits.argtypes = ctypes.c_int, [i64, i32]
         lib.fluxbin_kv_keep.restype, lib.fluxbin_kv_keep.argtypes = ctypes.c_int, [vp, i32, i32, vp, vp, vp, vp]
         lib.fluxbin_call_words.restype, lib.fluxbin_call_words.argtypes = ctypes.c_int, [i32, ctypes.c_char_p]
         _LIB = lib
@@ -554,6 +556,11 @@ def kv_attend_tree_status(*args) -> int:
 
 def kv_attend_tree_workspace_size(batch: int, tokens: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
     return int(_lib().fluxbin_kv_attend_tree_workspace_size(batch, tokens, q_heads, kv_heads, head_dim))
+
+
+def debug_tree_waits(limit_ns: int = 0, withheld: int = -1) -> None:
+    """Test hook: the limit of tree attention's waits, and a stage that is never full.  No arguments set both back."""
+    _check(_lib().fluxbin_debug_tree_waits(limit_ns, withheld), "fluxbin_debug_tree_waits")
 
 
 def kv_keep_status(*args) -> int:
