@@ -14,7 +14,7 @@ elsewhere still uses it, and is recorded on the current stream too, so it may be
 have to be ready on `stream` and are the caller's to keep until it is through, as with any torch call on another stream.
 
 Where query and key heads are normed first, NormedRotary(rope, q_weight, k_weight) takes rope's place; the cache then gets keys
-that are turned already.  A step that checks a tree of drafted tokens at once:
+that are turned already, and rounded to their type once more than those that append() turns on the way, in fp32.  A step that checks a tree of drafted tokens at once:
 
     tree = DraftTree(parents, step.query_start, step.lengths, nodes=64)   # masks and positions, once for all layers
     q, k = normed.apply(q, k, tree.positions)
@@ -461,7 +461,7 @@ class BlockTables:
         if _row_stride(table) < table.shape[1]:
             raise ValueError("table: rows that do not overlap are wanted (they are written)")
         self.table, self.free, self.block_tokens = table, free, block_tokens
-        self._tokens = self._sets = None
+        self._tokens, self._sets = None, {}              # the size of the last step; two sets of outputs of each of the last two sizes
         self._captured = []                              # sets that graphs write: as long as this object, whatever else it is asked
         self._free = _int32(free, free.shape[0], "free")
         self.batch, self.max_blocks = table.shape
@@ -476,7 +476,7 @@ class BlockTables:
     def advance(self, lengths: torch.Tensor, new_tokens: torch.Tensor, num_free: torch.Tensor, tokens: int, stream=None) -> SimpleNamespace:
         """One step: `new_tokens` int32 [batch] tokens to add (> 0) or drop (< 0), `tokens` the sum of those to add.  Returns
         lengths, num_free, granted, query_start, positions, slots, requests: int32 tensors that belong to this object, two
-        sets in turn, so that a step's outputs can be the next step's inputs; keep a copy of what has to live longer.  A step
+        sets in turn for each size, so that a step's outputs can be the next step's inputs; keep a copy of what has to live longer.  A step
         captured into a graph has a set of its own, which lives as long as this object."""
         B = self.batch
         lp, np_, fp = _int32(lengths, B, "lengths"), _int32(new_tokens, B, "new_tokens"), _int32(num_free, 1, "num_free")
@@ -486,12 +486,16 @@ class BlockTables:
             step = self._outputs(tokens, stream)
             self._captured.append(step)
         else:
-            if tokens != self._tokens:                   # (a decode loop keeps one size)
-                self._tokens, self._sets = tokens, [self._outputs(tokens, stream), self._outputs(tokens, stream)]
-            step, other = self._sets
-            self._sets = [other, step]
+            sets = self._sets.get(tokens)                # (a decode loop has one size, one that drops drafted tokens has 0 besides)
+            if sets is None:
+                if len(self._sets) == 2:
+                    self._sets = {self._tokens: self._sets[self._tokens]}
+                sets = self._sets[tokens] = [self._outputs(tokens, stream), self._outputs(tokens, stream)]
+            self._tokens = tokens
+            step = sets[0]
             if step.first <= lp < step.last or step.first <= np_ < step.last or step.first <= fp < step.last:
-                step = self._sets[1] = self._outputs(tokens, stream)  # an input of this step is an output of the last but one: keep that
+                step = self._outputs(tokens, stream)     # an input of this step is an output of the last but one: keep that
+            sets[0], sets[1] = sets[1], step
         on = _stream(stream)
         if on != step.made_on:                           # a set may be dropped while another stream still writes it
             step.num_free.record_stream(torch.cuda.current_stream() if stream is None else stream)
