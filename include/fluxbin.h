@@ -516,7 +516,8 @@ fluxbin_status_t fluxbin_rotary(const fluxbin_rotary_t *rotary, int32_t dtype, i
 /*
  * Norms of query and key heads with the rotary's turn in the same pass:  y = turn_p(w * x * r),  r = (mean(x^2) + eps)^(-1/2)
  * over the head_dim elements of a head; one gain w for all query heads and one for all key heads.  Everything between x and y
- * is fp32, y is rounded once.
+ * is fp32, y is rounded once.  (Keys that go into a cache are so rounded before fluxbin_kv_append quantises them; those that it turns
+ * itself are not.)
  *   d_q_weight, d_k_weight   DEVICE [head_dim] of weight_dtype, or NULL: 1
  *   eps                      > 0 and finite
  * The rest as fluxbin_rotary (k may be NULL, outputs may be the inputs themselves).  Errors: as fluxbin_rotary.

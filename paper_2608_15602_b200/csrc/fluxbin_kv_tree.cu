@@ -3,9 +3,17 @@
 
 namespace {
 
-// Rows that share a key head in an average request up to which the kernel for few rows is ahead.  16 requests of 8190 tokens, that kernel
-// against the other: head dimension 128 16 rows 94 us and 115, 24 rows 160 and 116; 64 16 rows 49 and 82, 32 rows 78 and 82, 64 rows
-// 148 and 82; 256 16 rows 56 and 77, 32 rows 87 and 88, 128 rows 293 and 93.
+// Rows that share a key head in an average request up to which the kernel for few rows is taken.  That kernel / the other, us, int8 and
+// bf16 (e4m3 and fp16: that kernel 3 to 8 % less, the other up to 3 % more):
+//                                        16 requests of 8190      2000 tokens   500          100          one of 16000
+//   64 query heads on 8 of 128, 16 rows  92 / 114                 43 / 45       26 / 28      20 / 17      35 / 43
+//                               24       161 / 114                60 / 45       36 / 28      20 / 17      41 / 44
+//   24 on 6 of 64, 32 rows               75 / 81                  35 / 33       19 / 21      13 / 15      25 / 31
+//                  48                    101 / 81                 42 / 34       26 / 22      13 / 15      26 / 32
+//   16 on 2 of 256, 32 rows              90 / 91                  40 / 49       23 / 33      14 / 24      36 / 235
+//                   48                   124 / 92                 50 / 51       24 / 34      14 / 25      37 / 244
+// Where the rule is wrong: 64 heads on 8 of 256 (32 rows 310 / 214), a request alone on two key heads of 256 (its 74 parts are joined one
+// after the other, 256 elements of a row by one thread), and batches that mix wide trees with single tokens, since it goes by the average.
 int few_rows(int head_dim) { return head_dim == 128 ? 16 : 32; }
 
 // (what fluxbin_debug_tree_waits set)
