@@ -14,7 +14,8 @@ elsewhere still uses it, and is recorded on the current stream too, so it may be
 have to be ready on `stream` and are the caller's to keep until it is through, as with any torch call on another stream.
 
 Where query and key heads are normed first, NormedRotary(rope, q_weight, k_weight) takes rope's place; the cache then gets keys
-that are turned already, and rounded to their type once more than those that append() turns on the way, in fp32.  A step that checks a tree of drafted tokens at once:
+that are turned already, and rounded to their type once more than those that append() turns on the way, in fp32.  A step that
+checks a tree of drafted tokens at once:
 
     tree = DraftTree(parents, step.query_start, step.lengths, nodes=64)   # masks and positions, once for all layers
     q, k = normed.apply(q, k, tree.positions)

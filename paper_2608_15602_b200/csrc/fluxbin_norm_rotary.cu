@@ -12,7 +12,8 @@
 // shared memory over all that a thread sees, then over the CTA, then by a second launch over the CTAs: no atomics, the same sums each time.
 // Bound by memory, with instructions close behind (a value at a time instead of two 109 us for the backward pass of 8190 tokens of 80
 // heads of 128 in bf16, two 85: 503 MB, 5.9 TB/s).  8191 tokens of 72 heads forward: 53 us, 302 MB, 5.7 TB/s.  In fp32 the same 80 heads take
-// 167 us forward and 271 backward (4.0 and 3.7 TB/s): half as many bytes of a head are on their way.
+// 167 us forward and 271 backward (4.0 and 3.7 TB/s): as many bytes on their way, but a lane's 16-byte copies lie 32 bytes apart, so every sector
+// is asked for twice.
 #include "fluxbin_rotary.cuh"
 
 #include <atomic>
